@@ -310,6 +310,106 @@ hill_status hill_score_noalloc(const hill_desc* desc, const void* q, const void*
                                const int32_t* lens, hill_score_mode mode, float* scores,
                                float* accum, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * A cache of bounded size.  The calls above leave every token in the cache
+ * and pass a kept set along; a program that evicts for good keeps a cache of
+ * `cap` slots instead, whose slots are taken again by accumulated attention
+ * weight (the importance of Sec. 4.1, summed over the steps).  Per decode
+ * step and layer: hill_cache_insert puts the new token in, then
+ * hill_window_attn attends over what is held and adds the step's weights to
+ * accum.  Both have a form for a cache held in 4 bits.
+ *
+ * State, caller-owned, per row = per sequence, or with kvh != 0 per
+ * (sequence, KV head), each KV head then keeping tokens of its own:
+ *   seen   [B] or [B][Hkv] int32         tokens inserted so far, 0 at first; the
+ *                                        row holds min(seen, cap) tokens, in the
+ *                                        slots from 0 on
+ *   pos    [B][cap] or [B][Hkv][cap] int32     the position (0-based count of the
+ *                                        sequence's tokens) that a slot holds
+ *   accum  [B][cap] or [B][Hkv][cap] float32   the slot's accumulated weight
+ * seen serves as `lens` of the attention: lens is clamped to [0, cap].
+ *
+ * 4-bit caches: a row of d = 128 channels is 64 bytes of codes (byte i:
+ * channel 2i in the low half, 2i + 1 in the high half) with a scale and a
+ * minimum in desc's 16-bit type, value = min + scale * code:
+ *   k4, v4  [B][Hkv][cap][64] uint8, dense, 16-byte aligned;
+ *   params  [B][Hkv][cap32][4] 16-bit (K scale, K min, V scale, V min), cap32 =
+ *           cap rounded up to 32, dense, 16-byte aligned.
+ * Finite rows give scale = (max - min) / 15 rounded to the 16-bit type and
+ * code = (x - min) / scale rounded to nearest even, clamped to [0, 15] (0 when
+ * the scale rounds to 0).  desc gives the sizes and the type; its K and V
+ * strides are not used for 4-bit caches.
+ *
+ * These calls read all their inputs after the dependency wait (see above). */
+
+/* Bytes of workspace of hill_window_attn and hill_window_attn_q4, with or
+ * without an accum.  Returns 0 for an invalid descriptor. */
+size_t hill_window_workspace_bytes(const hill_desc* desc, int32_t with_accum);
+
+/* Decode attention over the visible part of the cache: of the n = lens[row]
+ * tokens held (clamped to [0, cap]) the first `sinks` slots and the newest
+ * `window`, slots j < n with j < sinks or j >= n - window (Eq. 1 restricted to
+ * them):
+ *   out[b][h] = sum_j p_j V[b][g(h)][j],  p = softmax_j(q_h . K[b][g(h)][j] / sqrt(d)).
+ * A window of cap or more shows everything; with nothing visible the output
+ * is zero.  sinks and window count slots, so they are for caches in order of
+ * position (ones that have not evicted).  If accum is given, accum[row][j] +=
+ * sum of p_j over the row's query heads, for visible j only.
+ * lens and accum: [B] and [B][cap], kvh != 0: [B][Hkv] and [B][Hkv][cap] (B * Hkv
+ * <= 2048).  What lies in slots that are not visible does not matter, NaN
+ * included.  q, K, V as in the calls above; out 16-byte aligned. */
+hill_status hill_window_attn(const hill_desc* desc, const void* q, const void* k_cache, const void* v_cache,
+                             const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh, float* accum,
+                             float* out, void* ws, size_t ws_bytes, void* stream);
+
+/* hill_window_attn over a 4-bit cache: K and V are the values that the rows
+ * stand for (not rounded to 16 bits). */
+hill_status hill_window_attn_q4(const hill_desc* desc, const void* q, const uint8_t* k4, const uint8_t* v4,
+                                const void* params, const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh,
+                                float* accum, float* out, void* ws, size_t ws_bytes, void* stream);
+
+/* New tokens of every sequence, in order of position. */
+typedef struct {
+  const void* k;              /* [B][Hkv][max_new][d] in desc's type          */
+  const void* v;              /* the same                                     */
+  int64_t k_sb, k_sh, k_sn;   /* element strides, multiples of 8; d contiguous */
+  int64_t v_sb, v_sh, v_sn;
+  int32_t max_new;            /* new tokens per sequence, at most             */
+  const int32_t* count;       /* [B] how many of them (clamped), or NULL: all */
+  const float* weight;        /* [B][max_new] (kvh: [B][Hkv][max_new]) their
+                                 first accumulated weights, or NULL: 0        */
+} hill_new_rows;
+
+/* Inserts the new tokens: token i of a row gets position seen[row] + i and a
+ * slot, its rows are written there for the row's KV heads, pos and accum of
+ * the slot are set, and seen[row] grows by the number of new tokens.
+ * While slots are free, tokens take them in order.  The e tokens that find none
+ * take, in ascending order, the slots that are given up: among the held slots
+ * with a position p, sinks <= p < seen + new - recent (seen before the call),
+ * the last e in the order (accum descending, slot ascending).  So the first
+ * `sinks` tokens of the sequence and the `recent` newest, the new ones among
+ * them, stay.  slots [B][max_new] (kvh: [B][Hkv][max_new]) receives every new
+ * token's slot, -1 past a sequence's own.
+ * sinks + max(recent, max_new) must not exceed cap.  If pos names fewer slots
+ * that may go than are needed (positions that no insert made), the remaining
+ * tokens are dropped (slot -1) and HILL_ERR_DEVICE is recorded.  -0.0 ranks
+ * equal to +0.0; weights must be finite. */
+hill_status hill_cache_insert(const hill_desc* desc, const hill_new_rows* rows, void* k_cache, void* v_cache,
+                              int32_t* seen, int32_t* pos, float* accum, int32_t sinks, int32_t recent, int32_t kvh,
+                              int32_t* slots, void* stream);
+
+/* hill_cache_insert into a 4-bit cache. */
+hill_status hill_cache_insert_q4(const hill_desc* desc, const hill_new_rows* rows, uint8_t* k4, uint8_t* v4,
+                                 void* params, int32_t* seen, int32_t* pos, float* accum, int32_t sinks,
+                                 int32_t recent, int32_t kvh, int32_t* slots, void* stream);
+
+/* The values of slots [row_begin[b], row_end[b]) of every KV head of a 4-bit
+ * cache, rounded to desc's type, into 16-bit caches of desc's strides (for the
+ * calls that read those); max_rows bounds row_end - row_begin over b. */
+hill_status hill_cache_read_q4(const hill_desc* desc, const uint8_t* k4, const uint8_t* v4, const void* params,
+                               const int32_t* row_begin, const int32_t* row_end, int32_t max_rows, void* k_cache,
+                               void* v_cache, void* stream);
+
 /* Number of kernels this library has launched (or recorded into a CUDA graph
  * under stream capture) in this process so far, over all devices.  Lets a
  * caller count the kernels one call or one captured graph contains. */

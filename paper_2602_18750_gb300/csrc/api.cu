@@ -94,17 +94,19 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_tiled() {
   return fn;
 }
 
-// Tiled tensor map of the key cache for hill_score_kernel: dimension 0 is the
-// head dimension (contiguous, box 64 = 128 bytes, 128-byte swizzle); the
-// token, KV-head and sequence dimensions follow in increasing stride order
-// (so token-major caches work too), with a box of 32 tokens.
-hill_status make_kmap(const hill_desc* d, const void* k, ScoreArgs* a) {
+// Tiled tensor map of a 16-bit cache (K or V: p with strides sb, sh, sn):
+// dimension 0 is the head dimension (contiguous, box 64 = 128 bytes, 128-byte
+// swizzle); the token, KV-head and sequence dimensions follow in increasing
+// stride order (so token-major caches work too), with a box of 32 tokens.
+// where[0], [1], [2]: the map's dimensions of token, KV head and sequence.
+hill_status make_cache_map(const hill_desc* d, const void* p, int64_t sb, int64_t sh, int64_t sn, CUtensorMap* map,
+                           int where[3]) {
   auto fn = encode_tiled();
   if (!fn) return HILL_ERR_CUDA;
   struct Dim {
     int64_t n, stride;
     int which;  // 0 token, 1 head, 2 sequence
-  } v[3] = {{d->capacity, d->k_sn, 0}, {d->num_kv_heads, d->k_sh, 1}, {d->batch, d->k_sb, 2}};
+  } v[3] = {{d->capacity, sn, 0}, {d->num_kv_heads, sh, 1}, {d->batch, sb, 2}};
   std::stable_sort(v, v + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
   cuuint64_t gdim[4] = {(cuuint64_t)kHeadDim, 1, 1, 1};
   cuuint64_t gstr[3];
@@ -116,21 +118,41 @@ hill_status make_kmap(const hill_desc* d, const void* k, ScoreArgs* a) {
     int64_t st = v[i].stride;
     if (v[i].n <= 1) st = std::max<int64_t>(st, i ? (int64_t)gstr[i - 1] / 2 : kHeadDim);
     gstr[i] = (cuuint64_t)(st * 2);
-    if (v[i].which == 0) {
-      box[i + 1] = 32;
-      a->kdim_tok = i + 1;
-    } else if (v[i].which == 1) {
-      a->kdim_head = i + 1;
-    } else {
-      a->kdim_seq = i + 1;
-    }
+    where[v[i].which] = i + 1;
+    if (v[i].which == 0) box[i + 1] = 32;
   }
   for (int i = 0; i < 3; ++i)
     if (gstr[i] == 0 || (gstr[i] & 15)) return HILL_ERR_UNSUPPORTED;
   const CUtensorMapDataType dt =
       d->dtype == HILL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-  CUresult r = fn(&a->kmap, dt, 4, const_cast<void*>(k), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  CUresult r = fn(map, dt, 4, const_cast<void*>(p), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HILL_OK : HILL_ERR_UNSUPPORTED;
+}
+
+// The key cache for hill_score_kernel.
+hill_status make_kmap(const hill_desc* d, const void* k, ScoreArgs* a) {
+  int where[3];
+  const hill_status s = make_cache_map(d, k, d->k_sb, d->k_sh, d->k_sn, &a->kmap, where);
+  a->kdim_tok = where[0];
+  a->kdim_head = where[1];
+  a->kdim_seq = where[2];
+  return s;
+}
+
+// Codes of a 4-bit cache [B][Hkv][cap][64]: box = one row (64-byte swizzle) x
+// 32 tokens.  Rows past the capacity read as zeros.
+hill_status make_q4_map(const hill_desc* d, const void* codes, CUtensorMap* map) {
+  auto fn = encode_tiled();
+  if (!fn) return HILL_ERR_CUDA;
+  const cuuint64_t row = kHeadDim / 2, cap = (cuuint64_t)std::max(d->capacity, 1);
+  cuuint64_t gdim[3] = {row, cap, (cuuint64_t)std::max<int64_t>((int64_t)d->batch * d->num_kv_heads, 1)};
+  cuuint64_t gstr[2] = {row, cap * row};
+  cuuint32_t box[3] = {(cuuint32_t)row, 32, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(codes), gdim, gstr, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? HILL_OK : HILL_ERR_UNSUPPORTED;
 }
 
@@ -934,3 +956,237 @@ extern "C" hill_status hill_score_noalloc(const hill_desc* desc, const void* q, 
   return run_score(desc, q, k_cache, lens, mode, scores, accum, static_cast<unsigned char*>(scratch), L, di,
                    static_cast<cudaStream_t>(stream));
 }
+
+// ---------------------------------------------------------------------------
+// A cache of bounded size: attention over its visible part, inserts that
+// evict, 4-bit rows (window.cu, insert.cu).
+namespace hill {
+namespace {
+
+struct WindowLayout {
+  size_t part_o, part_ml, table, stats, logits, total;
+  int passes, heads;   // of query heads per KV head; at most so many in one
+};
+
+int cdiv(int a, int b) { return (a + b - 1) / b; }
+
+// Workspace regions of hill_window_attn(_q4); with_accum: room for the logits too.
+WindowLayout window_layout(const hill_desc* d, bool with_accum, int sms) {
+  WindowLayout L{};
+  const size_t B = d->batch, H = d->num_q_heads;
+  const int G = d->num_q_heads / d->num_kv_heads;
+  L.heads = window_heads_per_pass(G);
+  L.passes = cdiv(G, L.heads);
+  // the same for both formats: the larger number of warps
+  const size_t parts = (size_t)sms * std::max(window_warps(true, L.heads), window_warps(false, L.heads)) * 2 * L.heads;
+  size_t off = 0;
+  L.part_o = off;
+  off += align_up(parts * kHeadDim * sizeof(float));
+  L.part_ml = off;
+  off += align_up(parts * sizeof(float2));
+  L.table = off;
+  off += align_up((window_max_rows() + 1) * sizeof(int));
+  L.stats = off;
+  if (with_accum) off += align_up(B * H * sizeof(float2));
+  L.logits = off;
+  if (with_accum) off += align_up(B * H * (size_t)cap32_of(d) * sizeof(float));
+  L.total = off + kAlign;
+  return L;
+}
+
+// What hill_window_attn and its 4-bit form share.
+hill_status window_attn(const hill_desc* desc, const void* q, const void* k, const void* v, const void* params,
+                        const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh, float* accum, float* out,
+                        void* ws, size_t ws_bytes, void* stream) {
+  hill_status s = check_desc(desc);
+  if (s != HILL_OK) return s;
+  if (!q || !k || !v || !lens || !out || sinks < 0 || window < 0) return HILL_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (params && !aligned16(params)))
+    return HILL_ERR_INVALID_ARG;
+  if (kvh && (int64_t)desc->batch * desc->num_kv_heads > window_max_rows()) return HILL_ERR_UNSUPPORTED;
+  // the list of tiles is numbered in 32 bits
+  const int G = desc->num_q_heads / desc->num_kv_heads;
+  if ((int64_t)desc->batch * desc->num_kv_heads * cdiv(G, window_heads_per_pass(G)) * cdiv(desc->capacity, 32) >= INT32_MAX)
+    return HILL_ERR_UNSUPPORTED;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
+  const WindowLayout L = window_layout(desc, accum != nullptr, di.sms);
+  if (!ws || ws_bytes < L.total) return HILL_ERR_WORKSPACE;
+  if (desc->batch == 0) return HILL_OK;
+  unsigned char* base = ws_base(ws);
+  WindowArgs a{};
+  if (params) {
+    s = make_q4_map(desc, k, &a.kmap);
+    if (s == HILL_OK) s = make_q4_map(desc, v, &a.vmap);
+  } else {
+    int where[3];
+    s = make_cache_map(desc, k, desc->k_sb, desc->k_sh, desc->k_sn, &a.kmap, where);
+    a.kdim_tok = where[0];
+    a.kdim_head = where[1];
+    if (s == HILL_OK) s = make_cache_map(desc, v, desc->v_sb, desc->v_sh, desc->v_sn, &a.vmap, where);
+    a.vdim_tok = where[0];
+    a.vdim_head = where[1];
+  }
+  if (s != HILL_OK) return s;
+  a.params = static_cast<const uint2*>(params);
+  a.q = q;
+  a.q_sb = desc->q_sb;
+  a.q_sh = desc->q_sh;
+  a.lens = lens;
+  a.B = desc->batch;
+  a.H = desc->num_q_heads;
+  a.Hkv = desc->num_kv_heads;
+  a.G = G;
+  a.cap = desc->capacity;
+  a.cap32 = cap32_of(desc);
+  a.kvh = kvh ? 1 : 0;
+  a.sinks = sinks;
+  a.window = window;
+  a.passes = L.passes;
+  a.out = out;
+  a.accum = accum;
+  a.part_o = reinterpret_cast<float*>(base + L.part_o);
+  a.part_ml = reinterpret_cast<float2*>(base + L.part_ml);
+  a.table = reinterpret_cast<int*>(base + L.table);
+  if (accum) {
+    a.stats = reinterpret_cast<float2*>(base + L.stats);
+    a.logits = reinterpret_cast<float*>(base + L.logits);
+  }
+  a.err = di.err;
+  int kernels = 0;
+  const cudaError_t e =
+      launch_window_attn(a, desc->dtype, params != nullptr, di.sms, static_cast<cudaStream_t>(stream), &kernels);
+  return from_cuda(counted(e, kernels));
+}
+
+hill_status cache_insert(const hill_desc* desc, const hill_new_rows* n, void* k, void* v, uint8_t* k4, uint8_t* v4,
+                         void* params, int32_t* seen, int32_t* pos, float* accum, int32_t sinks, int32_t recent,
+                         int32_t kvh, int32_t* slots, void* stream) {
+  hill_status s = check_desc(desc);
+  if (s != HILL_OK) return s;
+  if (!n || n->max_new < 0 || sinks < 0 || recent < 0 || !seen || !pos || !accum) return HILL_ERR_INVALID_ARG;
+  if (n->max_new > 0 && (!n->k || !n->v || !slots || !aligned16(n->k) || !aligned16(n->v))) return HILL_ERR_INVALID_ARG;
+  if (!stride_ok(n->k_sb) || !stride_ok(n->k_sh) || !stride_ok(n->k_sn) || !stride_ok(n->v_sb) ||
+      !stride_ok(n->v_sh) || !stride_ok(n->v_sn))
+    return HILL_ERR_INVALID_ARG;
+  // a full cache has room for the new tokens beside what stays
+  if ((int64_t)sinks + std::max(recent, n->max_new) > desc->capacity) return HILL_ERR_INVALID_ARG;
+  if (desc->batch == 0 || n->max_new == 0) return HILL_OK;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
+  InsertArgs a{};
+  a.k_new = n->k;
+  a.v_new = n->v;
+  a.kn_sb = n->k_sb;
+  a.kn_sh = n->k_sh;
+  a.kn_sn = n->k_sn;
+  a.vn_sb = n->v_sb;
+  a.vn_sh = n->v_sh;
+  a.vn_sn = n->v_sn;
+  a.k = k;
+  a.v = v;
+  a.k_sb = desc->k_sb;
+  a.k_sh = desc->k_sh;
+  a.k_sn = desc->k_sn;
+  a.v_sb = desc->v_sb;
+  a.v_sh = desc->v_sh;
+  a.v_sn = desc->v_sn;
+  a.k4 = k4;
+  a.v4 = v4;
+  a.params = static_cast<uint2*>(params);
+  a.seen = seen;
+  a.pos = pos;
+  a.accum = accum;
+  a.n_new = n->count;
+  a.w_new = n->weight;
+  a.slots = slots;
+  a.B = desc->batch;
+  a.Hkv = desc->num_kv_heads;
+  a.cap = desc->capacity;
+  a.cap32 = cap32_of(desc);
+  a.kvh = kvh ? 1 : 0;
+  a.max_new = n->max_new;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.err = di.err;
+  int kernels = 0;
+  const cudaError_t e = launch_insert(a, desc->dtype, static_cast<cudaStream_t>(stream), &kernels);
+  return from_cuda(counted(e, kernels));
+}
+
+}  // namespace
+}  // namespace hill
+
+extern "C" {
+
+size_t hill_window_workspace_bytes(const hill_desc* desc, int32_t with_accum) {
+  if (check_desc(desc) != HILL_OK) return 0;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return 0;
+  return window_layout(desc, with_accum != 0, di.sms).total;
+}
+
+hill_status hill_window_attn(const hill_desc* desc, const void* q, const void* k_cache, const void* v_cache,
+                             const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh, float* accum,
+                             float* out, void* ws, size_t ws_bytes, void* stream) {
+  return window_attn(desc, q, k_cache, v_cache, nullptr, lens, sinks, window, kvh, accum, out, ws, ws_bytes, stream);
+}
+
+hill_status hill_window_attn_q4(const hill_desc* desc, const void* q, const uint8_t* k4, const uint8_t* v4,
+                                const void* params, const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh,
+                                float* accum, float* out, void* ws, size_t ws_bytes, void* stream) {
+  if (!params) return HILL_ERR_INVALID_ARG;
+  return window_attn(desc, q, k4, v4, params, lens, sinks, window, kvh, accum, out, ws, ws_bytes, stream);
+}
+
+hill_status hill_cache_insert(const hill_desc* desc, const hill_new_rows* rows, void* k_cache, void* v_cache,
+                              int32_t* seen, int32_t* pos, float* accum, int32_t sinks, int32_t recent, int32_t kvh,
+                              int32_t* slots, void* stream) {
+  if (!k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache)) return HILL_ERR_INVALID_ARG;
+  return cache_insert(desc, rows, k_cache, v_cache, nullptr, nullptr, nullptr, seen, pos, accum, sinks, recent, kvh,
+                      slots, stream);
+}
+
+hill_status hill_cache_insert_q4(const hill_desc* desc, const hill_new_rows* rows, uint8_t* k4, uint8_t* v4,
+                                 void* params, int32_t* seen, int32_t* pos, float* accum, int32_t sinks,
+                                 int32_t recent, int32_t kvh, int32_t* slots, void* stream) {
+  if (!k4 || !v4 || !params || !aligned16(k4) || !aligned16(v4) || !aligned16(params)) return HILL_ERR_INVALID_ARG;
+  return cache_insert(desc, rows, nullptr, nullptr, k4, v4, params, seen, pos, accum, sinks, recent, kvh, slots,
+                      stream);
+}
+
+hill_status hill_cache_read_q4(const hill_desc* desc, const uint8_t* k4, const uint8_t* v4, const void* params,
+                               const int32_t* row_begin, const int32_t* row_end, int32_t max_rows, void* k_cache,
+                               void* v_cache, void* stream) {
+  hill_status s = check_desc(desc);
+  if (s != HILL_OK) return s;
+  if (!k4 || !v4 || !params || !row_begin || !row_end || max_rows < 0 || !k_cache || !v_cache)
+    return HILL_ERR_INVALID_ARG;
+  if (!aligned16(k4) || !aligned16(v4) || !aligned16(params) || !aligned16(k_cache) || !aligned16(v_cache))
+    return HILL_ERR_INVALID_ARG;
+  if (desc->batch == 0 || desc->capacity == 0 || max_rows == 0) return HILL_OK;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
+  ReadQ4Args a{};
+  a.k4 = k4;
+  a.v4 = v4;
+  a.params = static_cast<const uint2*>(params);
+  a.row_begin = row_begin;
+  a.row_end = row_end;
+  a.k = k_cache;
+  a.v = v_cache;
+  a.k_sb = desc->k_sb;
+  a.k_sh = desc->k_sh;
+  a.k_sn = desc->k_sn;
+  a.v_sb = desc->v_sb;
+  a.v_sh = desc->v_sh;
+  a.v_sn = desc->v_sn;
+  a.B = desc->batch;
+  a.Hkv = desc->num_kv_heads;
+  a.cap = desc->capacity;
+  a.cap32 = cap32_of(desc);
+  return from_cuda(counted(launch_read_q4(a, desc->dtype, std::min(max_rows, desc->capacity),
+                                          static_cast<cudaStream_t>(stream)), 1));
+}
+
+}  // extern "C"

@@ -147,6 +147,63 @@ struct AttnArgs {
   unsigned* err;
 };
 
+// Attention over the visible part of a cache (window.cu).
+struct WindowArgs {
+  // 16 bits: 4-D maps of K and V, 128-byte swizzle, box = 64 dims x 32 tokens;
+  // 4 bits: 3-D maps (64 bytes, cap, B * Hkv) of the codes, 64-byte swizzle, box = 64 bytes x 32 tokens
+  CUtensorMap kmap, vmap;
+  int kdim_tok, kdim_head, vdim_tok, vdim_head;   // which dimension of a 4-D map holds token and KV head
+  const uint2* params;   // 4 bits: [B][Hkv][cap32] (K scale, K min, V scale, V min)
+  const void* q;
+  int64_t q_sb, q_sh;
+  const int32_t* lens;   // [B], kvh: [B][Hkv]
+  int B, H, Hkv, G, cap, cap32, kvh;
+  int sinks, window;
+  int passes;            // of at most window_heads_per_pass(G) query heads
+  float* out;            // [B][H][d]
+  float* accum;          // [B][cap], kvh: [B][Hkv][cap], or NULL
+  float* logits;         // [B][H][cap32] base-2 logits, or NULL (no accum)
+  float2* stats;         // [B][H] (max, 1 / sum), or NULL (no accum)
+  float* part_o;         // [warps][2][heads per pass][d] partials: of the pair a warp's part begins in, and ends in
+  float2* part_ml;       // [warps][2][heads per pass]
+  int* table;            // [rows + 1] first tile of each row of lens in the list
+  unsigned* err;
+};
+
+// Inserts into a cache of fixed size (insert.cu).
+struct InsertArgs {
+  const void* k_new;     // [B][Hkv][max_new][d], strides kn_*
+  const void* v_new;
+  int64_t kn_sb, kn_sh, kn_sn, vn_sb, vn_sh, vn_sn;
+  void* k;               // 16-bit caches, or NULL
+  void* v;
+  int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+  uint8_t* k4;           // 4-bit caches [B][Hkv][cap][64], or NULL
+  uint8_t* v4;
+  uint2* params;         // [B][Hkv][cap32]
+  int32_t* seen;         // [rows] tokens inserted so far (+=)
+  int32_t* pos;          // [rows][cap]
+  float* accum;          // [rows][cap]
+  const int32_t* n_new;  // [B] or NULL: max_new
+  const float* w_new;    // [rows][max_new] or NULL: 0
+  int32_t* slots;        // [rows][max_new]
+  int B, Hkv, cap, cap32, kvh, max_new, sinks, recent;
+  unsigned* err;
+};
+
+// 4-bit rows [row_begin[b], row_end[b]) as 16-bit values.
+struct ReadQ4Args {
+  const uint8_t* k4;
+  const uint8_t* v4;
+  const uint2* params;
+  const int32_t* row_begin;
+  const int32_t* row_end;
+  void* k;
+  void* v;
+  int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+  int B, Hkv, cap, cap32;
+};
+
 // Raise a kernel's dynamic shared-memory limit to `bytes` on the current
 // device if it is not there yet; `cache` (64 entries, one per device) records
 // what was set, so that steady-state launches -- including ones under stream
@@ -246,5 +303,16 @@ cudaError_t launch_sparse_attn_clusters(const AttnArgs& a, int dtype, int sms, c
 // The attention kernel for one pass of G heads per KV head, and (combine)
 // the merge of split partials over all heads.
 cudaError_t launch_sparse_attn(const AttnArgs& a, int dtype, int G, int grid, bool combine, cudaStream_t st);
+
+
+// window.cu
+int window_heads_per_pass(int G);
+int window_warps(bool q4, int heads_per_pass);   // per CTA, one CTA per SM
+int window_max_rows();
+cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms, cudaStream_t st, int* kernels);
+
+// insert.cu
+cudaError_t launch_insert(const InsertArgs& a, int dtype, cudaStream_t st, int* kernels);
+cudaError_t launch_read_q4(const ReadQ4Args& a, int dtype, int max_rows, cudaStream_t st);
 
 }  // namespace hill

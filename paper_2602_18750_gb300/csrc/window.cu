@@ -1,0 +1,883 @@
+// window.cu -- decode attention over the visible part of a cache: the first
+// `sinks` tokens and the newest `window` of each row (Eq. 1 restricted to
+// them), from 16-bit K/V or from a 4-bit cache, with the attention weights
+// optionally added to the running importance (Sec. 4.1 column sums).
+//
+// Three kernels, the last only with an importance:
+//  hill_window_attn_kernel   streams K and V once.  The work is a list of
+//    tiles of 32 tokens, ordered (sequence, KV head, pass of query heads, tile);
+//    every warp of the grid owns one contiguous part of it and brings its tiles
+//    into a ring of its own in shared memory by TMA.  A warp that holds all
+//    tiles of a (sequence, KV head, pass) writes the output; the others leave
+//    (max, sum, o) partials.
+//  hill_window_combine_kernel merges those partials.
+//  hill_window_accum_kernel  adds sum_h 2^(z - m_h) / l_h to the importance,
+//    from the logits that the first kernel stored.
+//
+// Mathematics of a tile, 32 tokens as two row blocks of 16 (mma m16n8k16):
+//  S = K q^T with the tokens as rows and the pass's query heads as columns.
+//  The weights p = 2^(z - m) of a running maximum m are then already laid out
+//  by column, and an 8x8 transpose of each block (movmatrix) makes them the
+//  column operand of O^T += V^T p, whose rows are the 128 channels.  m is
+//  raised only when a logit passes it by 2^8 (the accumulators then shrink by
+//  the same factor), so the usual tile takes one vote and no shuffles.
+//  p enters as a 16-bit high part plus its 16-bit residual, so that the output
+//  keeps float32-like accuracy; m sits 2^7 below the maximum at which it was set, so that
+//  fp16 holds both parts without underflow for weights down to 2^-32 of the
+//  largest.  With at most 4 query heads the residuals are columns 4 to 7 of
+//  the same product; with more they are a second one.
+//
+// 4-bit rows hold value = min + scale * code.  With an integer zero point z0
+// near -min / scale this is scale * (code - z0) + rest, the rest below half a
+// scale where the row has both signs: nothing large cancels.  code - z0 enters
+// mma as fp16 integers, the scale and rest in float32: z = scale (q . (code -
+// z0)) + rest sum(q), and o = sum p scale (code - z0) + sum p rest, where p scale / R
+// is the 16-bit operand and R a power of two at or above every scale so far.
+// The query is multiplied by a power of two that puts its largest element at 2^14
+// (bf16 queries fit fp16 that way).  (Codes left as fp16 subnormals, which
+// takes masks alone, lost 10 bits: mma aligns a subnormal's products by the
+// exponent of its unnormalised form, and the output was off by 1e-4.)
+//
+// Bound by HBM: 512 bytes per token and KV head in 16 bits, 136 in 4 bits.
+#include <algorithm>
+#include <type_traits>
+
+#include "hill_internal.h"
+
+namespace hill {
+namespace {
+
+constexpr int kT = 32;                    // tokens per tile
+constexpr int kBox = kT * 128;            // 16-bit: 32 rows x 64 dims
+constexpr int kQ4Codes = kT * 64;         // 4-bit: 32 rows of codes
+constexpr int kQ4Slot = 2 * kQ4Codes + kT * 8;   // K codes, V codes, params
+constexpr int kMaxRows = 2048;            // rows of lens
+
+template <bool Q4>
+struct Cfg {
+  static constexpr int kSlot = Q4 ? 2 * kQ4Codes + 512 : 2 * kBox;   // 16-bit: a K or a V tile
+  static constexpr int kSlots = 3;
+  static constexpr int smem(int warps) { return warps * kSlots * kSlot + 1024; }   // + alignment slack
+};
+
+// The visible tiles of a row of n tokens: [0, sink) and from tile `first` on.
+struct Tiles {
+  int n, start;        // tokens; first token of the window
+  int sink, first, count;
+  __device__ __forceinline__ Tiles() {}
+  __device__ __forceinline__ Tiles(int len, int cap, int sinks, int window) {
+    n = len < 0 ? 0 : min(len, cap);
+    start = max(0, n - window);
+    first = start / kT;
+    const int shown = min(sinks, start);   // sinks outside the window
+    const int win = start < n ? (n + kT - 1) / kT - first : 0;
+    sink = (shown + kT - 1) / kT;
+    if (win > 0) sink = min(sink, first);
+    count = sink + win;
+  }
+  __device__ __forceinline__ int token(int i) const { return (i < sink ? i : first + i - sink) * kT; }
+};
+
+// The part of the list that warp w of nw (at most as many as tiles) owns, and
+// the warp that owns item x.
+__device__ __forceinline__ int first_item(int w, int total, int nw) { return (int)((int64_t)w * total / nw); }
+__device__ __forceinline__ int warp_of(int x, int total, int nw) {
+  return (int)((((int64_t)x + 1) * nw - 1) / total);
+}
+
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+  return d;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar,
+                                            uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(dst),
+      "l"(tmap), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy)
+      : "memory");
+}
+
+// Four registers of two (code - zero point) each, as fp16 integers, from a
+// word of eight codes: codes (0, 4), (1, 5), (2, 6), (3, 7).  A code put under
+// the exponent of 1024 reads as 1024 + code (one place up: 1024 + 16 code),
+// exactly, and one fp16 operation takes the offset off, exactly.  z1024: 1024 +
+// the zero points of the two halves.
+__device__ __forceinline__ void codes_to_half(uint32_t w, __half2 z1024, uint32_t (&x)[4]) {
+  const __half2 one16 = __float2half2_rn(0.0625f);
+  const __half2 z64 = __hsub2(__float2half2_rn(960.f), z1024);   // -(64 + zero point)
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t v = h ? w >> 8 : w;
+    uint32_t lo = (v & 0x000f000fu) | 0x64006400u, hi = (v & 0x00f000f0u) | 0x64006400u;
+    const __half2 a = __hsub2(*reinterpret_cast<__half2*>(&lo), z1024);
+    const __half2 b = __hfma2(*reinterpret_cast<__half2*>(&hi), one16, z64);
+    x[2 * h] = *reinterpret_cast<const uint32_t*>(&a);
+    x[2 * h + 1] = *reinterpret_cast<const uint32_t*>(&b);
+  }
+}
+
+// The zero point of a row, the integer of [0, 15] nearest to -min / scale (any
+// would be right, this one leaves the smallest rest), 1024 added, as fp16 in
+// the high half over the row's scale in the low half; and the rest min + scale * zero point.
+template <int DT>
+__device__ __forceinline__ uint32_t zero_point(uint32_t param, float& rest) {
+  const float2 p = unpack2<DT>(param);
+  const float z = rintf(fminf(fmaxf(__fdividef(-p.y, p.x), 0.f), 15.f));
+  rest = fmaf(p.x, z, p.y);
+  return (param & 0xffffu) | ((uint32_t)__half_as_ushort(__float2half_rn(1024.f + z)) << 16);
+}
+
+__device__ __forceinline__ __half2 high_twice(uint32_t v) {   // the high half in both halves
+  const uint32_t d = __byte_perm(v, 0u, 0x3232);
+  return *reinterpret_cast<const __half2*>(&d);
+}
+
+__device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
+  return v;
+}
+
+// A power of two at or above s >= 0 (at least 2^-125, at most 2^127).
+__device__ __forceinline__ float pow2_above(float s) {
+  const uint32_t e = __float_as_uint(s) >> 23;
+  return __uint_as_float(min(max(e + 1, 2u), 254u) << 23);
+}
+
+template <int I> using Int = std::integral_constant<int, I>;
+template <bool I> using Bool = std::integral_constant<bool, I>;
+
+// Where the warp stands in the list.
+struct Cursor {
+  int row, pair, tile;   // pair: KV head and pass within the row
+  Tiles t;
+};
+
+template <int DT, bool Q4, int HC, int NW>
+__global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __grid_constant__ WindowArgs a) {
+  using C = Cfg<Q4>;
+  constexpr int kN = HC == 16 ? 2 : 1;         // column blocks of 8 heads
+  constexpr bool kFold = HC == 4;              // residuals in columns 4 to 7
+  extern __shared__ unsigned char wsm[];
+  __shared__ __align__(8) uint64_t s_bar[NW * C::kSlots];
+  __shared__ int s_start[kMaxRows + 1];        // first item of each row
+  __shared__ int s_sum[NW];
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int grp = lane >> 2, tig = lane & 3;
+  const uint32_t ring = ((smem_addr(wsm) + 1023u) & ~1023u) + warp * C::kSlots * C::kSlot;
+  const uint32_t bars = smem_addr(s_bar + warp * C::kSlots);
+  if (lane == 0) {
+    for (int i = 0; i < C::kSlots; ++i) mbar_init(bars + 8 * i, 1);
+    fence_barrier_init();
+    prefetch_tmap(&a.kmap);
+    prefetch_tmap(&a.vmap);
+  }
+  const int rows = a.kvh ? a.B * a.Hkv : a.B;
+  const int pairs = (a.kvh ? 1 : a.Hkv) * a.passes;   // (KV head, pass) of a row
+
+  pdl_wait();
+
+  // the list: every CTA scans the rows' tiles
+  auto row_tiles = [&](int r) { return Tiles(a.lens[r], a.cap, a.sinks, a.window); };
+  int total = 0;
+  for (int r0 = 0; r0 < rows; r0 += NW * 32) {
+    const int r = r0 + (int)threadIdx.x;
+    const int mine = r < rows ? row_tiles(r).count * pairs : 0;
+    int inc = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += y;
+    }
+    if (lane == 31) s_sum[warp] = inc;
+    __syncthreads();
+    int before = total;
+    for (int w = 0; w < NW; ++w) {
+      if (w < warp) before += s_sum[w];
+      total += s_sum[w];
+    }
+    if (r < rows) s_start[r] = before + inc - mine;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) s_start[rows] = total;
+  __syncthreads();
+  if (blockIdx.x == 0)
+    for (int r = threadIdx.x; r <= rows; r += NW * 32) a.table[r] = s_start[r];
+  // parts are numbered across the CTAs first, so that few tiles spread over all SMs
+  const int nw = min((int)gridDim.x * NW, total), w = warp * gridDim.x + blockIdx.x;
+  if (w >= nw) return;
+  const int i0 = first_item(w, total, nw), i1 = first_item(w + 1, total, nw);
+
+  const uint64_t policy = l2_evict_first_policy();
+  auto locate = [&](int item) {
+    Cursor c;
+    int lo = 0, hi = rows - 1;   // the last row that starts at or before item
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_start[mid] <= item) lo = mid;
+      else hi = mid - 1;
+    }
+    c.row = lo;
+    c.t = row_tiles(lo);
+    const int x = item - s_start[lo];
+    c.pair = x / c.t.count;
+    c.tile = x - c.pair * c.t.count;
+    return c;
+  };
+  auto advance = [&](Cursor& c) {   // only while an item follows
+    if (++c.tile < c.t.count) return;
+    c.tile = 0;
+    if (++c.pair < pairs) return;
+    c.pair = 0;
+    do {
+      ++c.row;
+    } while (s_start[c.row + 1] == s_start[c.row]);
+    c.t = row_tiles(c.row);
+  };
+  auto seq_of = [&](const Cursor& c) { return a.kvh ? c.row / a.Hkv : c.row; };
+  auto head_of = [&](const Cursor& c) { return a.kvh ? c.row % a.Hkv : c.pair / a.passes; };
+
+  // ------------------------------------------------------------ the ring
+  // A stage is a slot's content: a tile (4 bits), or a K or a V tile in turn.
+  constexpr int kPer = Q4 ? 1 : 2;
+  const int stages = (i1 - i0) * kPer;
+  Cursor cur = locate(i0), ahead = cur;
+  int issued = 0, slot_in = 0;
+  auto issue = [&] {   // the next stage, if there is one
+    if (issued >= stages) return;
+    if (lane == 0) {
+      const uint32_t dst = ring + slot_in * C::kSlot, bar = bars + 8 * slot_in;
+      const int b = seq_of(ahead), g = head_of(ahead), j = ahead.t.token(ahead.tile);
+      if (Q4) {
+        mbar_arrive_expect_tx(bar, kQ4Slot);
+        tma_load_3d(dst, &a.kmap, 0, j, b * a.Hkv + g, bar, policy);
+        tma_load_3d(dst + kQ4Codes, &a.vmap, 0, j, b * a.Hkv + g, bar, policy);
+        bulk_g2s(dst + 2 * kQ4Codes, a.params + ((int64_t)(b * a.Hkv + g) * a.cap32 + j), kT * 8, bar, policy);
+      } else {
+        const bool v = issued & 1;
+        const void* map = v ? &a.vmap : &a.kmap;
+        const int dt = v ? a.vdim_tok : a.kdim_tok, dh = v ? a.vdim_head : a.kdim_head;
+        const int c1 = dt == 1 ? j : (dh == 1 ? g : b);
+        const int c2 = dt == 2 ? j : (dh == 2 ? g : b);
+        const int c3 = dt == 3 ? j : (dh == 3 ? g : b);
+        mbar_arrive_expect_tx(bar, 2 * kBox);
+        tma_load_4d(dst, map, 0, c1, c2, c3, bar, policy);
+        tma_load_4d(dst + kBox, map, 64, c1, c2, c3, bar, policy);
+      }
+    }
+    ++issued;
+    slot_in = slot_in + 1 == C::kSlots ? 0 : slot_in + 1;
+    if (issued % kPer == 0 && issued < stages) advance(ahead);
+  };
+  int slot = 0, phase = 0, taken = 0;
+  bool alive = true;
+  auto arrive = [&] { alive = alive && mbar_wait(bars + 8 * slot, phase, a.err); };
+  auto next_slot = [&] {
+    ++taken;
+    if (++slot == C::kSlots) {
+      slot = 0;
+      phase ^= 1;
+    }
+  };
+  for (int i = 0; i < C::kSlots; ++i) issue();
+
+  // ------------------------------------------------------------ state of a pair
+  uint32_t qf[8][kN][2];                 // query heads as the column operand
+  float o[8][kN][4];                     // O^T: channels x heads
+  float m[kN][2], l[kN][2];              // columns 2 tig, 2 tig + 1; l of this lane's tokens only
+  float cz[kN][2], cq[kN][2], mp[kN][2]; // 4 bits: factor of q . (code - z0); of the K rest; sum p V rest
+  float R = 0.f, Rinv = 0.f;             // 4 bits: the power of two above the V scales
+  int b = 0, g = 0, h0 = 0, Gn = 0;      // the pair's sequence, KV head, first query head and heads
+
+  auto begin_pair = [&] {
+    b = seq_of(cur);
+    g = head_of(cur);
+    const int pass = cur.pair % a.passes;
+    h0 = g * a.G + pass * HC;
+    Gn = min(HC, a.G - pass * HC);
+#pragma unroll
+    for (int nt = 0; nt < kN; ++nt) {
+      const int col = kFold ? (grp & 3) : nt * 8 + grp;
+      const uint16_t* row = reinterpret_cast<const uint16_t*>(a.q) + (int64_t)b * a.q_sb + (int64_t)(h0 + col) * a.q_sh;
+      const bool there = col < Gn;
+      if (!Q4) {
+#pragma unroll
+        for (int kk = 0; kk < 8; ++kk) {
+          qf[kk][nt][0] = there ? *reinterpret_cast<const uint32_t*>(row + kk * 16 + 2 * tig) : 0u;
+          qf[kk][nt][1] = there ? *reinterpret_cast<const uint32_t*>(row + kk * 16 + 2 * tig + 8) : 0u;
+        }
+      } else {
+        // channels 32 tig .. 32 tig + 31, in the order in which codes_to_half takes the codes of a word
+        float top = 0.f, sum = 0.f;
+        uint4 raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          raw[i] = there ? *reinterpret_cast<const uint4*>(row + 32 * tig + 8 * i) : uint4{0u, 0u, 0u, 0u};
+          float f[8];
+          to_float8<DT>(raw[i], f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            top = fmaxf(top, fabsf(f[e]));
+            sum += f[e];
+          }
+        }
+#pragma unroll
+        for (int s = 1; s < 4; s <<= 1) {
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+          sum += __shfl_xor_sync(0xffffffffu, sum, s);
+        }
+        // up = 2^(14 - e) for a largest element of [2^e, 2^(e+1))
+        const int e = (int)((__float_as_uint(top) >> 23) & 0xffu);
+        const int ue = min(max(141 - e + 127, 1), 240);
+        const float up = __uint_as_float((uint32_t)ue << 23);
+        const float back = __uint_as_float((uint32_t)(254 - ue) << 23);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float f[8];
+          to_float8<DT>(raw[i], f);
+          qf[2 * i][nt][0] = pack2<0>(f[0] * up, f[4] * up);
+          qf[2 * i][nt][1] = pack2<0>(f[1] * up, f[5] * up);
+          qf[2 * i + 1][nt][0] = pack2<0>(f[2] * up, f[6] * up);
+          qf[2 * i + 1][nt][1] = pack2<0>(f[3] * up, f[7] * up);
+        }
+        const float cf = back * kLog2eInvSqrtD, qs = sum * kLog2eInvSqrtD;
+#pragma unroll
+        for (int e2 = 0; e2 < 2; ++e2) {
+          const int from = (kFold ? ((2 * tig + e2) & 3) : 2 * tig + e2) * 4;
+          cz[nt][e2] = __shfl_sync(0xffffffffu, cf, from);
+          cq[nt][e2] = __shfl_sync(0xffffffffu, qs, from);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m[nt][e] = kNegHuge;
+        l[nt][e] = 0.f;
+        mp[nt][e] = 0.f;
+      }
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[ct][nt][e] = 0.f;
+    }
+    R = Rinv = 0.f;
+  };
+
+  // ------------------------------------------------------------ one tile
+  // full: all its tokens are visible
+  auto tile = [&](auto full_tag) {
+    constexpr bool kFull = decltype(full_tag)::value;
+    const int j0 = cur.t.token(cur.tile);
+    auto visible = [&](int r) {
+      const int j = j0 + r;
+      return kFull || (j < cur.t.n && (j < a.sinks || j >= cur.t.start));
+    };
+    float z[2][kN][4];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[mt][nt][e] = 0.f;
+
+    arrive();
+    const uint32_t base = ring + slot * C::kSlot;
+    float smax = 0.f;           // 4 bits: this lane's V scale
+    float vs[2][2], vr[2][2];   // V scale, rest of tokens 16 mt + grp (+ 8)
+    uint32_t vz[2][2];          // 1024 + V zero points of tokens 16 mt (+ 8) + 2 tig, 2 tig + 1
+    if constexpr (Q4) {
+      // each lane prepares a token's parameters and leaves them for the warp, in the
+      // places of the ring that no copy writes
+      auto note = [&](int r) { return ring + (r >> 4) * C::kSlot + kQ4Slot + (r & 15) * 16; };
+      {
+        uint2 pr = lds64(base + 2 * kQ4Codes + lane * 8);
+        if (!visible(lane)) pr = uint2{0u, 0u};
+        uint4 n;
+        float rest;
+        n.x = zero_point<DT>(pr.x, rest);
+        n.y = __float_as_uint(rest);
+        n.z = zero_point<DT>(pr.y, rest);
+        n.w = __float_as_uint(rest);
+        sts128(note(lane), n);
+        smax = unpack2<DT>(pr.y).x;
+        __syncwarp();
+      }
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        uint4 wv[2];
+        float ks[2], kr[2];
+        __half2 kz[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int r = mt * 16 + e * 8 + grp;
+          wv[e] = lds128(base + r * 64 + ((tig ^ ((r >> 1) & 3)) << 4));
+          const uint4 n = lds128(note(r));
+          ks[e] = unpack2<DT>(n.x).x;
+          kz[e] = high_twice(n.x);
+          kr[e] = __uint_as_float(n.y);
+          vs[mt][e] = unpack2<DT>(n.z).x;
+          const __half2 z2 = high_twice(n.z);
+          vz[mt][e] = transpose8(*reinterpret_cast<const uint32_t*>(&z2));
+          vr[mt][e] = __uint_as_float(n.w);
+        }
+        const uint32_t x[4] = {wv[0].x, wv[0].y, wv[0].z, wv[0].w}, y[4] = {wv[1].x, wv[1].y, wv[1].z, wv[1].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t u[4], v[4];
+          codes_to_half(x[i], kz[0], u);
+          codes_to_half(y[i], kz[1], v);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t A[4] = {u[2 * h], v[2 * h], u[2 * h + 1], v[2 * h + 1]};
+#pragma unroll
+            for (int nt = 0; nt < kN; ++nt) mma_16816<0>(z[mt][nt], A, qf[2 * i + h][nt][0], qf[2 * i + h][nt][1]);
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            z[mt][nt][e] = fmaf(z[mt][nt][e] * ks[e >> 1], cz[nt][e & 1], kr[e >> 1] * cq[nt][e & 1]);
+      }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+          const int r = mt * 16 + (lane & 15), ch = kk * 2 + (lane >> 4);
+          uint32_t A[4];
+          ldmatrix_x4(base + (ch >> 3) * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4), A);
+#pragma unroll
+          for (int nt = 0; nt < kN; ++nt) mma_16816<DT>(z[mt][nt], A, qf[kk][nt][0], qf[kk][nt][1]);
+        }
+      __syncwarp();
+      next_slot();
+      issue();
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[mt][nt][e] *= kLog2eInvSqrtD;
+    }
+    if (!kFull) {
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!visible(mt * 16 + (e >> 1) * 8 + grp))
+#pragma unroll
+            for (int nt = 0; nt < kN; ++nt) z[mt][nt][e] = -INFINITY;
+    }
+    if (a.logits) {
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int col = nt * 8 + 2 * tig + e;
+          if (col >= Gn) continue;
+          float* to = a.logits + ((int64_t)b * a.H + h0 + col) * a.cap32 + j0 + grp;
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt) {
+            to[mt * 16] = z[mt][nt][e];
+            to[mt * 16 + 8] = z[mt][nt][2 + e];
+          }
+        }
+    }
+
+    // the running maximum (and R) where a logit (a scale) has passed it
+    bool over = false;
+#pragma unroll
+    for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float t = fmaxf(fmaxf(z[0][nt][e], z[0][nt][2 + e]), fmaxf(z[1][nt][e], z[1][nt][2 + e]));
+        over = over || t > m[nt][e] + 15.f;
+      }
+    if (Q4) over = over || smax > R;
+    if (__any_sync(0xffffffffu, over)) {
+      float shrink = 1.f;
+      if (Q4) {
+        smax = warp_max(smax);
+        if (smax > R || R == 0.f) {
+          const float Rn = pow2_above(smax);
+          shrink = R * (1.f / Rn);
+          R = Rn;
+          Rinv = 1.f / Rn;
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt) {
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float t = fmaxf(fmaxf(z[0][nt][e], z[0][nt][2 + e]), fmaxf(z[1][nt][e], z[1][nt][2 + e]));
+#pragma unroll
+          for (int s = 4; s < 32; s <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, s));
+          const float mn = fmaxf(m[nt][e], t - 7.f);
+          f[e] = ex2(m[nt][e] - mn);
+          m[nt][e] = mn;
+          l[nt][e] *= f[e];
+          if (Q4) mp[nt][e] *= f[e];
+          f[e] *= shrink;
+        }
+#pragma unroll
+        for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[ct][nt][e] *= f[e & 1];
+      }
+    }
+
+    // weights, and the column operand: high parts and residuals
+    uint32_t ph[2][kN][2], pl[2][kN][2];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+        for (int t8 = 0; t8 < 2; ++t8) {
+          float wgt[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float p = ex2(z[mt][nt][2 * t8 + e] - m[nt][e]);
+            l[nt][e] += p;
+            wgt[e] = p;
+            if (Q4) {
+              mp[nt][e] = fmaf(p, vr[mt][t8], mp[nt][e]);
+              wgt[e] = p * (vs[mt][t8] * Rinv);
+            }
+          }
+          constexpr int PT = Q4 ? 0 : DT;
+          const uint32_t hi = pack2<PT>(wgt[0], wgt[1]);
+          const float2 hf = unpack2<PT>(hi);
+          const uint32_t lo = pack2<PT>(wgt[0] - hf.x, wgt[1] - hf.y);
+          if (kFold) {
+            ph[mt][nt][t8] = transpose8(tig < 2 ? hi : lo);
+          } else {
+            ph[mt][nt][t8] = transpose8(hi);
+            pl[mt][nt][t8] = transpose8(lo);
+          }
+        }
+
+    // O^T += V^T p.  mma rounds its sums towards zero, which over the thousands
+    // of tiles of a long row adds up (to 2e-5 of the output); so a tile is
+    // summed from zero and added in float32.
+    auto add_to = [&](int ct, const uint32_t (&A0)[4], const uint32_t (&A1)[4]) {   // both row blocks
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt) {
+        constexpr int PT = Q4 ? 0 : DT;
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
+        mma_16816<PT>(t, A0, ph[0][nt][0], ph[0][nt][1]);
+        mma_16816<PT>(t, A1, ph[1][nt][0], ph[1][nt][1]);
+        if (!kFold) {
+          mma_16816<PT>(t, A0, pl[0][nt][0], pl[0][nt][1]);
+          mma_16816<PT>(t, A1, pl[1][nt][0], pl[1][nt][1]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[ct][nt][e] += t[e];
+      }
+    };
+    if constexpr (Q4) {
+      const uint32_t vb = base + kQ4Codes;
+#pragma unroll
+      for (int x2 = 0; x2 < 2; ++x2) {   // 16-byte pieces 2 x2 and 2 x2 + 1 of the rows
+        uint32_t v[2][4];   // tokens 0-7 and 8-15 of a row block's piece 2 x2, then of 2 x2 + 1
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+          const int r = mt * 16 + (lane & 15), c = 2 * x2 + (lane >> 4);
+          ldmatrix_x4_trans(vb + r * 64 + ((c ^ ((r >> 1) & 3)) << 4), v[mt]);
+        }
+#pragma unroll
+        for (int xi = 0; xi < 2; ++xi) {
+          uint32_t u[2][2][4];
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              codes_to_half(v[mt][2 * xi + e], *reinterpret_cast<const __half2*>(&vz[mt][e]), u[mt][e]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t A0[4] = {u[0][0][2 * h], u[0][0][2 * h + 1], u[0][1][2 * h], u[0][1][2 * h + 1]};
+            const uint32_t A1[4] = {u[1][0][2 * h], u[1][0][2 * h + 1], u[1][1][2 * h], u[1][1][2 * h + 1]};
+            add_to((2 * x2 + xi) * 2 + h, A0, A1);
+          }
+        }
+      }
+    } else {
+      arrive();
+      const uint32_t vb = ring + slot * C::kSlot;
+      uint32_t keep[2][2];   // tokens 2 tig, 2 tig + 1 and 8 after, of the row blocks
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int r = mt * 16 + e * 8 + 2 * tig;
+          keep[mt][e] = (visible(r) ? 0xffffu : 0u) | (visible(r + 1) ? 0xffff0000u : 0u);
+        }
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct) {
+        uint32_t A[2][4];
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt) {
+          const int r = mt * 16 + (lane & 7) + ((lane >> 4) << 3), ch = ct * 2 + ((lane >> 3) & 1);
+          ldmatrix_x4_trans(vb + (ch >> 3) * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4), A[mt]);
+          if (!kFull) {   // rows that nobody sees may hold anything, NaN among it
+            A[mt][0] &= keep[mt][0];
+            A[mt][1] &= keep[mt][0];
+            A[mt][2] &= keep[mt][1];
+            A[mt][3] &= keep[mt][1];
+          }
+        }
+        add_to(ct, A[0], A[1]);
+      }
+    }
+    __syncwarp();
+    next_slot();
+    issue();
+  };
+
+  // ------------------------------------------------------------ a pair's end
+  auto end_pair = [&](int item) {   // item: its last one here
+    const int x0 = item - cur.tile, x1 = x0 + cur.t.count;
+    const bool whole = x0 >= i0 && x1 <= i1;
+    const int64_t pbase = ((int64_t)w * 2 + (x0 >= i0 ? 1 : 0)) * HC;
+#pragma unroll
+    for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float ls = l[nt][e], ms = mp[nt][e];
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1) {
+          ls += __shfl_xor_sync(0xffffffffu, ls, s);
+          if (Q4) ms += __shfl_xor_sync(0xffffffffu, ms, s);
+        }
+        const int col = nt * 8 + 2 * tig + e;
+        const bool mine = col < Gn;
+        const float inv = whole ? 1.f / ls : 1.f;
+        float* to = whole ? a.out + ((int64_t)b * a.H + h0 + col) * kHeadDim : a.part_o + (pbase + col) * kHeadDim;
+#pragma unroll
+        for (int ct = 0; ct < 8; ct += 2) {
+          float v[4] = {o[ct][nt][e], o[ct][nt][2 + e], o[ct + 1][nt][e], o[ct + 1][nt][2 + e]};
+          if (kFold) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 2);
+          }
+          if (!mine) continue;
+          if (Q4) {
+            *reinterpret_cast<float4*>(to + ct * 16 + 4 * grp) =
+                float4{fmaf(v[0], R, ms) * inv, fmaf(v[1], R, ms) * inv, fmaf(v[2], R, ms) * inv, fmaf(v[3], R, ms) * inv};
+          } else {
+            to[ct * 16 + grp] = v[0] * inv;
+            to[ct * 16 + 8 + grp] = v[1] * inv;
+            to[ct * 16 + 16 + grp] = v[2] * inv;
+            to[ct * 16 + 24 + grp] = v[3] * inv;
+          }
+        }
+        if (mine && grp == 0) {
+          if (!whole) a.part_ml[pbase + col] = float2{m[nt][e], ls};
+          else if (a.stats) a.stats[(int64_t)b * a.H + h0 + col] = float2{m[nt][e], 1.f / ls};
+        }
+      }
+  };
+
+  begin_pair();
+  for (int item = i0; item < i1; ++item) {
+    const int j0 = cur.t.token(cur.tile);
+    const bool full = j0 + kT <= cur.t.n && (j0 >= cur.t.start || j0 + kT <= a.sinks);
+    if (full) tile(Bool<true>{});
+    else tile(Bool<false>{});
+    if (!alive) break;
+    const bool last = cur.tile + 1 == cur.t.count;
+    if (last || item + 1 == i1) end_pair(item);
+    if (item + 1 < i1) {
+      advance(cur);
+      if (last) begin_pair();
+    }
+  }
+  // a wait ran out: the copies under way have to land before the CTA goes
+  while (!alive && taken < issued) {
+    mbar_wait(bars + 8 * slot, phase, a.err);
+    next_slot();
+  }
+}
+
+// ---------------------------------------------------------------- merge
+// One CTA per (sequence, query head): its warps take the partials in turn, a lane
+// four channels.
+__global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps_in_all) {
+  __shared__ float s_o[32][kHeadDim];
+  __shared__ float2 s_ml[32];
+  const int h = blockIdx.x, b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warps = blockDim.x >> 5;
+  const int g = h / a.G, hg = h - g * a.G, pass = hg / HC, col = hg - pass * HC;
+  const int row = a.kvh ? b * a.Hkv + g : b;
+  const int rows = a.kvh ? a.B * a.Hkv : a.B;
+  const int pairs = (a.kvh ? 1 : a.Hkv) * a.passes;
+  const int pair = (a.kvh ? 0 : g * a.passes) + pass;
+  pdl_wait();
+  pdl_launch_dependents();
+  const int total = a.table[rows], start = a.table[row], count = (a.table[row + 1] - start) / pairs;
+  float* out = a.out + ((int64_t)b * a.H + h) * kHeadDim;
+  if (count == 0) {   // nothing is visible
+    if (threadIdx.x < kHeadDim) out[threadIdx.x] = 0.f;
+    return;
+  }
+  const int x0 = start + pair * count, nw = min(warps_in_all, total);
+  const int w0 = warp_of(x0, total, nw), w1 = warp_of(x0 + count - 1, total, nw);
+  if (w0 == w1) return;   // written by its warp
+  float m = kNegHuge, l = 0.f;
+  float4 o{0.f, 0.f, 0.f, 0.f};
+  constexpr int kU = 4;
+  for (int w = w0 + warp; w <= w1; w += warps * kU) {
+    float2 ml[kU];
+    float4 v[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int wu = w + u * warps;
+      ml[u] = float2{kNegHuge, 0.f};
+      v[u] = float4{0.f, 0.f, 0.f, 0.f};
+      if (wu <= w1) {
+        const int64_t p = ((int64_t)wu * 2 + (wu == w0 ? 1 : 0)) * HC + col;
+        ml[u] = a.part_ml[p];
+        v[u] = *reinterpret_cast<const float4*>(a.part_o + p * kHeadDim + 4 * lane);
+      }
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) mn = fmaxf(mn, ml[u].x);
+    const float f = ex2(m - mn);
+    m = mn;
+    l *= f;
+    o.x *= f;
+    o.y *= f;
+    o.z *= f;
+    o.w *= f;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const float s = ex2(ml[u].x - mn);
+      l = fmaf(ml[u].y, s, l);
+      o.x = fmaf(v[u].x, s, o.x);
+      o.y = fmaf(v[u].y, s, o.y);
+      o.z = fmaf(v[u].z, s, o.z);
+      o.w = fmaf(v[u].w, s, o.w);
+    }
+  }
+  *reinterpret_cast<float4*>(&s_o[warp][4 * lane]) = o;
+  if (lane == 0) s_ml[warp] = float2{m, l};
+  __syncthreads();
+  if (threadIdx.x >= kHeadDim) return;
+  float M = kNegHuge, L = 0.f, O = 0.f;
+  for (int i = 0; i < warps; ++i) M = fmaxf(M, s_ml[i].x);
+  for (int i = 0; i < warps; ++i) {
+    const float s = ex2(s_ml[i].x - M);
+    L = fmaf(s_ml[i].y, s, L);
+    O = fmaf(s_o[i][threadIdx.x], s, O);
+  }
+  out[threadIdx.x] = O / L;
+  if (a.stats && threadIdx.x == 0) a.stats[(int64_t)b * a.H + h] = float2{M, 1.f / L};
+}
+
+// ---------------------------------------------------------------- importance
+// A CTA takes four visible tiles of a row: a lane four consecutive tokens, the
+// warps the heads in turn.  The sums are added in a fixed order.
+constexpr int kAccWarps = 8;
+
+__global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const WindowArgs a) {
+  __shared__ float4 s_sum[kAccWarps][32];
+  const int row = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int b = a.kvh ? row / a.Hkv : row;
+  const int h0 = a.kvh ? (row - b * a.Hkv) * a.G : 0, nh = a.kvh ? a.G : a.H;
+  pdl_wait();
+  pdl_launch_dependents();
+  const Tiles t(a.lens[row], a.cap, a.sinks, a.window);
+  const int i = blockIdx.x * 4 + (lane >> 3);
+  if (blockIdx.x * 4 >= t.count) return;
+  const bool there = i < t.count;
+  const int j = there ? t.token(i) + (lane & 7) * 4 : 0;
+  float4 sum{0.f, 0.f, 0.f, 0.f};
+  if (there) {
+#pragma unroll 4
+    for (int h = warp; h < nh; h += kAccWarps) {
+      const int64_t at = (int64_t)b * a.H + h0 + h;
+      const float2 st = a.stats[at];
+      const float4 z = *reinterpret_cast<const float4*>(a.logits + at * a.cap32 + j);
+      sum.x = fmaf(ex2(z.x - st.x), st.y, sum.x);
+      sum.y = fmaf(ex2(z.y - st.x), st.y, sum.y);
+      sum.z = fmaf(ex2(z.z - st.x), st.y, sum.z);
+      sum.w = fmaf(ex2(z.w - st.x), st.y, sum.w);
+    }
+  }
+  s_sum[warp][lane] = sum;
+  __syncthreads();
+  if (warp || !there) return;
+  for (int k = 1; k < kAccWarps; ++k) {
+    const float4 v = s_sum[k][lane];
+    sum.x += v.x;
+    sum.y += v.y;
+    sum.z += v.z;
+    sum.w += v.w;
+  }
+  float* to = a.accum + (int64_t)row * a.cap + j;
+  const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)   // (a token that is not visible has weight 0, and its place is not touched)
+    if (j + e < t.n && (j + e < a.sinks || j + e >= t.start)) to[e] += v[e];
+}
+
+template <bool Q4>
+constexpr int warps_for(int HC) {
+  return Q4 && HC < 16 ? 16 : 8;
+}
+
+template <int DT, bool Q4, int HC>
+cudaError_t launch_attn_t(const WindowArgs& a, int sms, cudaStream_t st) {
+  constexpr int NW = warps_for<Q4>(HC);
+  auto kern = hill_window_attn_kernel<DT, Q4, HC, NW>;
+  static int cache[64] = {0};
+  const int smem = Cfg<Q4>::smem(NW);
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), smem, cache);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kern, dim3(sms), dim3(NW * 32), smem, st, 0, a);
+}
+
+}  // namespace
+
+int window_heads_per_pass(int G) { return G <= 4 ? 4 : (G <= 8 ? 8 : 16); }
+int window_warps(bool q4, int HC) { return q4 ? warps_for<true>(HC) : warps_for<false>(HC); }
+int window_max_rows() { return kMaxRows; }
+
+cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms, cudaStream_t st, int* kernels) {
+  const int HC = window_heads_per_pass(a.G);
+  cudaError_t e = cudaErrorInvalidValue;
+  auto go = [&](auto dt, auto is4) {
+    constexpr int DT = decltype(dt)::value;
+    constexpr bool Q4 = decltype(is4)::value;
+    return HC == 4 ? launch_attn_t<DT, Q4, 4>(a, sms, st)
+                   : HC == 8 ? launch_attn_t<DT, Q4, 8>(a, sms, st) : launch_attn_t<DT, Q4, 16>(a, sms, st);
+  };
+  if (q4) e = dtype ? go(Int<1>{}, Bool<true>{}) : go(Int<0>{}, Bool<true>{});
+  else e = dtype ? go(Int<1>{}, Bool<false>{}) : go(Int<0>{}, Bool<false>{});
+  if (e != cudaSuccess) return e;
+  const int nw = sms * window_warps(q4, HC);
+  // about four partials to a warp
+  const int64_t per = nw / std::max<int64_t>(1, (int64_t)a.B * a.Hkv * a.passes) + 1;
+  int warps = 4;
+  while (warps < 32 && warps * 4 < per) warps <<= 1;
+  e = launch_pdl(hill_window_combine_kernel, dim3(a.H, a.B), dim3(warps * 32), 0, st, 0, a, HC, nw);
+  *kernels = 2;
+  if (e != cudaSuccess || !a.accum) return e;
+  const int64_t all = (a.cap + kT - 1) / kT;
+  const int64_t tiles = std::min<int64_t>(all, ((int64_t)a.sinks + kT - 1) / kT + ((int64_t)a.window + kT - 1) / kT + 1);
+  *kernels = 3;
+  return launch_pdl(hill_window_accum_kernel, dim3((unsigned)std::max<int64_t>(1, (tiles + 3) / 4), a.kvh ? a.B * a.Hkv : a.B),
+                    dim3(kAccWarps * 32), 0, st, 0, a);
+}
+
+}  // namespace hill

@@ -10,7 +10,9 @@ Names follow the C ABI: :func:`hill_score`, :func:`hill_topk_select`,
 :func:`hill_gather_sparse_attn`, :func:`hill_evict_step`, :func:`hill_topk_select_bkp`,
 :func:`hill_evict_step_bkp`, :func:`hill_quantize_k`, :func:`hill_score_f8`, :func:`hill_evict_step_f8`,
 :func:`hill_evict_step_kvh`, :func:`hill_evict_step_begin`, :func:`hill_evict_step_begin_f8`,
-:func:`hill_evict_step_end`, :func:`hill_workspace_bytes`, :func:`hill_sync_status`.
+:func:`hill_evict_step_end`, :func:`hill_workspace_bytes`, :func:`hill_sync_status`; for a cache of bounded
+size :func:`hill_window_attn`, :func:`hill_window_attn_q4`, :func:`hill_cache_insert`, :func:`hill_cache_insert_q4`,
+:func:`hill_cache_read_q4`, :func:`hill_window_workspace_bytes`.
 """
 from __future__ import annotations
 
@@ -52,6 +54,15 @@ class hill_desc(ctypes.Structure):
     ]
 
 
+class hill_new_rows(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_sb", ctypes.c_int64), ("k_sh", ctypes.c_int64), ("k_sn", ctypes.c_int64),
+        ("v_sb", ctypes.c_int64), ("v_sh", ctypes.c_int64), ("v_sn", ctypes.c_int64),
+        ("max_new", ctypes.c_int32), ("count", ctypes.c_void_p), ("weight", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -84,6 +95,14 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.hill_evict_step_f8.argtypes = [D, P, P, P, P, P, P, P, I32, I32, P, P, P, P, P, P, SZ, P]
     lib.hill_score_noalloc.argtypes = [D, P, P, P, I32, P, P, P]
     lib.hill_score_noalloc.restype = I32
+    lib.hill_window_workspace_bytes.argtypes = [D, I32]
+    lib.hill_window_workspace_bytes.restype = SZ
+    lib.hill_window_attn.argtypes = [D, P, P, P, P, I32, I32, I32, P, P, P, SZ, P]
+    lib.hill_window_attn_q4.argtypes = [D, P, P, P, P, P, I32, I32, I32, P, P, P, SZ, P]
+    N = ctypes.POINTER(hill_new_rows)
+    lib.hill_cache_insert.argtypes = [D, N, P, P, P, P, P, I32, I32, I32, P, P]
+    lib.hill_cache_insert_q4.argtypes = [D, N, P, P, P, P, P, P, I32, I32, I32, P, P]
+    lib.hill_cache_read_q4.argtypes = [D, P, P, P, P, P, I32, P, P, P]
     lib.hill_sync_status.argtypes = [P]
     lib.hill_status_string.argtypes = [I32]
     lib.hill_status_string.restype = ctypes.c_char_p
@@ -92,7 +111,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
     for name in ("hill_score", "hill_topk_select", "hill_gather_sparse_attn", "hill_evict_step",
                  "hill_topk_select_bkp", "hill_evict_step_bkp", "hill_quantize_k", "hill_score_f8",
                  "hill_evict_step_f8", "hill_evict_step_kvh", "hill_evict_step_begin", "hill_evict_step_begin_f8",
-                 "hill_evict_step_end", "hill_selftest_wait", "hill_sync_status"):
+                 "hill_evict_step_end", "hill_selftest_wait", "hill_sync_status", "hill_window_attn",
+                 "hill_window_attn_q4", "hill_cache_insert", "hill_cache_insert_q4", "hill_cache_read_q4"):
         getattr(lib, name).restype = I32
     _lib = lib
     return lib
@@ -281,6 +301,95 @@ def hill_evict_step_f8(desc, q, k8, kscale, k_cache, v_cache, lens, k, max_k, mo
            "hill_evict_step_f8")
 
 
+def make_desc_q4(q: torch.Tensor, k4: torch.Tensor) -> hill_desc:
+    """Descriptor from q [B][H][d] and the codes of a 4-bit cache [B][Hkv][cap][d / 2]."""
+    B, H, d = q.shape
+    Bk, Hkv, cap, half = k4.shape
+    if Bk != B or 2 * half != d:
+        raise ValueError(f"shape mismatch q {tuple(q.shape)} vs codes {tuple(k4.shape)}")
+    if q.stride(-1) != 1:
+        raise ValueError("head dimension must be contiguous")
+    dt = {torch.float16: HILL_F16, torch.bfloat16: HILL_BF16}.get(q.dtype)
+    if dt is None:
+        raise ValueError(f"unsupported dtype {q.dtype}")
+    return hill_desc(B, H, Hkv, d, cap, dt, q.stride(0), q.stride(1), Hkv * cap * d, cap * d, d, Hkv * cap * d, cap * d, d)
+
+
+def q4_shape(B: int, Hkv: int, cap: int, d: int = 128):
+    """Shapes of a 4-bit cache: codes (of K, and of V) [B][Hkv][cap][d / 2], params [B][Hkv][cap32][4]."""
+    return (B, Hkv, cap, d // 2), (B, Hkv, (cap + 31) // 32 * 32, 4)
+
+
+def alloc_q4(B: int, Hkv: int, cap: int, dtype=torch.float16, device="cuda"):
+    """(k4, v4, params) of an empty 4-bit cache."""
+    cs, ps = q4_shape(B, Hkv, cap)
+    return (torch.zeros(cs, dtype=torch.uint8, device=device), torch.zeros(cs, dtype=torch.uint8, device=device),
+            torch.zeros(ps, dtype=dtype, device=device))
+
+
+def hill_window_workspace_bytes(desc: hill_desc, with_accum: bool) -> int:
+    return int(load().hill_window_workspace_bytes(ctypes.byref(desc), int(bool(with_accum))))
+
+
+def alloc_window_workspace(desc: hill_desc, with_accum: bool, device="cuda") -> torch.Tensor:
+    n = hill_window_workspace_bytes(desc, with_accum)
+    if n == 0:
+        raise HillError(HILL_ERR_INVALID_ARG, "hill_window_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def hill_window_attn(desc, q, k_cache, v_cache, lens, sinks, window, out, accum=None, kvh=False, ws=None,
+                     stream=None) -> None:
+    """Attention over the first `sinks` and the newest `window` tokens; accum += the weights."""
+    wp, wn = _ws(ws)
+    _check(load().hill_window_attn(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(lens), int(sinks),
+                                   int(window), int(bool(kvh)), _ptr(accum), _ptr(out), wp, wn, _stream(stream)),
+           "hill_window_attn")
+
+
+def hill_window_attn_q4(desc, q, k4, v4, params, lens, sinks, window, out, accum=None, kvh=False, ws=None,
+                        stream=None) -> None:
+    """hill_window_attn over a cache held in 4 bits."""
+    wp, wn = _ws(ws)
+    _check(load().hill_window_attn_q4(ctypes.byref(desc), _ptr(q), _ptr(k4), _ptr(v4), _ptr(params), _ptr(lens),
+                                      int(sinks), int(window), int(bool(kvh)), _ptr(accum), _ptr(out), wp, wn,
+                                      _stream(stream)), "hill_window_attn_q4")
+
+
+def _new_rows(desc, k_new, v_new, n_new, w_new) -> hill_new_rows:
+    want = (desc.batch, desc.num_kv_heads, k_new.shape[2], desc.head_dim)
+    for x in (k_new, v_new):
+        if tuple(x.shape) != want or x.stride(-1) != 1 or x.dtype != (torch.bfloat16 if desc.dtype else torch.float16):
+            raise ValueError(f"new rows must be {want} in the cache's type, the last dimension contiguous")
+    return hill_new_rows(k_new.data_ptr(), v_new.data_ptr(), *k_new.stride()[:3], *v_new.stride()[:3], want[2],
+                         _ptr(n_new), _ptr(w_new))
+
+
+def hill_cache_insert(desc, k_new, v_new, k_cache, v_cache, seen, pos, accum, sinks, recent, slots, n_new=None,
+                      w_new=None, kvh=False, stream=None) -> None:
+    """New tokens [B][Hkv][T][d] into a cache of fixed size, in place; a full one evicts by accumulated weight."""
+    rows = _new_rows(desc, k_new, v_new, n_new, w_new)
+    _check(load().hill_cache_insert(ctypes.byref(desc), ctypes.byref(rows), _ptr(k_cache), _ptr(v_cache), _ptr(seen),
+                                    _ptr(pos), _ptr(accum), int(sinks), int(recent), int(bool(kvh)), _ptr(slots),
+                                    _stream(stream)), "hill_cache_insert")
+
+
+def hill_cache_insert_q4(desc, k_new, v_new, k4, v4, params, seen, pos, accum, sinks, recent, slots, n_new=None,
+                         w_new=None, kvh=False, stream=None) -> None:
+    """hill_cache_insert into a 4-bit cache."""
+    rows = _new_rows(desc, k_new, v_new, n_new, w_new)
+    _check(load().hill_cache_insert_q4(ctypes.byref(desc), ctypes.byref(rows), _ptr(k4), _ptr(v4), _ptr(params),
+                                       _ptr(seen), _ptr(pos), _ptr(accum), int(sinks), int(recent), int(bool(kvh)),
+                                       _ptr(slots), _stream(stream)), "hill_cache_insert_q4")
+
+
+def hill_cache_read_q4(desc, k4, v4, params, row_begin, row_end, max_rows, k_cache, v_cache, stream=None) -> None:
+    """What slots [row_begin, row_end) of a 4-bit cache stand for, into 16-bit caches."""
+    _check(load().hill_cache_read_q4(ctypes.byref(desc), _ptr(k4), _ptr(v4), _ptr(params), _ptr(row_begin),
+                                     _ptr(row_end), int(max_rows), _ptr(k_cache), _ptr(v_cache), _stream(stream)),
+           "hill_cache_read_q4")
+
+
 def hill_selftest_wait(limit_us: int, stream=None) -> None:
     """Run the bounded-wait self test (its expiry shows up in hill_sync_status)."""
     _check(load().hill_selftest_wait(int(limit_us), _stream(stream)), "hill_selftest_wait")
@@ -319,3 +428,65 @@ class Evictor:
         hill_evict_step(self.desc, q, k_cache, v_cache, lens, k, self.max_k, self.mode, accum,
                         self.scores, self.idx, self.count, self.out, self.ws, stream)
         return self
+
+
+class BoundedCache:
+    """The cache of one layer with a fixed number of slots: its buffers and state, allocated once.
+
+    ``insert`` puts new tokens in (a full cache evicts by accumulated weight), ``attend`` runs the attention over
+    what is held and adds the weights; ``step`` does both.  ``bits`` is 16 or 4.  With ``kvh`` every KV head keeps
+    tokens of its own.
+    """
+
+    def __init__(self, batch: int, heads: int, kv_heads: int, capacity: int, dtype=torch.float16, bits: int = 16,
+                 sinks: int = 4, recent: int = 0, kvh: bool = False, max_new: int = 1, device="cuda"):
+        if bits not in (4, 16):
+            raise ValueError("bits must be 16 or 4")
+        self.bits, self.sinks, self.recent, self.kvh, self.max_new = bits, int(sinks), int(recent), bool(kvh), int(max_new)
+        rows = (batch, kv_heads) if kvh else (batch,)
+        q = torch.empty(batch, heads, 128, dtype=dtype, device=device)
+        if bits == 4:
+            self.k4, self.v4, self.params = alloc_q4(batch, kv_heads, capacity, dtype, device)
+            self.desc = make_desc_q4(q, self.k4)
+        else:
+            self.K, self.V = (torch.zeros(batch, kv_heads, capacity, 128, dtype=dtype, device=device) for _ in range(2))
+            self.desc = make_desc(q, self.K, self.V)
+        self.seen = torch.zeros(rows, dtype=torch.int32, device=device)
+        self.pos = torch.zeros(*rows, capacity, dtype=torch.int32, device=device)
+        self.accum = torch.zeros(*rows, capacity, dtype=torch.float32, device=device)
+        self.slots = torch.full((*rows, self.max_new), -1, dtype=torch.int32, device=device)
+        self.out = torch.empty(batch, heads, 128, dtype=torch.float32, device=device)
+        self.ws = alloc_window_workspace(self.desc, True, device)
+
+    def insert(self, k_new, v_new, n_new=None, w_new=None, stream=None):
+        """New tokens [B][Hkv][T][d], T <= max_new; slots[..., :T] says where they went."""
+        T = k_new.shape[2]
+        if T > self.max_new:
+            raise ValueError(f"{T} new tokens, at most {self.max_new}")
+        slots = self.slots if T == self.max_new else self.slots.flatten()[:self.seen.numel() * T].view(*self.seen.shape, T)
+        if self.bits == 4:
+            hill_cache_insert_q4(self.desc, k_new, v_new, self.k4, self.v4, self.params, self.seen, self.pos, self.accum,
+                                 self.sinks, self.recent, slots, n_new, w_new, self.kvh, stream)
+        else:
+            hill_cache_insert(self.desc, k_new, v_new, self.K, self.V, self.seen, self.pos, self.accum, self.sinks,
+                              self.recent, slots, n_new, w_new, self.kvh, stream)
+        return slots
+
+    def attend(self, q, stream=None):
+        """Attention of q [B][H][d] over the held tokens; their weights are added to accum."""
+        if q.shape != self.out.shape or q.stride(-1) != 1:
+            raise ValueError(f"q must be {tuple(self.out.shape)} with the last dimension contiguous")
+        self.desc.q_sb, self.desc.q_sh = q.stride(0), q.stride(1)
+        everything = self.desc.capacity
+        if self.bits == 4:
+            hill_window_attn_q4(self.desc, q, self.k4, self.v4, self.params, self.seen, 0, everything, self.out,
+                                self.accum, self.kvh, self.ws, stream)
+        else:
+            hill_window_attn(self.desc, q, self.K, self.V, self.seen, 0, everything, self.out, self.accum, self.kvh,
+                             self.ws, stream)
+        return self.out
+
+    def step(self, q, k_new, v_new, stream=None):
+        """One decode step: the new token in, then its attention."""
+        self.insert(k_new, v_new, stream=stream)
+        return self.attend(q, stream)
