@@ -141,14 +141,14 @@ hill_status make_kmap(const hill_desc* d, const void* k, ScoreArgs* a) {
 }
 
 // Codes of a 4-bit cache [B][Hkv][cap][64]: box = one row (64-byte swizzle) x
-// 32 tokens.  Rows past the capacity read as zeros.
-hill_status make_q4_map(const hill_desc* d, const void* codes, CUtensorMap* map) {
+// a tile of tokens.  Rows past the capacity read as zeros.
+hill_status make_q4_map(const hill_desc* d, const void* codes, int tile, CUtensorMap* map) {
   auto fn = encode_tiled();
   if (!fn) return HILL_ERR_CUDA;
   const cuuint64_t row = kHeadDim / 2, cap = (cuuint64_t)std::max(d->capacity, 1);
   cuuint64_t gdim[3] = {row, cap, (cuuint64_t)std::max<int64_t>((int64_t)d->batch * d->num_kv_heads, 1)};
   cuuint64_t gstr[2] = {row, cap * row};
-  cuuint32_t box[3] = {(cuuint32_t)row, 32, 1};
+  cuuint32_t box[3] = {(cuuint32_t)row, (cuuint32_t)tile, 1};
   cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(codes), gdim, gstr, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
@@ -989,7 +989,7 @@ WindowLayout window_layout(const hill_desc* d, bool with_accum, int sms) {
   L.stats = off;
   if (with_accum) off += align_up(B * H * sizeof(float2));
   L.logits = off;
-  if (with_accum) off += align_up(B * H * (size_t)cap32_of(d) * sizeof(float));
+  if (with_accum) off += align_up(B * H * (size_t)((d->capacity + 63) & ~63) * sizeof(float));
   L.total = off + kAlign;
   return L;
 }
@@ -1016,8 +1016,9 @@ hill_status window_attn(const hill_desc* desc, const void* q, const void* k, con
   unsigned char* base = ws_base(ws);
   WindowArgs a{};
   if (params) {
-    s = make_q4_map(desc, k, &a.kmap);
-    if (s == HILL_OK) s = make_q4_map(desc, v, &a.vmap);
+    const int tile = window_q4_tile(L.heads);
+    s = make_q4_map(desc, k, tile, &a.kmap);
+    if (s == HILL_OK) s = make_q4_map(desc, v, tile, &a.vmap);
   } else {
     int where[3];
     s = make_cache_map(desc, k, desc->k_sb, desc->k_sh, desc->k_sn, &a.kmap, where);
@@ -1051,6 +1052,7 @@ hill_status window_attn(const hill_desc* desc, const void* q, const void* k, con
   if (accum) {
     a.stats = reinterpret_cast<float2*>(base + L.stats);
     a.logits = reinterpret_cast<float*>(base + L.logits);
+    a.lstride = (desc->capacity + 63) & ~63;
   }
   a.err = di.err;
   int kernels = 0;

@@ -150,7 +150,7 @@ struct AttnArgs {
 // Attention over the visible part of a cache (window.cu).
 struct WindowArgs {
   // 16 bits: 4-D maps of K and V, 128-byte swizzle, box = 64 dims x 32 tokens;
-  // 4 bits: 3-D maps (64 bytes, cap, B * Hkv) of the codes, 64-byte swizzle, box = 64 bytes x 32 tokens
+  // 4 bits: 3-D maps (64 bytes, cap, B * Hkv) of the codes, 64-byte swizzle, box = 64 bytes x a tile
   CUtensorMap kmap, vmap;
   int kdim_tok, kdim_head, vdim_tok, vdim_head;   // which dimension of a 4-D map holds token and KV head
   const uint2* params;   // 4 bits: [B][Hkv][cap32] (K scale, K min, V scale, V min)
@@ -162,7 +162,8 @@ struct WindowArgs {
   int passes;            // of at most window_heads_per_pass(G) query heads
   float* out;            // [B][H][d]
   float* accum;          // [B][cap], kvh: [B][Hkv][cap], or NULL
-  float* logits;         // [B][H][cap32] base-2 logits, or NULL (no accum)
+  float* logits;         // [B][H][lstride] base-2 logits, or NULL (no accum)
+  int lstride;           // cap rounded up to whole tiles
   float2* stats;         // [B][H] (max, 1 / sum), or NULL (no accum)
   float* part_o;         // [warps][2][heads per pass][d] partials: of the pair a warp's part begins in, and ends in
   float2* part_ml;       // [warps][2][heads per pass]
@@ -308,6 +309,7 @@ cudaError_t launch_sparse_attn(const AttnArgs& a, int dtype, int G, int grid, bo
 // window.cu
 int window_heads_per_pass(int G);
 int window_warps(bool q4, int heads_per_pass);   // per CTA, one CTA per SM
+int window_q4_tile(int heads_per_pass);           // tokens
 int window_max_rows();
 cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms, cudaStream_t st, int* kernels);
 

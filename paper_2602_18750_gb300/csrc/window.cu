@@ -47,35 +47,40 @@
 namespace hill {
 namespace {
 
-constexpr int kT = 32;                    // tokens per tile
-constexpr int kBox = kT * 128;            // 16-bit: 32 rows x 64 dims
-constexpr int kQ4Codes = kT * 64;         // 4-bit: 32 rows of codes
-constexpr int kQ4Slot = 2 * kQ4Codes + kT * 8;   // K codes, V codes, params
 constexpr int kMaxRows = 2048;            // rows of lens
 
-template <bool Q4>
+// Tiles and rings.  4 bits: a slot holds the K codes, V codes and parameters of
+// a tile, and after them 16 bytes per two tokens that no copy writes (notes);
+// 16 bits: a K or a V tile in turn, 32 rows x 64 dims twice.
+template <bool Q4, int HC>
 struct Cfg {
-  static constexpr int kSlot = Q4 ? 2 * kQ4Codes + 512 : 2 * kBox;   // 16-bit: a K or a V tile
-  static constexpr int kSlots = 3;
-  static constexpr int smem(int warps) { return warps * kSlots * kSlot + 1024; }   // + alignment slack
+  static constexpr int kNW = !Q4 || HC == 16 ? 8 : 12;   // warps
+  static constexpr int kMT = !Q4 || HC == 16 ? 2 : 4;    // row blocks of 16 tokens
+  static constexpr int kT = 16 * kMT;                    // tokens per tile
+  static constexpr int kSlots = kMT == 4 ? 2 : 3;
+  static constexpr int kCodes = kT * 64;
+  static constexpr int kNotes = 2 * kCodes + kT * 8;     // where the notes begin
+  static constexpr int kBox = kT * 128;
+  static constexpr int kSlot = Q4 ? kNotes + kT * 8 : 2 * kBox;
+  static constexpr int kSmem = kNW * kSlots * kSlot + 1024;   // + alignment slack
 };
 
 // The visible tiles of a row of n tokens: [0, sink) and from tile `first` on.
+template <int T>
 struct Tiles {
   int n, start;        // tokens; first token of the window
   int sink, first, count;
-  __device__ __forceinline__ Tiles() {}
   __device__ __forceinline__ Tiles(int len, int cap, int sinks, int window) {
     n = len < 0 ? 0 : min(len, cap);
     start = max(0, n - window);
-    first = start / kT;
+    first = start / T;
     const int shown = min(sinks, start);   // sinks outside the window
-    const int win = start < n ? (n + kT - 1) / kT - first : 0;
-    sink = (shown + kT - 1) / kT;
+    const int win = start < n ? (n + T - 1) / T - first : 0;
+    sink = (shown + T - 1) / T;
     if (win > 0) sink = min(sink, first);
     count = sink + win;
   }
-  __device__ __forceinline__ int token(int i) const { return (i < sink ? i : first + i - sink) * kT; }
+  __device__ __forceinline__ int token(int i) const { return (i < sink ? i : first + i - sink) * T; }
 };
 
 // The part of the list that warp w of nw (at most as many as tiles) owns, and
@@ -120,14 +125,13 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, __half2 z1024, uint32_
 }
 
 // The zero point of a row, the integer of [0, 15] nearest to -min / scale (any
-// would be right, this one leaves the smallest rest), 1024 added, as fp16 in
-// the high half over the row's scale in the low half; and the rest min + scale * zero point.
-template <int DT>
-__device__ __forceinline__ uint32_t zero_point(uint32_t param, float& rest) {
-  const float2 p = unpack2<DT>(param);
-  const float z = rintf(fminf(fmaxf(__fdividef(-p.y, p.x), 0.f), 15.f));
-  rest = fmaf(p.x, z, p.y);
-  return (param & 0xffffu) | ((uint32_t)__half_as_ushort(__float2half_rn(1024.f + z)) << 16);
+// would be right, this one leaves the smallest rest): 1024 + it, as a float that fp16 holds, and
+// the rest min + scale * zero point.
+__device__ __forceinline__ float zero_point(float2 p, float& rest) {
+  const float t = fminf(fmaxf(__fdividef(-p.y, p.x) + 1024.f, 1024.f), 1039.f);
+  const float z = __half2float(__float2half_rn(t));   // (fp16 steps by 1 there)
+  rest = fmaf(p.x, z - 1024.f, p.y);
+  return z;
 }
 
 __device__ __forceinline__ __half2 high_twice(uint32_t v) {   // the high half in both halves
@@ -154,15 +158,17 @@ __device__ __forceinline__ float pow2_above(float s) {
 template <int I> using Int = std::integral_constant<int, I>;
 template <bool I> using Bool = std::integral_constant<bool, I>;
 
-// Where the warp stands in the list.
-struct Cursor {
-  int row, pair, tile;   // pair: KV head and pass within the row
-  Tiles t;
+// Where the warp stands in the list: a run of tiles of consecutive tokens.
+struct Walk {
+  int row, pair, tile;   // pair: KV head and pass within the row; tile: the run's first
+  int j, left;           // first token and length of the run
 };
 
-template <int DT, bool Q4, int HC, int NW>
-__global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __grid_constant__ WindowArgs a) {
-  using C = Cfg<Q4>;
+template <int DT, bool Q4, int HC>
+__global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_kernel(const __grid_constant__ WindowArgs a) {
+  using C = Cfg<Q4, HC>;
+  using Tl = Tiles<C::kT>;
+  constexpr int NW = C::kNW, MT = C::kMT;
   constexpr int kN = HC == 16 ? 2 : 1;         // column blocks of 8 heads
   constexpr bool kFold = HC == 4;              // residuals in columns 4 to 7
   extern __shared__ unsigned char wsm[];
@@ -186,7 +192,7 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
   pdl_wait();
 
   // the list: every CTA scans the rows' tiles
-  auto row_tiles = [&](int r) { return Tiles(a.lens[r], a.cap, a.sinks, a.window); };
+  auto row_tiles = [&](int r) { return Tl(a.lens[r], a.cap, a.sinks, a.window); };
   int total = 0;
   for (int r0 = 0; r0 < rows; r0 += NW * 32) {
     const int r = r0 + (int)threadIdx.x;
@@ -217,65 +223,81 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
   const int i0 = first_item(w, total, nw), i1 = first_item(w + 1, total, nw);
 
   const uint64_t policy = l2_evict_first_policy();
-  auto locate = [&](int item) {
-    Cursor c;
-    int lo = 0, hi = rows - 1;   // the last row that starts at or before item
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_start[mid] <= item) lo = mid;
-      else hi = mid - 1;
-    }
-    c.row = lo;
-    c.t = row_tiles(lo);
-    const int x = item - s_start[lo];
-    c.pair = x / c.t.count;
-    c.tile = x - c.pair * c.t.count;
-    return c;
+  auto set_run = [&](Walk& c, const Tl& t) {
+    c.j = t.token(c.tile);
+    c.left = (c.tile < t.sink ? t.sink : t.count) - c.tile;
   };
-  auto advance = [&](Cursor& c) {   // only while an item follows
-    if (++c.tile < c.t.count) return;
-    c.tile = 0;
-    if (++c.pair < pairs) return;
-    c.pair = 0;
-    do {
-      ++c.row;
-    } while (s_start[c.row + 1] == s_start[c.row]);
-    c.t = row_tiles(c.row);
-  };
-  auto seq_of = [&](const Cursor& c) { return a.kvh ? c.row / a.Hkv : c.row; };
-  auto head_of = [&](const Cursor& c) { return a.kvh ? c.row % a.Hkv : c.pair / a.passes; };
-
-  // ------------------------------------------------------------ the ring
-  // A stage is a slot's content: a tile (4 bits), or a K or a V tile in turn.
-  constexpr int kPer = Q4 ? 1 : 2;
-  const int stages = (i1 - i0) * kPer;
-  Cursor cur = locate(i0), ahead = cur;
-  int issued = 0, slot_in = 0;
-  auto issue = [&] {   // the next stage, if there is one
-    if (issued >= stages) return;
-    if (lane == 0) {
-      const uint32_t dst = ring + slot_in * C::kSlot, bar = bars + 8 * slot_in;
-      const int b = seq_of(ahead), g = head_of(ahead), j = ahead.t.token(ahead.tile);
-      if (Q4) {
-        mbar_arrive_expect_tx(bar, kQ4Slot);
-        tma_load_3d(dst, &a.kmap, 0, j, b * a.Hkv + g, bar, policy);
-        tma_load_3d(dst + kQ4Codes, &a.vmap, 0, j, b * a.Hkv + g, bar, policy);
-        bulk_g2s(dst + 2 * kQ4Codes, a.params + ((int64_t)(b * a.Hkv + g) * a.cap32 + j), kT * 8, bar, policy);
-      } else {
-        const bool v = issued & 1;
-        const void* map = v ? &a.vmap : &a.kmap;
-        const int dt = v ? a.vdim_tok : a.kdim_tok, dh = v ? a.vdim_head : a.kdim_head;
-        const int c1 = dt == 1 ? j : (dh == 1 ? g : b);
-        const int c2 = dt == 2 ? j : (dh == 2 ? g : b);
-        const int c3 = dt == 3 ? j : (dh == 3 ? g : b);
-        mbar_arrive_expect_tx(bar, 2 * kBox);
-        tma_load_4d(dst, map, 0, c1, c2, c3, bar, policy);
-        tma_load_4d(dst + kBox, map, 64, c1, c2, c3, bar, policy);
+  auto next_run = [&](Walk& c) {   // c.tile has passed the run; only while an item follows
+    Tl t = row_tiles(c.row);
+    if (c.tile == t.count) {
+      c.tile = 0;
+      if (++c.pair == pairs) {
+        c.pair = 0;
+        do {
+          ++c.row;
+        } while (s_start[c.row + 1] == s_start[c.row]);
+        t = row_tiles(c.row);
       }
     }
-    ++issued;
+    set_run(c, t);
+  };
+  auto seq_of = [&](const Walk& c) { return a.kvh ? c.row / a.Hkv : c.row; };
+  auto head_of = [&](const Walk& c) { return a.kvh ? c.row % a.Hkv : c.pair / a.passes; };
+  Walk cur;
+  {
+    int lo = 0, hi = rows - 1;   // the last row that starts at or before i0
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_start[mid] <= i0) lo = mid;
+      else hi = mid - 1;
+    }
+    const Tl t = row_tiles(lo);
+    const int x = i0 - s_start[lo];
+    cur.row = lo;
+    cur.pair = x / t.count;
+    cur.tile = x - cur.pair * t.count;
+    set_run(cur, t);
+  }
+
+  // ------------------------------------------------------------ the ring
+  // A stage is a slot's content.  The state of what is asked for next:
+  Walk ahead = cur;
+  int to_ask = i1 - i0, run_left = cur.left, ask_b = seq_of(cur), ask_g = head_of(cur);
+  int asked = 0, slot_in = 0;   // stages
+  auto issue = [&] {            // the next stage, if there is one
+    if (to_ask == 0) return;
+    if (lane == 0) {
+      const uint32_t dst = ring + slot_in * C::kSlot, bar = bars + 8 * slot_in;
+      if (Q4) {
+        const int bg = ask_b * a.Hkv + ask_g;
+        const uint32_t pbytes = min(C::kT, a.cap32 - ahead.j) * 8;   // (a row of parameters ends at cap32)
+        mbar_arrive_expect_tx(bar, 2 * C::kCodes + pbytes);
+        tma_load_3d(dst, &a.kmap, 0, ahead.j, bg, bar, policy);
+        tma_load_3d(dst + C::kCodes, &a.vmap, 0, ahead.j, bg, bar, policy);
+        bulk_g2s(dst + 2 * C::kCodes, a.params + ((int64_t)bg * a.cap32 + ahead.j), pbytes, bar, policy);
+      } else {
+        const bool v = asked & 1;
+        const void* map = v ? &a.vmap : &a.kmap;
+        const int dt = v ? a.vdim_tok : a.kdim_tok, dh = v ? a.vdim_head : a.kdim_head;
+        const int c1 = dt == 1 ? ahead.j : (dh == 1 ? ask_g : ask_b);
+        const int c2 = dt == 2 ? ahead.j : (dh == 2 ? ask_g : ask_b);
+        const int c3 = dt == 3 ? ahead.j : (dh == 3 ? ask_g : ask_b);
+        mbar_arrive_expect_tx(bar, 2 * C::kBox);
+        tma_load_4d(dst, map, 0, c1, c2, c3, bar, policy);
+        tma_load_4d(dst + C::kBox, map, 64, c1, c2, c3, bar, policy);
+      }
+    }
+    ++asked;
     slot_in = slot_in + 1 == C::kSlots ? 0 : slot_in + 1;
-    if (issued % kPer == 0 && issued < stages) advance(ahead);
+    if (!Q4 && (asked & 1)) return;   // V of the same tile follows
+    ahead.j += C::kT;
+    if (--to_ask > 0 && --run_left == 0) {
+      ahead.tile += ahead.left;
+      next_run(ahead);
+      run_left = ahead.left;
+      ask_b = seq_of(ahead);
+      ask_g = head_of(ahead);
+    }
   };
   int slot = 0, phase = 0, taken = 0;
   bool alive = true;
@@ -371,17 +393,16 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
   };
 
   // ------------------------------------------------------------ one tile
-  // full: all its tokens are visible
-  auto tile = [&](auto full_tag) {
+  // From token j0 on; full: all its tokens are visible (of n, from `start` on or below the sinks)
+  auto tile = [&](auto full_tag, int j0, int n, int start) {
     constexpr bool kFull = decltype(full_tag)::value;
-    const int j0 = cur.t.token(cur.tile);
     auto visible = [&](int r) {
       const int j = j0 + r;
-      return kFull || (j < cur.t.n && (j < a.sinks || j >= cur.t.start));
+      return kFull || (j < n && (j < a.sinks || j >= start));
     };
-    float z[2][kN][4];
+    float z[MT][kN][4];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
@@ -389,28 +410,30 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
 
     arrive();
     const uint32_t base = ring + slot * C::kSlot;
-    float smax = 0.f;           // 4 bits: this lane's V scale
-    float vs[2][2], vr[2][2];   // V scale, rest of tokens 16 mt + grp (+ 8)
-    uint32_t vz[2][2];          // 1024 + V zero points of tokens 16 mt (+ 8) + 2 tig, 2 tig + 1
+    float smax = 0.f;            // 4 bits: the largest of this lane's V scales
+    float vs[MT][2], vr[MT][2];  // V scale, rest of tokens 16 mt + grp (+ 8)
+    uint32_t vz[MT][2];          // 1024 + V zero points of tokens 16 mt (+ 8) + 2 tig, 2 tig + 1
     if constexpr (Q4) {
-      // each lane prepares a token's parameters and leaves them for the warp, in the
-      // places of the ring that no copy writes
-      auto note = [&](int r) { return ring + (r >> 4) * C::kSlot + kQ4Slot + (r & 15) * 16; };
-      {
-        uint2 pr = lds64(base + 2 * kQ4Codes + lane * 8);
-        if (!visible(lane)) pr = uint2{0u, 0u};
-        uint4 n;
-        float rest;
-        n.x = zero_point<DT>(pr.x, rest);
-        n.y = __float_as_uint(rest);
-        n.z = zero_point<DT>(pr.y, rest);
-        n.w = __float_as_uint(rest);
-        sts128(note(lane), n);
-        smax = unpack2<DT>(pr.y).x;
-        __syncwarp();
-      }
+      // each lane prepares the parameters of a few tokens and leaves notes of
+      // them for the warp: zero point and scale of K (16 bits each), rest, the same of V
+      constexpr int kPer = C::kT / 2;   // notes per slot
+      static_assert(C::kSlots * kPer >= C::kT, "room for the notes");
+      auto note = [&](int r) { return ring + (r / kPer) * C::kSlot + C::kNotes + (r % kPer) * 16; };
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt) {
+      for (int i = 0; i < C::kT / 32; ++i) {
+        const int r = i * 32 + lane;
+        uint2 pr = lds64(base + 2 * C::kCodes + r * 8);
+        if (!visible(r)) pr = uint2{0u, 0u};
+        const float2 vp = unpack2<DT>(pr.y);
+        float kr, vrest;
+        const uint32_t zz = pack2<0>(zero_point(unpack2<DT>(pr.x), kr), zero_point(vp, vrest));
+        sts128(note(r), uint4{__byte_perm(pr.x, zz, 0x5410), __float_as_uint(kr), __byte_perm(pr.y, zz, 0x7610),
+                              __float_as_uint(vrest)});
+        smax = fmaxf(smax, vp.x);
+      }
+      __syncwarp();
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
         uint4 wv[2];
         float ks[2], kr[2];
         __half2 kz[2];
@@ -418,14 +441,14 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
         for (int e = 0; e < 2; ++e) {
           const int r = mt * 16 + e * 8 + grp;
           wv[e] = lds128(base + r * 64 + ((tig ^ ((r >> 1) & 3)) << 4));
-          const uint4 n = lds128(note(r));
-          ks[e] = unpack2<DT>(n.x).x;
-          kz[e] = high_twice(n.x);
-          kr[e] = __uint_as_float(n.y);
-          vs[mt][e] = unpack2<DT>(n.z).x;
-          const __half2 z2 = high_twice(n.z);
+          const uint4 n4 = lds128(note(r));
+          ks[e] = unpack2<DT>(n4.x).x;
+          kz[e] = high_twice(n4.x);
+          kr[e] = __uint_as_float(n4.y);
+          vs[mt][e] = unpack2<DT>(n4.z).x;
+          const __half2 z2 = high_twice(n4.z);
           vz[mt][e] = transpose8(*reinterpret_cast<const uint32_t*>(&z2));
-          vr[mt][e] = __uint_as_float(n.w);
+          vr[mt][e] = __uint_as_float(n4.w);
         }
         const uint32_t x[4] = {wv[0].x, wv[0].y, wv[0].z, wv[0].w}, y[4] = {wv[1].x, wv[1].y, wv[1].z, wv[1].w};
 #pragma unroll
@@ -450,10 +473,10 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
           const int r = mt * 16 + (lane & 15), ch = kk * 2 + (lane >> 4);
           uint32_t A[4];
-          ldmatrix_x4(base + (ch >> 3) * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4), A);
+          ldmatrix_x4(base + (ch >> 3) * C::kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4), A);
 #pragma unroll
           for (int nt = 0; nt < kN; ++nt) mma_16816<DT>(z[mt][nt], A, qf[kk][nt][0], qf[kk][nt][1]);
         }
@@ -461,7 +484,7 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
       next_slot();
       issue();
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
@@ -469,7 +492,7 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
     }
     if (!kFull) {
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (!visible(mt * 16 + (e >> 1) * 8 + grp))
@@ -483,9 +506,9 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
         for (int e = 0; e < 2; ++e) {
           const int col = nt * 8 + 2 * tig + e;
           if (col >= Gn) continue;
-          float* to = a.logits + ((int64_t)b * a.H + h0 + col) * a.cap32 + j0 + grp;
+          float* to = a.logits + ((int64_t)b * a.H + h0 + col) * a.lstride + j0 + grp;
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt) {
+          for (int mt = 0; mt < MT; ++mt) {
             to[mt * 16] = z[mt][nt][e];
             to[mt * 16 + 8] = z[mt][nt][2 + e];
           }
@@ -493,15 +516,17 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
     }
 
     // the running maximum (and R) where a logit (a scale) has passed it
-    bool over = false;
+    auto top = [&](int nt, int e) {
+      float t = fmaxf(z[0][nt][e], z[0][nt][2 + e]);
+#pragma unroll
+      for (int mt = 1; mt < MT; ++mt) t = fmaxf(t, fmaxf(z[mt][nt][e], z[mt][nt][2 + e]));
+      return t;
+    };
+    bool over = Q4 && smax > R;
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float t = fmaxf(fmaxf(z[0][nt][e], z[0][nt][2 + e]), fmaxf(z[1][nt][e], z[1][nt][2 + e]));
-        over = over || t > m[nt][e] + 15.f;
-      }
-    if (Q4) over = over || smax > R;
+      for (int e = 0; e < 2; ++e) over = over || top(nt, e) > m[nt][e] + 15.f;
     if (__any_sync(0xffffffffu, over)) {
       float shrink = 1.f;
       if (Q4) {
@@ -518,7 +543,7 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
         float f[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float t = fmaxf(fmaxf(z[0][nt][e], z[0][nt][2 + e]), fmaxf(z[1][nt][e], z[1][nt][2 + e]));
+          float t = top(nt, e);
 #pragma unroll
           for (int s = 4; s < 32; s <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, s));
           const float mn = fmaxf(m[nt][e], t - 7.f);
@@ -536,25 +561,23 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
     }
 
     // weights, and the column operand: high parts and residuals
-    uint32_t ph[2][kN][2], pl[2][kN][2];
+    constexpr int PT = Q4 ? 0 : DT;
+    uint32_t ph[MT][kN][2], pl[MT][kN][2];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int nt = 0; nt < kN; ++nt)
+      for (int t8 = 0; t8 < 2; ++t8) {
+        const float f = Q4 ? vs[mt][t8] * Rinv : 1.f;
 #pragma unroll
-        for (int t8 = 0; t8 < 2; ++t8) {
+        for (int nt = 0; nt < kN; ++nt) {
           float wgt[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const float p = ex2(z[mt][nt][2 * t8 + e] - m[nt][e]);
             l[nt][e] += p;
-            wgt[e] = p;
-            if (Q4) {
-              mp[nt][e] = fmaf(p, vr[mt][t8], mp[nt][e]);
-              wgt[e] = p * (vs[mt][t8] * Rinv);
-            }
+            if (Q4) mp[nt][e] = fmaf(p, vr[mt][t8], mp[nt][e]);
+            wgt[e] = Q4 ? p * f : p;
           }
-          constexpr int PT = Q4 ? 0 : DT;
           const uint32_t hi = pack2<PT>(wgt[0], wgt[1]);
           const float2 hf = unpack2<PT>(hi);
           const uint32_t lo = pack2<PT>(wgt[0] - hf.x, wgt[1] - hf.y);
@@ -565,57 +588,62 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
             pl[mt][nt][t8] = transpose8(lo);
           }
         }
+      }
 
     // O^T += V^T p.  mma rounds its sums towards zero, which over the thousands
     // of tiles of a long row adds up (to 2e-5 of the output); so a tile is
     // summed from zero and added in float32.
-    auto add_to = [&](int ct, const uint32_t (&A0)[4], const uint32_t (&A1)[4]) {   // both row blocks
+    auto times = [&](float (&t)[kN][4], const uint32_t (&A)[4], int mt) {
 #pragma unroll
       for (int nt = 0; nt < kN; ++nt) {
-        constexpr int PT = Q4 ? 0 : DT;
-        float t[4] = {0.f, 0.f, 0.f, 0.f};
-        mma_16816<PT>(t, A0, ph[0][nt][0], ph[0][nt][1]);
-        mma_16816<PT>(t, A1, ph[1][nt][0], ph[1][nt][1]);
-        if (!kFold) {
-          mma_16816<PT>(t, A0, pl[0][nt][0], pl[0][nt][1]);
-          mma_16816<PT>(t, A1, pl[1][nt][0], pl[1][nt][1]);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[ct][nt][e] += t[e];
+        mma_16816<PT>(t[nt], A, ph[mt][nt][0], ph[mt][nt][1]);
+        if (!kFold) mma_16816<PT>(t[nt], A, pl[mt][nt][0], pl[mt][nt][1]);
       }
     };
     if constexpr (Q4) {
-      const uint32_t vb = base + kQ4Codes;
+      const uint32_t vb = base + C::kCodes;
 #pragma unroll
       for (int x2 = 0; x2 < 2; ++x2) {   // 16-byte pieces 2 x2 and 2 x2 + 1 of the rows
-        uint32_t v[2][4];   // tokens 0-7 and 8-15 of a row block's piece 2 x2, then of 2 x2 + 1
+        uint32_t v[MT][4];   // tokens 0-7 and 8-15 of a row block's piece 2 x2, then of 2 x2 + 1
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
+        for (int mt = 0; mt < MT; ++mt) {
           const int r = mt * 16 + (lane & 15), c = 2 * x2 + (lane >> 4);
           ldmatrix_x4_trans(vb + r * 64 + ((c ^ ((r >> 1) & 3)) << 4), v[mt]);
         }
 #pragma unroll
         for (int xi = 0; xi < 2; ++xi) {
-          uint32_t u[2][2][4];
+          float t[2][kN][4];
 #pragma unroll
-          for (int mt = 0; mt < 2; ++mt)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-              codes_to_half(v[mt][2 * xi + e], *reinterpret_cast<const __half2*>(&vz[mt][e]), u[mt][e]);
+            for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t A0[4] = {u[0][0][2 * h], u[0][0][2 * h + 1], u[0][1][2 * h], u[0][1][2 * h + 1]};
-            const uint32_t A1[4] = {u[1][0][2 * h], u[1][0][2 * h + 1], u[1][1][2 * h], u[1][1][2 * h + 1]};
-            add_to((2 * x2 + xi) * 2 + h, A0, A1);
+              for (int e = 0; e < 4; ++e) t[h][nt][e] = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
+            uint32_t u0[4], u1[4];
+            codes_to_half(v[mt][2 * xi], *reinterpret_cast<const __half2*>(&vz[mt][0]), u0);
+            codes_to_half(v[mt][2 * xi + 1], *reinterpret_cast<const __half2*>(&vz[mt][1]), u1);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t A[4] = {u0[2 * h], u0[2 * h + 1], u1[2 * h], u1[2 * h + 1]};
+              times(t[h], A, mt);
+            }
           }
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[(2 * x2 + xi) * 2 + h][nt][e] += t[h][nt][e];
         }
       }
     } else {
       arrive();
       const uint32_t vb = ring + slot * C::kSlot;
-      uint32_t keep[2][2];   // tokens 2 tig, 2 tig + 1 and 8 after, of the row blocks
+      uint32_t keep[MT][2];   // tokens 2 tig, 2 tig + 1 and 8 after, of the row blocks
 #pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
+      for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           const int r = mt * 16 + e * 8 + 2 * tig;
@@ -623,19 +651,28 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
         }
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct) {
-        uint32_t A[2][4];
+        float t[kN][4];
 #pragma unroll
-        for (int mt = 0; mt < 2; ++mt) {
+        for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) t[nt][e] = 0.f;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
           const int r = mt * 16 + (lane & 7) + ((lane >> 4) << 3), ch = ct * 2 + ((lane >> 3) & 1);
-          ldmatrix_x4_trans(vb + (ch >> 3) * kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4), A[mt]);
+          uint32_t A[4];
+          ldmatrix_x4_trans(vb + (ch >> 3) * C::kBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4), A);
           if (!kFull) {   // rows that nobody sees may hold anything, NaN among it
-            A[mt][0] &= keep[mt][0];
-            A[mt][1] &= keep[mt][0];
-            A[mt][2] &= keep[mt][1];
-            A[mt][3] &= keep[mt][1];
+            A[0] &= keep[mt][0];
+            A[1] &= keep[mt][0];
+            A[2] &= keep[mt][1];
+            A[3] &= keep[mt][1];
           }
+          times(t, A, mt);
         }
-        add_to(ct, A[0], A[1]);
+#pragma unroll
+        for (int nt = 0; nt < kN; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[ct][nt][e] += t[nt][e];
       }
     }
     __syncwarp();
@@ -644,8 +681,7 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
   };
 
   // ------------------------------------------------------------ a pair's end
-  auto end_pair = [&](int item) {   // item: its last one here
-    const int x0 = item - cur.tile, x1 = x0 + cur.t.count;
+  auto end_pair = [&](int x0, int x1) {   // its items
     const bool whole = x0 >= i0 && x1 <= i1;
     const int64_t pbase = ((int64_t)w * 2 + (x0 >= i0 ? 1 : 0)) * HC;
 #pragma unroll
@@ -687,22 +723,31 @@ __global__ void __launch_bounds__(NW * 32, 1) hill_window_attn_kernel(const __gr
       }
   };
 
-  begin_pair();
-  for (int item = i0; item < i1; ++item) {
-    const int j0 = cur.t.token(cur.tile);
-    const bool full = j0 + kT <= cur.t.n && (j0 >= cur.t.start || j0 + kT <= a.sinks);
-    if (full) tile(Bool<true>{});
-    else tile(Bool<false>{});
-    if (!alive) break;
-    const bool last = cur.tile + 1 == cur.t.count;
-    if (last || item + 1 == i1) end_pair(item);
-    if (item + 1 < i1) {
-      advance(cur);
-      if (last) begin_pair();
+  for (int item = i0; alive;) {
+    begin_pair();
+    int count, n;
+    for (;;) {   // the pair's runs: the sinks, the window
+      const Tl t = row_tiles(cur.row);
+      count = t.count;
+      n = t.n;
+      const bool in_window = cur.tile >= t.sink;
+      const int lo = in_window ? t.start : 0, hi = in_window ? n : min(n, a.sinks);   // tokens all visible
+      const int run = min(cur.left, i1 - item);
+      for (int k = 0, j = cur.j; k < run && alive; ++k, j += C::kT) {
+        if (j >= lo && j + C::kT <= hi) tile(Bool<true>{}, j, n, t.start);
+        else tile(Bool<false>{}, j, n, t.start);
+      }
+      item += run;
+      cur.tile += run;
+      if (cur.tile == count || item == i1 || !alive) break;
+      next_run(cur);
     }
+    if (alive) end_pair(item - cur.tile, item - cur.tile + count);
+    if (item == i1) break;
+    next_run(cur);
   }
   // a wait ran out: the copies under way have to land before the CTA goes
-  while (!alive && taken < issued) {
+  while (!alive && taken < asked) {
     mbar_wait(bars + 8 * slot, phase, a.err);
     next_slot();
   }
@@ -796,7 +841,7 @@ __global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const
   const int h0 = a.kvh ? (row - b * a.Hkv) * a.G : 0, nh = a.kvh ? a.G : a.H;
   pdl_wait();
   pdl_launch_dependents();
-  const Tiles t(a.lens[row], a.cap, a.sinks, a.window);
+  const Tiles<32> t(a.lens[row], a.cap, a.sinks, a.window);
   const int i = blockIdx.x * 4 + (lane >> 3);
   if (blockIdx.x * 4 >= t.count) return;
   const bool there = i < t.count;
@@ -807,7 +852,7 @@ __global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const
     for (int h = warp; h < nh; h += kAccWarps) {
       const int64_t at = (int64_t)b * a.H + h0 + h;
       const float2 st = a.stats[at];
-      const float4 z = *reinterpret_cast<const float4*>(a.logits + at * a.cap32 + j);
+      const float4 z = *reinterpret_cast<const float4*>(a.logits + at * a.lstride + j);
       sum.x = fmaf(ex2(z.x - st.x), st.y, sum.x);
       sum.y = fmaf(ex2(z.y - st.x), st.y, sum.y);
       sum.z = fmaf(ex2(z.z - st.x), st.y, sum.z);
@@ -831,26 +876,26 @@ __global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const
     if (j + e < t.n && (j + e < a.sinks || j + e >= t.start)) to[e] += v[e];
 }
 
-template <bool Q4>
-constexpr int warps_for(int HC) {
-  return Q4 && HC < 16 ? 16 : 8;
-}
-
 template <int DT, bool Q4, int HC>
 cudaError_t launch_attn_t(const WindowArgs& a, int sms, cudaStream_t st) {
-  constexpr int NW = warps_for<Q4>(HC);
-  auto kern = hill_window_attn_kernel<DT, Q4, HC, NW>;
+  using C = Cfg<Q4, HC>;
+  auto kern = hill_window_attn_kernel<DT, Q4, HC>;
   static int cache[64] = {0};
-  const int smem = Cfg<Q4>::smem(NW);
-  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), smem, cache);
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), C::kSmem, cache);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kern, dim3(sms), dim3(NW * 32), smem, st, 0, a);
+  return launch_pdl(kern, dim3(sms), dim3(C::kNW * 32), C::kSmem, st, 0, a);
+}
+
+template <bool Q4>
+int warps_for(int HC) {
+  return HC == 4 ? Cfg<Q4, 4>::kNW : (HC == 8 ? Cfg<Q4, 8>::kNW : Cfg<Q4, 16>::kNW);
 }
 
 }  // namespace
 
 int window_heads_per_pass(int G) { return G <= 4 ? 4 : (G <= 8 ? 8 : 16); }
 int window_warps(bool q4, int HC) { return q4 ? warps_for<true>(HC) : warps_for<false>(HC); }
+int window_q4_tile(int HC) { return HC == 16 ? Cfg<true, 16>::kT : Cfg<true, 4>::kT; }
 int window_max_rows() { return kMaxRows; }
 
 cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms, cudaStream_t st, int* kernels) {
@@ -873,8 +918,7 @@ cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms,
   e = launch_pdl(hill_window_combine_kernel, dim3(a.H, a.B), dim3(warps * 32), 0, st, 0, a, HC, nw);
   *kernels = 2;
   if (e != cudaSuccess || !a.accum) return e;
-  const int64_t all = (a.cap + kT - 1) / kT;
-  const int64_t tiles = std::min<int64_t>(all, ((int64_t)a.sinks + kT - 1) / kT + ((int64_t)a.window + kT - 1) / kT + 1);
+  const int64_t tiles = std::min<int64_t>((a.cap + 31) / 32, ((int64_t)a.sinks + 31) / 32 + ((int64_t)a.window + 31) / 32 + 1);
   *kernels = 3;
   return launch_pdl(hill_window_accum_kernel, dim3((unsigned)std::max<int64_t>(1, (tiles + 3) / 4), a.kvh ? a.B * a.Hkv : a.B),
                     dim3(kAccWarps * 32), 0, st, 0, a);
