@@ -105,6 +105,15 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int 
       : "memory");
 }
 
+// (a & M) | 0x64006400 in one instruction (the compiler's own choice for the
+// C expression was two: 8 x 64K tokens of 32 heads 480 us, with this 412).
+template <uint32_t M>
+__device__ __forceinline__ uint32_t and_or(uint32_t a) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(a), "n"(M), "r"(0x64006400u));
+  return d;
+}
+
 // Four registers of two (code - zero point) each, as fp16 integers, from a
 // word of eight codes: codes (0, 4), (1, 5), (2, 6), (3, 7).  A code put under
 // the exponent of 1024 reads as 1024 + code (one place up: 1024 + 16 code),
@@ -116,7 +125,7 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, __half2 z1024, uint32_
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const uint32_t v = h ? w >> 8 : w;
-    uint32_t lo = (v & 0x000f000fu) | 0x64006400u, hi = (v & 0x00f000f0u) | 0x64006400u;
+    uint32_t lo = and_or<0x000f000fu>(v), hi = and_or<0x00f000f0u>(v);
     const __half2 a = __hsub2(*reinterpret_cast<__half2*>(&lo), z1024);
     const __half2 b = __hfma2(*reinterpret_cast<__half2*>(&hi), one16, z64);
     x[2 * h] = *reinterpret_cast<const uint32_t*>(&a);
@@ -314,8 +323,8 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   // ------------------------------------------------------------ state of a pair
   uint32_t qf[8][kN][2];                 // query heads as the column operand
   float o[8][kN][4];                     // O^T: channels x heads
-  float m[kN][2], l[kN][2];              // columns 2 tig, 2 tig + 1; l of this lane's tokens only
-  float cz[kN][2], cq[kN][2], mp[kN][2]; // 4 bits: factor of q . (code - z0); of the K rest; sum p V rest
+  float2 m[kN], l[kN];                   // columns 2 tig, 2 tig + 1; l of this lane's tokens only
+  float2 cz[kN], cq[kN], mp[kN];         // 4 bits: factor of q . (code - z0); of the K rest; sum p V rest
   float R = 0.f, Rinv = 0.f;             // 4 bits: the power of two above the V scales
   int b = 0, g = 0, h0 = 0, Gn = 0;      // the pair's sequence, KV head, first query head and heads
 
@@ -371,19 +380,12 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
           qf[2 * i + 1][nt][1] = pack2<0>(f[3] * up, f[7] * up);
         }
         const float cf = back * kLog2eInvSqrtD, qs = sum * kLog2eInvSqrtD;
-#pragma unroll
-        for (int e2 = 0; e2 < 2; ++e2) {
-          const int from = (kFold ? ((2 * tig + e2) & 3) : 2 * tig + e2) * 4;
-          cz[nt][e2] = __shfl_sync(0xffffffffu, cf, from);
-          cq[nt][e2] = __shfl_sync(0xffffffffu, qs, from);
-        }
+        const int from = (kFold ? ((2 * tig) & 3) : 2 * tig) * 4;
+        cz[nt] = float2{__shfl_sync(0xffffffffu, cf, from), __shfl_sync(0xffffffffu, cf, from + 4)};
+        cq[nt] = float2{__shfl_sync(0xffffffffu, qs, from), __shfl_sync(0xffffffffu, qs, from + 4)};
       }
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        m[nt][e] = kNegHuge;
-        l[nt][e] = 0.f;
-        mp[nt][e] = 0.f;
-      }
+      m[nt] = both(kNegHuge);
+      l[nt] = mp[nt] = both(0.f);
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
@@ -466,8 +468,12 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
 #pragma unroll
         for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            z[mt][nt][e] = fmaf(z[mt][nt][e] * ks[e >> 1], cz[nt][e & 1], kr[e >> 1] * cq[nt][e & 1]);
+          for (int e = 0; e < 2; ++e) {
+            const float2 v = fma2(mul2(float2{z[mt][nt][2 * e], z[mt][nt][2 * e + 1]}, both(ks[e])), cz[nt],
+                                  mul2(both(kr[e]), cq[nt]));
+            z[mt][nt][2 * e] = v.x;
+            z[mt][nt][2 * e + 1] = v.y;
+          }
       }
     } else {
 #pragma unroll
@@ -525,8 +531,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     bool over = Q4 && smax > R;
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) over = over || top(nt, e) > m[nt][e] + 15.f;
+      over = over || top(nt, 0) > m[nt].x + 15.f || top(nt, 1) > m[nt].y + 15.f;
     if (__any_sync(0xffffffffu, over)) {
       float shrink = 1.f;
       if (Q4) {
@@ -540,23 +545,22 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
       }
 #pragma unroll
       for (int nt = 0; nt < kN; ++nt) {
-        float f[2];
+        float2 t{top(nt, 0), top(nt, 1)};
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float t = top(nt, e);
-#pragma unroll
-          for (int s = 4; s < 32; s <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, s));
-          const float mn = fmaxf(m[nt][e], t - 7.f);
-          f[e] = ex2(m[nt][e] - mn);
-          m[nt][e] = mn;
-          l[nt][e] *= f[e];
-          if (Q4) mp[nt][e] *= f[e];
-          f[e] *= shrink;
+        for (int s = 4; s < 32; s <<= 1) {
+          t.x = fmaxf(t.x, __shfl_xor_sync(0xffffffffu, t.x, s));
+          t.y = fmaxf(t.y, __shfl_xor_sync(0xffffffffu, t.y, s));
         }
+        const float2 mn{fmaxf(m[nt].x, t.x - 7.f), fmaxf(m[nt].y, t.y - 7.f)};
+        float2 f{ex2(m[nt].x - mn.x), ex2(m[nt].y - mn.y)};
+        m[nt] = mn;
+        l[nt] = mul2(l[nt], f);
+        if (Q4) mp[nt] = mul2(mp[nt], f);
+        f = mul2(f, both(shrink));
 #pragma unroll
         for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[ct][nt][e] *= f[e & 1];
+          for (int e = 0; e < 4; ++e) o[ct][nt][e] *= e & 1 ? f.y : f.x;
       }
     }
 
@@ -570,17 +574,16 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         const float f = Q4 ? vs[mt][t8] * Rinv : 1.f;
 #pragma unroll
         for (int nt = 0; nt < kN; ++nt) {
-          float wgt[2];
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float p = ex2(z[mt][nt][2 * t8 + e] - m[nt][e]);
-            l[nt][e] += p;
-            if (Q4) mp[nt][e] = fmaf(p, vr[mt][t8], mp[nt][e]);
-            wgt[e] = Q4 ? p * f : p;
+          const float2 d = add2(float2{z[mt][nt][2 * t8], z[mt][nt][2 * t8 + 1]}, float2{-m[nt].x, -m[nt].y});
+          float2 p{ex2(d.x), ex2(d.y)};
+          l[nt] = add2(l[nt], p);
+          if (Q4) {
+            mp[nt] = fma2(p, both(vr[mt][t8]), mp[nt]);
+            p = mul2(p, both(f));
           }
-          const uint32_t hi = pack2<PT>(wgt[0], wgt[1]);
-          const float2 hf = unpack2<PT>(hi);
-          const uint32_t lo = pack2<PT>(wgt[0] - hf.x, wgt[1] - hf.y);
+          const uint32_t hi = pack2<PT>(p.x, p.y);
+          const float2 hf = unpack2<PT>(hi), rest = add2(p, float2{-hf.x, -hf.y});
+          const uint32_t lo = pack2<PT>(rest.x, rest.y);
           if (kFold) {
             ph[mt][nt][t8] = transpose8(tig < 2 ? hi : lo);
           } else {
@@ -593,6 +596,11 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     // O^T += V^T p.  mma rounds its sums towards zero, which over the thousands
     // of tiles of a long row adds up (to 2e-5 of the output); so a tile is
     // summed from zero and added in float32.
+    auto plus = [](float (&to)[4], const float (&t)[4], int e) {
+      const float2 v = add2(float2{to[e], to[e + 1]}, float2{t[e], t[e + 1]});
+      to[e] = v.x;
+      to[e + 1] = v.y;
+    };
     auto times = [&](float (&t)[kN][4], const uint32_t (&A)[4], int mt) {
 #pragma unroll
       for (int nt = 0; nt < kN; ++nt) {
@@ -635,7 +643,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
 #pragma unroll
             for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[(2 * x2 + xi) * 2 + h][nt][e] += t[h][nt][e];
+              for (int e = 0; e < 4; e += 2) plus(o[(2 * x2 + xi) * 2 + h][nt], t[h][nt], e);
         }
       }
     } else {
@@ -672,7 +680,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
 #pragma unroll
         for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[ct][nt][e] += t[nt][e];
+          for (int e = 0; e < 4; e += 2) plus(o[ct][nt], t[nt], e);
       }
     }
     __syncwarp();
@@ -688,7 +696,8 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float ls = l[nt][e], ms = mp[nt][e];
+        float ls = e ? l[nt].y : l[nt].x, ms = e ? mp[nt].y : mp[nt].x;
+        const float mx = e ? m[nt].y : m[nt].x;
 #pragma unroll
         for (int s = 4; s < 32; s <<= 1) {
           ls += __shfl_xor_sync(0xffffffffu, ls, s);
@@ -717,8 +726,8 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
           }
         }
         if (mine && grp == 0) {
-          if (!whole) a.part_ml[pbase + col] = float2{m[nt][e], ls};
-          else if (a.stats) a.stats[(int64_t)b * a.H + h0 + col] = float2{m[nt][e], 1.f / ls};
+          if (!whole) a.part_ml[pbase + col] = float2{mx, ls};
+          else if (a.stats) a.stats[(int64_t)b * a.H + h0 + col] = float2{mx, 1.f / ls};
         }
       }
   };
@@ -830,50 +839,74 @@ __global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps
 }
 
 // ---------------------------------------------------------------- importance
-// A CTA takes four visible tiles of a row: a lane four consecutive tokens, the
-// warps the heads in turn.  The sums are added in a fixed order.
+// A warp takes four visible tiles of 32 tokens of a row, a lane four
+// consecutive tokens, and every kSplit-th head; the parts are added in a fixed
+// order.  Bound by the logits' bytes (most still in L2); few tokens are split over
+// the heads to fill the SMs.
 constexpr int kAccWarps = 8;
 
+template <int kSplit>
 __global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const WindowArgs a) {
-  __shared__ float4 s_sum[kAccWarps][32];
+  __shared__ float4 s_sum[kSplit > 1 ? kAccWarps : 1][32];
   const int row = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int part = warp % kSplit, quad = blockIdx.x * (kAccWarps / kSplit) + warp / kSplit;
   const int b = a.kvh ? row / a.Hkv : row;
   const int h0 = a.kvh ? (row - b * a.Hkv) * a.G : 0, nh = a.kvh ? a.G : a.H;
   pdl_wait();
   pdl_launch_dependents();
   const Tiles<32> t(a.lens[row], a.cap, a.sinks, a.window);
-  const int i = blockIdx.x * 4 + (lane >> 3);
-  if (blockIdx.x * 4 >= t.count) return;
+  if (blockIdx.x * (kAccWarps / kSplit) * 4 >= t.count) return;
+  const int i = quad * 4 + (lane >> 3);
   const bool there = i < t.count;
   const int j = there ? t.token(i) + (lane & 7) * 4 : 0;
   float4 sum{0.f, 0.f, 0.f, 0.f};
   if (there) {
-#pragma unroll 4
-    for (int h = warp; h < nh; h += kAccWarps) {
-      const int64_t at = (int64_t)b * a.H + h0 + h;
-      const float2 st = a.stats[at];
-      const float4 z = *reinterpret_cast<const float4*>(a.logits + at * a.lstride + j);
-      sum.x = fmaf(ex2(z.x - st.x), st.y, sum.x);
-      sum.y = fmaf(ex2(z.y - st.x), st.y, sum.y);
-      sum.z = fmaf(ex2(z.z - st.x), st.y, sum.z);
-      sum.w = fmaf(ex2(z.w - st.x), st.y, sum.w);
+    const int64_t at = (int64_t)b * a.H + h0;
+    constexpr int kU = 8;   // heads in flight
+    for (int h = part; h < nh; h += kSplit * kU) {
+      float4 z[kU];
+      float2 st[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int hu = h + u * kSplit;
+        st[u] = hu < nh ? a.stats[at + hu] : float2{0.f, 0.f};
+        z[u] = hu < nh ? __ldcs(reinterpret_cast<const float4*>(a.logits + (at + hu) * a.lstride + j))
+                       : float4{0.f, 0.f, 0.f, 0.f};
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        sum.x = fmaf(ex2(z[u].x - st[u].x), st[u].y, sum.x);
+        sum.y = fmaf(ex2(z[u].y - st[u].x), st[u].y, sum.y);
+        sum.z = fmaf(ex2(z[u].z - st[u].x), st[u].y, sum.z);
+        sum.w = fmaf(ex2(z[u].w - st[u].x), st[u].y, sum.w);
+      }
     }
   }
-  s_sum[warp][lane] = sum;
-  __syncthreads();
-  if (warp || !there) return;
-  for (int k = 1; k < kAccWarps; ++k) {
-    const float4 v = s_sum[k][lane];
-    sum.x += v.x;
-    sum.y += v.y;
-    sum.z += v.z;
-    sum.w += v.w;
+  if (kSplit > 1) {
+    s_sum[warp][lane] = sum;
+    __syncthreads();
+    if (part) return;
+    for (int k = 1; k < kSplit; ++k) {
+      const float4 v = s_sum[warp + k][lane];
+      sum.x += v.x;
+      sum.y += v.y;
+      sum.z += v.z;
+      sum.w += v.w;
+    }
   }
+  if (!there) return;
   float* to = a.accum + (int64_t)row * a.cap + j;
   const float v[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
   for (int e = 0; e < 4; ++e)   // (a token that is not visible has weight 0, and its place is not touched)
     if (j + e < t.n && (j + e < a.sinks || j + e >= t.start)) to[e] += v[e];
+}
+
+template <int kSplit>
+cudaError_t launch_accum_t(const WindowArgs& a, int64_t tiles, cudaStream_t st) {
+  constexpr int kPer = kAccWarps / kSplit * 4;
+  return launch_pdl(hill_window_accum_kernel<kSplit>, dim3((unsigned)((tiles + kPer - 1) / kPer), a.kvh ? a.B * a.Hkv : a.B),
+                    dim3(kAccWarps * 32), 0, st, 0, a);
 }
 
 template <int DT, bool Q4, int HC>
@@ -920,8 +953,12 @@ cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms,
   if (e != cudaSuccess || !a.accum) return e;
   const int64_t tiles = std::min<int64_t>((a.cap + 31) / 32, ((int64_t)a.sinks + 31) / 32 + ((int64_t)a.window + 31) / 32 + 1);
   *kernels = 3;
-  return launch_pdl(hill_window_accum_kernel, dim3((unsigned)std::max<int64_t>(1, (tiles + 3) / 4), a.kvh ? a.B * a.Hkv : a.B),
-                    dim3(kAccWarps * 32), 0, st, 0, a);
+  // the heads of a row are split over 2 or 8 warps while the tokens alone leave
+  // more than three quarters (half) of the SMs' warps without work
+  const int64_t quads = (tiles + 3) / 4 * (a.kvh ? a.B * a.Hkv : a.B), nh = a.kvh ? a.G : a.H;
+  if (nh >= 8 && quads < sms * 16) return launch_accum_t<8>(a, std::max<int64_t>(tiles, 1), st);
+  if (nh >= 2 && quads < sms * 32) return launch_accum_t<2>(a, std::max<int64_t>(tiles, 1), st);
+  return launch_accum_t<1>(a, std::max<int64_t>(tiles, 1), st);
 }
 
 }  // namespace hill

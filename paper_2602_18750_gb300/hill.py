@@ -135,8 +135,14 @@ def _ptr(t) -> int | None:
     return t.data_ptr()
 
 
+# the handle of the current stream without a Stream object around it (2.5 us of a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int | None:
     if stream is None:
+        if _raw_stream is not None:
+            return _raw_stream(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, int):
         return stream
@@ -357,12 +363,15 @@ def hill_window_attn_q4(desc, q, k4, v4, params, lens, sinks, window, out, accum
 
 
 def _new_rows(desc, k_new, v_new, n_new, w_new) -> hill_new_rows:
-    want = (desc.batch, desc.num_kv_heads, k_new.shape[2], desc.head_dim)
-    for x in (k_new, v_new):
-        if tuple(x.shape) != want or x.stride(-1) != 1 or x.dtype != (torch.bfloat16 if desc.dtype else torch.float16):
-            raise ValueError(f"new rows must be {want} in the cache's type, the last dimension contiguous")
-    return hill_new_rows(k_new.data_ptr(), v_new.data_ptr(), *k_new.stride()[:3], *v_new.stride()[:3], want[2],
-                         _ptr(n_new), _ptr(w_new))
+    shape, dtype = k_new.shape, torch.bfloat16 if desc.dtype else torch.float16
+    if len(shape) != 4 or shape != v_new.shape or k_new.dtype != dtype or v_new.dtype != dtype:
+        raise ValueError("new rows must be [B][Hkv][T][d], K and V alike, in the cache's type")
+    (kb, kh, kn, k1), (vb, vh, vn, v1) = k_new.stride(), v_new.stride()
+    B, Hkv, T, d = shape
+    if B != desc.batch or Hkv != desc.num_kv_heads or d != desc.head_dim or k1 != 1 or v1 != 1:
+        raise ValueError(f"new rows must be [{desc.batch}][{desc.num_kv_heads}][T][{desc.head_dim}], the last dimension "
+                         f"contiguous; got {tuple(shape)}")
+    return hill_new_rows(k_new.data_ptr(), v_new.data_ptr(), kb, kh, kn, vb, vh, vn, T, _ptr(n_new), _ptr(w_new))
 
 
 def hill_cache_insert(desc, k_new, v_new, k_cache, v_cache, seen, pos, accum, sinks, recent, slots, n_new=None,
