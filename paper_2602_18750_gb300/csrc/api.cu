@@ -1112,7 +1112,7 @@ hill_status cache_insert(const hill_desc* desc, const hill_new_rows* n, void* k,
   a.recent = recent;
   a.err = di.err;
   int kernels = 0;
-  const cudaError_t e = launch_insert(a, desc->dtype, static_cast<cudaStream_t>(stream), &kernels);
+  const cudaError_t e = launch_insert(a, desc->dtype, di.sms, static_cast<cudaStream_t>(stream), &kernels);
   return from_cuda(counted(e, kernels));
 }
 

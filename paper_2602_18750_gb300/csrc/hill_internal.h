@@ -314,7 +314,7 @@ int window_max_rows();
 cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms, cudaStream_t st, int* kernels);
 
 // insert.cu
-cudaError_t launch_insert(const InsertArgs& a, int dtype, cudaStream_t st, int* kernels);
+cudaError_t launch_insert(const InsertArgs& a, int dtype, int sms, cudaStream_t st, int* kernels);
 cudaError_t launch_read_q4(const ReadQ4Args& a, int dtype, int max_rows, cudaStream_t st);
 
 }  // namespace hill

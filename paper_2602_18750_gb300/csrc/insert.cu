@@ -37,80 +37,108 @@ template <int DT> struct Pair;
 template <> struct Pair<0> { using T = __half2; };
 template <> struct Pair<1> { using T = __nv_bfloat162; };
 
-// One 16-bit row by the 16 lanes of a half-warp: 8 channels each.
-// Its 4-bit form: 4 bytes per lane, and (scale, min) in the low and high half of a word.
-// A code is the quotient (x - min) / scale, correctly rounded to float32, rounded to nearest even.
-// An IEEE division per channel made the long inserts compute-bound (158 us for 525
-// thousand token rows of K and V, against 50 of HBM time); the product with the approximate reciprocal is off
-// by less than 15 * 2^-22, so it gives the same code unless it lies that close to
-// half-way between two, and only rows with such a channel are divided.
+// One 16-bit row by 8 lanes, 16 channels each (8 from 8 l on, 8 from 64 + 8 l).
+// Its 4-bit form: 4 bytes of each, and (scale, min) in the low and high half of a word.
+// A code is (x - min) / scale rounded to nearest even; exact ties are not rare, as
+// rows and scales have few bits (every tenth row of normal fp16 values has one).
+// The quotient is the product with the approximate reciprocal, corrected once by
+// its remainder, which fma gives exactly (Markstein 1990): a quotient that
+// float32 holds, such as a tie, then comes out exactly.  (A library division per
+// channel took 158 us for 525 thousand token rows of K and V, against 50 of HBM
+// time; products whose near ties went another way 94 to 104.)
 template <int DT>
-__device__ __forceinline__ uint32_t encode_row(const uint4& raw, uint32_t& param) {
+__device__ __forceinline__ uint2 encode_row(const uint4 (&raw)[2], uint32_t& param) {
   using P = typename Pair<DT>::T;
-  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+  const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
   auto pr = [](const uint32_t& v) { return *reinterpret_cast<const P*>(&v); };
   auto un = [](const P& v) { return *reinterpret_cast<const uint32_t*>(&v); };
-  const uint32_t lo = un(__hmin2(__hmin2(pr(w[0]), pr(w[1])), __hmin2(pr(w[2]), pr(w[3]))));
-  const uint32_t hi = un(__hmax2(__hmax2(pr(w[0]), pr(w[1])), __hmax2(pr(w[2]), pr(w[3]))));
+  uint32_t lo = w[0], hi = w[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    lo = un(__hmin2(pr(lo), pr(w[i])));
+    hi = un(__hmax2(pr(hi), pr(w[i])));
+  }
   // (min, -max) side by side: halves 0 and 1 of each, joined
   uint32_t v = un(__hmin2(pr(__byte_perm(lo, hi, 0x5410) ^ 0x80000000u), pr(__byte_perm(lo, hi, 0x7632) ^ 0x80000000u)));
 #pragma unroll
-  for (int s = 1; s < 16; s <<= 1) v = un(__hmin2(pr(v), pr(__shfl_xor_sync(0xffffffffu, v, s))));
+  for (int s = 1; s < 8; s <<= 1) v = un(__hmin2(pr(v), pr(__shfl_xor_sync(0xffffffffu, v, s))));
   const float2 ends = unpack2<DT>(v);
   const float mn = ends.x, mx = -ends.y;
   param = pack2<DT>(__fdiv_rn(mx - mn, 15.f), mn);
   const float scale = unpack2<DT>(param).x;
-  float inv;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
-  constexpr float kRound = 12582912.f;   // 1.5 * 2^23: adding it rounds to an integer
-  float off = 0.f;
-  float2 c[4];
+  uint32_t y[16];   // the codes, in the low bits
+  if (scale > (DT ? 1e-30f : 1e-4f)) {
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(scale));
+    constexpr float kRound = 12582912.f;   // 1.5 * 2^23: adding it rounds to an integer, to even half-way
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float2 q = mul2(add2(unpack2<DT>(w[i]), both(-mn)), both(inv));
-    q.x = fminf(q.x, 15.f);
-    q.y = fminf(q.y, 15.f);
-    c[i] = add2(add2(q, both(kRound)), both(-kRound));
-    const float2 d = add2(q, float2{-c[i].x, -c[i].y});
-    off = fmaxf(off, fmaxf(fabsf(d.x), fabsf(d.y)));
-  }
-  if (!(scale > 1e-30f) || off > 0.49999f) {   // near a half, or a scale without a reciprocal
+    for (int i = 0; i < 8; ++i) {
+      const float2 t = add2(unpack2<DT>(w[i]), both(-mn));
+      float2 q = mul2(t, both(inv));
+      q = add2(fma2(fma2(q, both(-scale), t), both(inv), q), both(kRound));
+      y[2 * i] = __float_as_uint(q.x);
+      y[2 * i + 1] = __float_as_uint(q.y);
+    }
+  } else {   // no reciprocal, or a scale that rounding moved so far that a quotient passes 15
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
       const float2 x = unpack2<DT>(w[i]);
-      c[i].x = scale > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x.x - mn, scale)), 0.f), 15.f) : 0.f;
-      c[i].y = scale > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(x.y - mn, scale)), 0.f), 15.f) : 0.f;
+      y[2 * i] = scale > 0.f ? (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(x.x - mn, scale)), 0.f), 15.f) : 0u;
+      y[2 * i + 1] = scale > 0.f ? (uint32_t)(int)fminf(fmaxf(rintf(__fdiv_rn(x.y - mn, scale)), 0.f), 15.f) : 0u;
     }
   }
-  // eight codes: two bytes as one float of 16 bits
-  const float b01 = fmaf(fmaf(c[1].y, 16.f, c[1].x), 256.f, fmaf(c[0].y, 16.f, c[0].x));
-  const float b23 = fmaf(fmaf(c[3].y, 16.f, c[3].x), 256.f, fmaf(c[2].y, 16.f, c[2].x));
-  return __byte_perm(__float_as_uint(b01 + 8388608.f), __float_as_uint(b23 + 8388608.f), 0x5410);
+  auto low_bytes = [](uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+  };
+  return uint2{low_bytes(y[0], y[2], y[4], y[6]) + (low_bytes(y[1], y[3], y[5], y[7]) << 4),
+               low_bytes(y[8], y[10], y[12], y[14]) + (low_bytes(y[9], y[11], y[13], y[15]) << 4)};
 }
 
-// New token i of (b, g) into `slot`, by one warp: lanes 0-15 the key row, 16-31 the value row.
+// Two new tokens by one warp, half a warp each: 8 lanes the key row, 8 the value
+// row, of a KV head.
 template <int DT, bool Q4>
 struct RowCopy {
-  uint4 raw;
-  __device__ __forceinline__ void load(const InsertArgs& a, int b, int g, int i) {
-    const int lane = threadIdx.x & 31, c = (lane & 15) * 8;
-    const uint16_t* src = lane < 16 ? row16(a.k_new, b * a.kn_sb + g * a.kn_sh + i * a.kn_sn)
-                                    : row16(a.v_new, b * a.vn_sb + g * a.vn_sh + i * a.vn_sn);
-    raw = *reinterpret_cast<const uint4*>(src + c);
+  const uint16_t* src;
+  int64_t src_step, dst_step;   // per token; per slot
+  char* dst;
+  uint32_t* par;
+  __device__ __forceinline__ RowCopy(const InsertArgs& a, int b, int g) {
+    const int l8 = threadIdx.x & 7;
+    const bool v = threadIdx.x & 8;
+    src = (v ? row16(a.v_new, b * a.vn_sb + g * a.vn_sh) : row16(a.k_new, b * a.kn_sb + g * a.kn_sh)) + l8 * 8;
+    src_step = v ? a.vn_sn : a.kn_sn;
+    if (Q4) {
+      const int64_t bg = (int64_t)b * a.Hkv + g;
+      dst = reinterpret_cast<char*>((v ? a.v4 : a.k4) + bg * a.cap * 64 + l8 * 4);
+      par = reinterpret_cast<uint32_t*>(a.params + bg * a.cap32) + (v ? 1 : 0);
+      dst_step = 64;
+    } else {
+      dst = static_cast<char*>(v ? a.v : a.k) + 2 * (v ? b * a.v_sb + g * a.v_sh : b * a.k_sb + g * a.k_sh) + l8 * 16;
+      dst_step = 2 * (v ? a.v_sn : a.k_sn);
+    }
   }
-  __device__ __forceinline__ void store(const InsertArgs& a, int b, int g, int slot) const {
-    const int lane = threadIdx.x & 31, l16 = lane & 15;
+  // Token i of this lane's half; slot < 0: none.
+  __device__ __forceinline__ void load(int i, int slot, uint4 (&raw)[2]) const {
+    raw[0] = raw[1] = uint4{0u, 0u, 0u, 0u};
+    if (slot < 0) return;
+    const uint16_t* p = src + i * src_step;
+    raw[0] = ldg_nc128(p);
+    raw[1] = ldg_nc128(p + 64);
+  }
+  __device__ __forceinline__ void store(int slot, const uint4 (&raw)[2]) const {   // by whole warps
     if (!Q4) {
-      uint16_t* dst = lane < 16 ? const_cast<uint16_t*>(row16(a.k, b * a.k_sb + g * a.k_sh + slot * a.k_sn))
-                                : const_cast<uint16_t*>(row16(a.v, b * a.v_sb + g * a.v_sh + slot * a.v_sn));
-      *reinterpret_cast<uint4*>(dst + l16 * 8) = raw;
+      if (slot < 0) return;
+      char* p = dst + slot * dst_step;
+      *reinterpret_cast<uint4*>(p) = raw[0];
+      *reinterpret_cast<uint4*>(p + 128) = raw[1];
     } else {
       uint32_t param;
-      const uint32_t codes = encode_row<DT>(raw, param);
-      const int64_t bg = (int64_t)b * a.Hkv + g;
-      uint8_t* dst = (lane < 16 ? a.k4 : a.v4) + (bg * a.cap + slot) * 64;
-      reinterpret_cast<uint32_t*>(dst)[l16] = codes;
-      if (l16 == 0) reinterpret_cast<uint32_t*>(a.params + bg * a.cap32 + slot)[lane >> 4] = param;
+      const uint2 codes = encode_row<DT>(raw, param);
+      if (slot < 0) return;
+      char* p = dst + (int64_t)slot * 64;
+      *reinterpret_cast<uint32_t*>(p) = codes.x;
+      *reinterpret_cast<uint32_t*>(p + 32) = codes.y;
+      if ((threadIdx.x & 7) == 0) par[2 * (int64_t)slot] = param;
     }
   }
 };
@@ -264,56 +292,73 @@ __global__ void __launch_bounds__(kIT) hill_insert_kernel(const InsertArgs a) {
   if (tid == 0) a.seen[row] = seen + t;
   if (ROWS) {
     const int heads = a.kvh ? 1 : a.Hkv, g0 = a.kvh ? row - b * a.Hkv : 0;
-    for (int x = warp; x < heads * t; x += kIWarps) {
-      const int i = x / heads, g = g0 + x - i * heads;
-      RowCopy<DT, Q4> c;
-      c.load(a, b, g, i);
-      const int slot = slots[i];
-      if (slot >= 0) c.store(a, b, g, slot);
+    for (int x0 = warp * 2; x0 < heads * t; x0 += kIWarps * 2) {
+      const int x = x0 + (lane >> 4), i = x / heads, g = g0 + x - i * heads;
+      const int slot = i < t ? slots[i] : -1;
+      const RowCopy<DT, Q4> c(a, b, g);
+      uint4 raw[2];
+      c.load(i, slot, raw);
+      c.store(slot, raw);
     }
   }
 }
 
-// The new rows of (b, g) into the slots that hill_insert_kernel found, kRun to a warp at a time.
-constexpr int kRun = 4;
+// The new rows of (b, g) into the slots that hill_insert_kernel found: a CTA takes
+// `tokens` of them, a warp pairs of tokens in turn with kAhead pairs' rows under way
+// (with the rows of two pairs loaded, then written, 2.5 TB/s, three 7 % faster).
+constexpr int kAhead = 3;
+constexpr int kRowWarps = kRowThreads / 32;
+constexpr int kCtaTokens = 256;   // at most
 
 template <int DT, bool Q4>
-__global__ void __launch_bounds__(kRowThreads) hill_insert_rows_kernel(const InsertArgs a) {
+__global__ void __launch_bounds__(kRowThreads) hill_insert_rows_kernel(const InsertArgs a, int tokens) {
+  __shared__ int s_slot[kCtaTokens];
   const int g = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
-  const int i0 = (blockIdx.y * (kRowThreads / 32) + (threadIdx.x >> 5)) * kRun;
+  const int i0 = blockIdx.y * tokens, n = min(tokens, a.max_new - i0);
   pdl_wait();
-  const int32_t* slots = a.slots + (int64_t)(a.kvh ? (int)blockIdx.x : b) * a.max_new;
-  RowCopy<DT, Q4> c[kRun];
-  int slot[kRun];
+  const int32_t* slots = a.slots + (int64_t)(a.kvh ? (int)blockIdx.x : b) * a.max_new + i0;
+  for (int i = threadIdx.x; i < n; i += kRowThreads) s_slot[i] = slots[i];
+  __syncthreads();
+  const RowCopy<DT, Q4> c(a, b, g);
+  const int first = (threadIdx.x >> 5) * 2 + ((threadIdx.x >> 4) & 1);
+  uint4 raw[kAhead][2];
+  int slot[kAhead];
+  auto load = [&](int u, int i) {
+    slot[u] = i < n ? s_slot[i] : -1;
+    c.load(i0 + i, slot[u], raw[u]);
+  };
 #pragma unroll
-  for (int u = 0; u < kRun; ++u) slot[u] = i0 + u < a.max_new ? slots[i0 + u] : -1;
+  for (int u = 0; u < kAhead; ++u) load(u, first + u * 2 * kRowWarps);
+  for (int i = first; i - (first & 1) < n; i += kAhead * 2 * kRowWarps) {   // (whole warps)
 #pragma unroll
-  for (int u = 0; u < kRun; ++u)
-    if (slot[u] >= 0) c[u].load(a, b, g, i0 + u);
-#pragma unroll
-  for (int u = 0; u < kRun; ++u)
-    if (slot[u] >= 0) c[u].store(a, b, g, slot[u]);
+    for (int u = 0; u < kAhead; ++u) {
+      c.store(slot[u], raw[u]);
+      load(u, i + (kAhead + u) * 2 * kRowWarps);
+    }
+  }
 }
 
-// 4-bit rows as 16-bit values: a warp takes the key and the value row of a token.
+// 4-bit rows as 16-bit values: a warp takes the key and the value rows of kRead tokens.
+constexpr int kRead = 4;
+
 template <int DT>
 __global__ void __launch_bounds__(kRowThreads) hill_read_q4_kernel(const ReadQ4Args a) {
   const int g = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
   const int lane = threadIdx.x & 31, l16 = lane & 15;
   pdl_wait();
   const int begin = min(max(a.row_begin[b], 0), a.cap), end = min(max(a.row_end[b], 0), a.cap);
-  const int j0 = begin + (blockIdx.y * (kRowThreads / 32) + (threadIdx.x >> 5)) * kRun;
+  const int j0 = begin + (blockIdx.y * (kRowThreads / 32) + (threadIdx.x >> 5)) * kRead;
   const int64_t bg = blockIdx.x;
-  uint32_t codes[kRun];
-  uint2 par[kRun];
+  uint32_t codes[kRead];
+  uint2 par[kRead];
 #pragma unroll
-  for (int u = 0; u < kRun; ++u)
+  for (int u = 0; u < kRead; ++u)
     if (j0 + u < end) {
       codes[u] = reinterpret_cast<const uint32_t*>((lane < 16 ? a.k4 : a.v4) + (bg * a.cap + j0 + u) * 64)[l16];
       par[u] = a.params[bg * a.cap32 + j0 + u];
     }
 #pragma unroll
-  for (int u = 0; u < kRun; ++u)
+  for (int u = 0; u < kRead; ++u)
     if (j0 + u < end) {
       const float2 p = unpack2<DT>(lane < 16 ? par[u].x : par[u].y);
       uint32_t v[4];
@@ -328,7 +373,7 @@ __global__ void __launch_bounds__(kRowThreads) hill_read_q4_kernel(const ReadQ4A
 }
 
 template <int DT, bool Q4>
-cudaError_t launch_insert_t(const InsertArgs& a, cudaStream_t st, int* kernels) {
+cudaError_t launch_insert_t(const InsertArgs& a, int sms, cudaStream_t st, int* kernels) {
   // at most this many (token, KV head) rows per row of the state are written by its own CTA
   const int heads = a.kvh ? 1 : a.Hkv;
   const bool rows = (int64_t)a.max_new * heads <= 2 * kIWarps;
@@ -341,20 +386,22 @@ cudaError_t launch_insert_t(const InsertArgs& a, cudaStream_t st, int* kernels) 
   e = launch_pdl(kern, dim3(a.kvh ? a.B * a.Hkv : a.B), dim3(kIT), smem, st, 0, a);
   if (e != cudaSuccess || rows) return e;
   *kernels = 2;
-  const int per = kRowThreads / 32 * kRun;
-  return launch_pdl(hill_insert_rows_kernel<DT, Q4>, dim3(a.B * a.Hkv, (a.max_new + per - 1) / per), dim3(kRowThreads),
-                    0, st, 0, a);
+  // long CTAs where there are enough of them, about two to an SM
+  const int64_t heads_all = (int64_t)a.B * a.Hkv;
+  const int tokens = heads_all * (a.max_new / kCtaTokens) >= 2 * sms ? kCtaTokens : kCtaTokens / 4;
+  return launch_pdl(hill_insert_rows_kernel<DT, Q4>, dim3((unsigned)heads_all, (a.max_new + tokens - 1) / tokens),
+                    dim3(kRowThreads), 0, st, 0, a, tokens);
 }
 
 }  // namespace
 
-cudaError_t launch_insert(const InsertArgs& a, int dtype, cudaStream_t st, int* kernels) {
-  if (a.k4) return dtype ? launch_insert_t<1, true>(a, st, kernels) : launch_insert_t<0, true>(a, st, kernels);
-  return dtype ? launch_insert_t<1, false>(a, st, kernels) : launch_insert_t<0, false>(a, st, kernels);
+cudaError_t launch_insert(const InsertArgs& a, int dtype, int sms, cudaStream_t st, int* kernels) {
+  if (a.k4) return dtype ? launch_insert_t<1, true>(a, sms, st, kernels) : launch_insert_t<0, true>(a, sms, st, kernels);
+  return dtype ? launch_insert_t<1, false>(a, sms, st, kernels) : launch_insert_t<0, false>(a, sms, st, kernels);
 }
 
 cudaError_t launch_read_q4(const ReadQ4Args& a, int dtype, int max_rows, cudaStream_t st) {
-  const int per = kRowThreads / 32 * kRun;
+  const int per = kRowThreads / 32 * kRead;
   const dim3 grid(a.B * a.Hkv, (max_rows + per - 1) / per);
   return dtype ? launch_pdl(hill_read_q4_kernel<1>, grid, dim3(kRowThreads), 0, st, 0, a)
                : launch_pdl(hill_read_q4_kernel<0>, grid, dim3(kRowThreads), 0, st, 0, a);
