@@ -39,10 +39,15 @@
 // exponent of its unnormalised form, and the output was off by 1e-4.)
 //
 // Bound by HBM: 512 bytes per token and KV head in 16 bits, 136 in 4 bits.
+#include <cooperative_groups.h>
+
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "hill_internal.h"
+
+namespace cg = cooperative_groups;
 
 namespace hill {
 namespace {
@@ -173,7 +178,30 @@ struct Walk {
   int j, left;           // first token and length of the run
 };
 
-template <int DT, bool Q4, int HC>
+// Weighted sums of one query head, four channels per lane, from partials.
+struct Merged {
+  float m = kNegHuge, l = 0.f;
+  float4 o{0.f, 0.f, 0.f, 0.f};
+  template <int N>
+  __device__ __forceinline__ void add(const float2 (&ml)[N], const float4 (&v)[N]) {
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < N; ++u) mn = fmaxf(mn, ml[u].x);
+    const float f = ex2(m - mn);
+    m = mn;
+    l *= f;
+    o = float4{o.x * f, o.y * f, o.z * f, o.w * f};
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const float s = ex2(ml[u].x - mn);
+      l = fmaf(ml[u].y, s, l);
+      o = float4{fmaf(v[u].x, s, o.x), fmaf(v[u].y, s, o.y), fmaf(v[u].z, s, o.z), fmaf(v[u].w, s, o.w)};
+    }
+  }
+};
+
+// CL: a cluster of CTAs takes one (row, KV head, pass).
+template <int DT, bool Q4, int HC, bool CL>
 __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_kernel(const __grid_constant__ WindowArgs a) {
   using C = Cfg<Q4, HC>;
   using Tl = Tiles<C::kT>;
@@ -182,7 +210,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   constexpr bool kFold = HC == 4;              // residuals in columns 4 to 7
   extern __shared__ unsigned char wsm[];
   __shared__ __align__(8) uint64_t s_bar[NW * C::kSlots];
-  __shared__ int s_start[kMaxRows + 1];        // first item of each row
+  __shared__ int s_start[CL ? 1 : kMaxRows + 1];   // first item of each row
   __shared__ int s_sum[NW];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -200,8 +228,30 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
 
   pdl_wait();
 
-  // the list: every CTA scans the rows' tiles
   auto row_tiles = [&](int r) { return Tl(a.lens[r], a.cap, a.sinks, a.window); };
+  auto set_run = [&](Walk& c, const Tl& t) {
+    c.j = t.token(c.tile);
+    c.left = (c.tile < t.sink ? t.sink : t.count) - c.tile;
+  };
+  Walk cur{};
+  int i0 = 0, i1 = 0;   // this warp's items
+  int w = 0;            // its number
+  if constexpr (CL) {
+    cg::cluster_group cluster = cg::this_cluster();
+    const int size = cluster.num_blocks(), unit = blockIdx.x / size;
+    cur.row = unit / pairs;
+    cur.pair = unit - cur.row * pairs;
+    const Tl t = row_tiles(cur.row);
+    const int nw = min(size * NW, t.count);
+    w = warp * size + cluster.block_rank();
+    if (w < nw) {
+      i0 = first_item(w, t.count, nw);
+      i1 = first_item(w + 1, t.count, nw);
+      cur.tile = i0;
+      set_run(cur, t);
+    }
+  } else {
+  // the list: every CTA scans the rows' tiles
   int total = 0;
   for (int r0 = 0; r0 < rows; r0 += NW * 32) {
     const int r = r0 + (int)threadIdx.x;
@@ -227,18 +277,29 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   if (blockIdx.x == 0)
     for (int r = threadIdx.x; r <= rows; r += NW * 32) a.table[r] = s_start[r];
   // parts are numbered across the CTAs first, so that few tiles spread over all SMs
-  const int nw = min((int)gridDim.x * NW, total), w = warp * gridDim.x + blockIdx.x;
+  const int nw = min((int)gridDim.x * NW, total);
+  w = warp * gridDim.x + blockIdx.x;
   if (w >= nw) return;
-  const int i0 = first_item(w, total, nw), i1 = first_item(w + 1, total, nw);
+  i0 = first_item(w, total, nw);
+  i1 = first_item(w + 1, total, nw);
+  int lo = 0, hi = rows - 1;   // the last row that starts at or before i0
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (s_start[mid] <= i0) lo = mid;
+    else hi = mid - 1;
+  }
+  const Tl t = row_tiles(lo);
+  const int x = i0 - s_start[lo];
+  cur.row = lo;
+  cur.pair = x / t.count;
+  cur.tile = x - cur.pair * t.count;
+  set_run(cur, t);
+  }
 
   const uint64_t policy = l2_evict_first_policy();
-  auto set_run = [&](Walk& c, const Tl& t) {
-    c.j = t.token(c.tile);
-    c.left = (c.tile < t.sink ? t.sink : t.count) - c.tile;
-  };
   auto next_run = [&](Walk& c) {   // c.tile has passed the run; only while an item follows
     Tl t = row_tiles(c.row);
-    if (c.tile == t.count) {
+    if (!CL && c.tile == t.count) {
       c.tile = 0;
       if (++c.pair == pairs) {
         c.pair = 0;
@@ -252,21 +313,6 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   };
   auto seq_of = [&](const Walk& c) { return a.kvh ? c.row / a.Hkv : c.row; };
   auto head_of = [&](const Walk& c) { return a.kvh ? c.row % a.Hkv : c.pair / a.passes; };
-  Walk cur;
-  {
-    int lo = 0, hi = rows - 1;   // the last row that starts at or before i0
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_start[mid] <= i0) lo = mid;
-      else hi = mid - 1;
-    }
-    const Tl t = row_tiles(lo);
-    const int x = i0 - s_start[lo];
-    cur.row = lo;
-    cur.pair = x / t.count;
-    cur.tile = x - cur.pair * t.count;
-    set_run(cur, t);
-  }
 
   // ------------------------------------------------------------ the ring
   // A stage is a slot's content.  The state of what is asked for next:
@@ -689,9 +735,15 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   };
 
   // ------------------------------------------------------------ a pair's end
-  auto end_pair = [&](int x0, int x1) {   // its items
-    const bool whole = x0 >= i0 && x1 <= i1;
-    const int64_t pbase = ((int64_t)w * 2 + (x0 >= i0 ? 1 : 0)) * HC;
+  // Its items.  What is not whole goes, as a partial (max, sum, o) of each head, to the workspace; in a
+  // cluster to the warp's part of the ring, which is free then.
+  float* const ring_o = reinterpret_cast<float*>(wsm + (ring - smem_addr(wsm)));
+  float2* const ring_ml = reinterpret_cast<float2*>(ring_o + HC * kHeadDim);
+  auto end_pair = [&](int x0, int x1) {
+    const bool whole = !CL && x0 >= i0 && x1 <= i1;
+    const int64_t pbase = CL ? 0 : ((int64_t)w * 2 + (x0 >= i0 ? 1 : 0)) * HC;
+    float* const part_o = CL ? ring_o : a.part_o + pbase * kHeadDim;
+    float2* const part_ml = CL ? ring_ml : a.part_ml + pbase;
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
@@ -706,7 +758,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         const int col = nt * 8 + 2 * tig + e;
         const bool mine = col < Gn;
         const float inv = whole ? 1.f / ls : 1.f;
-        float* to = whole ? a.out + ((int64_t)b * a.H + h0 + col) * kHeadDim : a.part_o + (pbase + col) * kHeadDim;
+        float* to = whole ? a.out + ((int64_t)b * a.H + h0 + col) * kHeadDim : part_o + col * kHeadDim;
 #pragma unroll
         for (int ct = 0; ct < 8; ct += 2) {
           float v[4] = {o[ct][nt][e], o[ct][nt][2 + e], o[ct + 1][nt][e], o[ct + 1][nt][2 + e]};
@@ -726,13 +778,13 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
           }
         }
         if (mine && grp == 0) {
-          if (!whole) a.part_ml[pbase + col] = float2{mx, ls};
+          if (!whole) part_ml[col] = float2{mx, ls};
           else if (a.stats) a.stats[(int64_t)b * a.H + h0 + col] = float2{mx, 1.f / ls};
         }
       }
   };
 
-  for (int item = i0; alive;) {
+  for (int item = i0; item < i1 && alive;) {
     begin_pair();
     int count, n;
     for (;;) {   // the pair's runs: the sinks, the window
@@ -752,13 +804,67 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
       next_run(cur);
     }
     if (alive) end_pair(item - cur.tile, item - cur.tile + count);
-    if (item == i1) break;
-    next_run(cur);
+    if (item < i1) next_run(cur);
   }
   // a wait ran out: the copies under way have to land before the CTA goes
   while (!alive && taken < asked) {
     mbar_wait(bars + 8 * slot, phase, a.err);
     next_slot();
+  }
+  if constexpr (CL) {
+    // the warps' partials of each head are summed within every CTA, into the first warp's
+    // place, and these by the cluster, its CTAs taking the heads in turn
+    cg::cluster_group cluster = cg::this_cluster();
+    const int size = cluster.num_blocks(), rank = cluster.block_rank();
+    if (i0 >= i1 && lane < HC) ring_ml[lane] = float2{kNegHuge, 0.f};   // nothing of this warp
+    pdl_launch_dependents();
+    __syncthreads();
+    const int b = seq_of(cur), pass = cur.pair % a.passes, h0 = head_of(cur) * a.G + pass * HC;
+    const int heads = min(HC, a.G - pass * HC);
+    constexpr int kStride = C::kSlots * C::kSlot / 4;   // floats from warp to warp
+    float* const first = ring_o - warp * kStride;
+    constexpr int kU = 4;
+    for (int col = warp; col < heads; col += NW) {
+      Merged s;
+#pragma unroll
+      for (int u0 = 0; u0 < NW; u0 += kU) {
+        float2 ml[kU];
+        float4 v[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const float* from = first + (u0 + u) * kStride;
+          ml[u] = reinterpret_cast<const float2*>(from + HC * kHeadDim)[col];
+          v[u] = ml[u].y > 0.f ? *reinterpret_cast<const float4*>(from + col * kHeadDim + 4 * lane) : float4{0.f, 0.f, 0.f, 0.f};
+        }
+        s.add(ml, v);
+      }
+      *reinterpret_cast<float4*>(first + col * kHeadDim + 4 * lane) = s.o;
+      __syncwarp();   // every lane has read the head's max and sum
+      if (lane == 0) reinterpret_cast<float2*>(first + HC * kHeadDim)[col] = float2{s.m, s.l};
+    }
+    cluster.sync();
+    for (int col = rank + warp * size; col < heads; col += NW * size) {
+      Merged s;
+      for (int u0 = 0; u0 < size; u0 += kU) {
+        float2 ml[kU];
+        float4 v[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const float* from = cluster.map_shared_rank(first, u0 + u < size ? u0 + u : rank);
+          ml[u] = reinterpret_cast<const float2*>(from + HC * kHeadDim)[col];
+          v[u] = *reinterpret_cast<const float4*>(from + col * kHeadDim + 4 * lane);
+          if (u0 + u >= size) ml[u] = float2{kNegHuge, 0.f};
+        }
+        s.add(ml, v);
+      }
+      // (nothing visible: no sum, zeros)
+      const float inv = s.l > 0.f ? 1.f / s.l : 0.f;
+      const int64_t at = (int64_t)b * a.H + h0 + col;
+      const float4 out{s.o.x * inv, s.o.y * inv, s.o.z * inv, s.o.w * inv};
+      *reinterpret_cast<float4*>(a.out + at * kHeadDim + 4 * lane) = s.l > 0.f ? out : float4{0.f, 0.f, 0.f, 0.f};
+      if (a.stats && lane == 0) a.stats[at] = float2{s.m, inv};
+    }
+    cluster.sync();   // no CTA leaves while another reads its sums
   }
 }
 
@@ -786,8 +892,7 @@ __global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps
   const int x0 = start + pair * count, nw = min(warps_in_all, total);
   const int w0 = warp_of(x0, total, nw), w1 = warp_of(x0 + count - 1, total, nw);
   if (w0 == w1) return;   // written by its warp
-  float m = kNegHuge, l = 0.f;
-  float4 o{0.f, 0.f, 0.f, 0.f};
+  Merged s;
   constexpr int kU = 4;
   for (int w = w0 + warp; w <= w1; w += warps * kU) {
     float2 ml[kU];
@@ -803,28 +908,10 @@ __global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps
         v[u] = *reinterpret_cast<const float4*>(a.part_o + p * kHeadDim + 4 * lane);
       }
     }
-    float mn = m;
-#pragma unroll
-    for (int u = 0; u < kU; ++u) mn = fmaxf(mn, ml[u].x);
-    const float f = ex2(m - mn);
-    m = mn;
-    l *= f;
-    o.x *= f;
-    o.y *= f;
-    o.z *= f;
-    o.w *= f;
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const float s = ex2(ml[u].x - mn);
-      l = fmaf(ml[u].y, s, l);
-      o.x = fmaf(v[u].x, s, o.x);
-      o.y = fmaf(v[u].y, s, o.y);
-      o.z = fmaf(v[u].z, s, o.z);
-      o.w = fmaf(v[u].w, s, o.w);
-    }
+    s.add(ml, v);
   }
-  *reinterpret_cast<float4*>(&s_o[warp][4 * lane]) = o;
-  if (lane == 0) s_ml[warp] = float2{m, l};
+  *reinterpret_cast<float4*>(&s_o[warp][4 * lane]) = s.o;
+  if (lane == 0) s_ml[warp] = float2{s.m, s.l};
   __syncthreads();
   if (threadIdx.x >= kHeadDim) return;
   float M = kNegHuge, L = 0.f, O = 0.f;
@@ -909,14 +996,83 @@ cudaError_t launch_accum_t(const WindowArgs& a, int64_t tiles, cudaStream_t st) 
                     dim3(kAccWarps * 32), 0, st, 0, a);
 }
 
-template <int DT, bool Q4, int HC>
-cudaError_t launch_attn_t(const WindowArgs& a, int sms, cudaStream_t st) {
+// The most tiles of T tokens that a row may show.
+int64_t tiles_at_most(const WindowArgs& a, int T) {
+  const int64_t all = ((int64_t)a.cap + T - 1) / T;
+  return std::min<int64_t>(all, ((int64_t)a.sinks + T - 1) / T + ((int64_t)a.window + T - 1) / T + 1);
+}
+
+// Launch as clusters of `cluster` CTAs, or (0) as a list over `grid` CTAs.
+// count: only how many of those clusters fit the GPU at a time.
+template <int DT, bool Q4, int HC, bool CL>
+cudaError_t launch_attn_cl(const WindowArgs& a, int grid, int cluster, cudaStream_t st, int* count = nullptr) {
   using C = Cfg<Q4, HC>;
-  auto kern = hill_window_attn_kernel<DT, Q4, HC>;
+  auto kern = hill_window_attn_kernel<DT, Q4, HC, CL>;
   static int cache[64] = {0};
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), C::kSmem, cache);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kern, dim3(sms), dim3(C::kNW * 32), C::kSmem, st, 0, a);
+  if (!count) return launch_pdl(kern, dim3(grid), dim3(C::kNW * 32), C::kSmem, st, CL ? cluster : 0, a);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(cluster);
+  cfg.blockDim = dim3(C::kNW * 32);
+  cfg.dynamicSmemBytes = C::kSmem;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaOccupancyMaxActiveClusters(count, kern, &cfg);
+}
+
+constexpr int kSizes = 4;   // clusters of 1, 2, 4, 8 CTAs
+
+// One (row, KV head, pass) to a cluster, all of them at once, or the list over
+// all SMs with a second kernel that merges?  The list costs 2.5 us (and 2 us of the
+// host's time) for the merge; the clusters leave SMs idle: the rounds of tiles
+// that a warp makes, less those that it would make if all SMs had an equal share.
+// Measured (us, list / clusters; rounds - share): 4 bits 32 heads 8192 tokens
+// 16.0 / 13.6 (3 - 2.25), 8 KV heads 8192 tokens 11.0 / 10.3 (2 - 0.56), 4 KV heads
+// 8192 tokens 10.2 / 11.0 (2 - 0.28), 32 heads 32768 tokens 34.6 / 37.0 (11 - 9.0).
+// In 16 bits 64 CTAs already draw all of HBM's rate, and what counts is that: 8 KV
+// heads 32768 tokens 25.7 / 23.9 (16 - 6.7), 4 KV heads 14.7 / 23.8 (16 - 3.4, 32
+// CTAs); longer rows keep the list, which evens out rows of different lengths.
+constexpr double kIdleRounds = 1.45;
+constexpr int kStreamCtas = 64, kStreamRounds = 16;
+
+// *whole: the outputs are complete, there is nothing to merge.
+template <int DT, bool Q4, int HC>
+cudaError_t launch_attn_t(const WindowArgs& a, int sms, cudaStream_t st, bool* whole) {
+  using C = Cfg<Q4, HC>;
+  const int64_t tiles = tiles_at_most(a, C::kT), units = (int64_t)a.B * a.Hkv * a.passes;
+  *whole = false;
+  if (units <= sms) {
+    // the clusters of each size that fit at a time, asked once per device
+    static std::atomic<int> fit[64][kSizes];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    int size = 0;
+    for (int i = 0, s = 1; i < kSizes && (s == 1 || (int64_t)s / 2 * C::kNW < tiles); ++i, s *= 2) {
+      if (s * units > sms) break;
+      int n = fit[dev][i].load(std::memory_order_relaxed);
+      if (n == 0) {
+        e = launch_attn_cl<DT, Q4, HC, true>(a, 0, s, st, &n);
+        if (e != cudaSuccess) return e;
+        fit[dev][i].store(n > 0 ? n : -1, std::memory_order_relaxed);
+      }
+      if (n >= units) size = s;
+    }
+    if (size > 0) {
+      const int64_t per = (int64_t)size * C::kNW, rounds = (tiles + per - 1) / per;
+      const double share = (double)tiles * units / ((double)sms * C::kNW);
+      *whole = rounds - share <= kIdleRounds ||
+               (!Q4 && HC < 16 && units * size >= kStreamCtas && rounds <= kStreamRounds);
+      if (*whole) return launch_attn_cl<DT, Q4, HC, true>(a, (int)units * size, size, st);
+    }
+  }
+  return launch_attn_cl<DT, Q4, HC, false>(a, sms, 0, st);
 }
 
 template <bool Q4>
@@ -934,25 +1090,30 @@ int window_max_rows() { return kMaxRows; }
 cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms, cudaStream_t st, int* kernels) {
   const int HC = window_heads_per_pass(a.G);
   cudaError_t e = cudaErrorInvalidValue;
+  bool whole = false;
   auto go = [&](auto dt, auto is4) {
     constexpr int DT = decltype(dt)::value;
     constexpr bool Q4 = decltype(is4)::value;
-    return HC == 4 ? launch_attn_t<DT, Q4, 4>(a, sms, st)
-                   : HC == 8 ? launch_attn_t<DT, Q4, 8>(a, sms, st) : launch_attn_t<DT, Q4, 16>(a, sms, st);
+    return HC == 4   ? launch_attn_t<DT, Q4, 4>(a, sms, st, &whole)
+           : HC == 8 ? launch_attn_t<DT, Q4, 8>(a, sms, st, &whole)
+                     : launch_attn_t<DT, Q4, 16>(a, sms, st, &whole);
   };
   if (q4) e = dtype ? go(Int<1>{}, Bool<true>{}) : go(Int<0>{}, Bool<true>{});
   else e = dtype ? go(Int<1>{}, Bool<false>{}) : go(Int<0>{}, Bool<false>{});
   if (e != cudaSuccess) return e;
-  const int nw = sms * window_warps(q4, HC);
-  // about four partials to a warp
-  const int64_t per = nw / std::max<int64_t>(1, (int64_t)a.B * a.Hkv * a.passes) + 1;
-  int warps = 4;
-  while (warps < 32 && warps * 4 < per) warps <<= 1;
-  e = launch_pdl(hill_window_combine_kernel, dim3(a.H, a.B), dim3(warps * 32), 0, st, 0, a, HC, nw);
-  *kernels = 2;
+  *kernels = 1;
+  if (!whole) {
+    const int nw = sms * window_warps(q4, HC);
+    // about four partials to a warp
+    const int64_t per = nw / std::max<int64_t>(1, (int64_t)a.B * a.Hkv * a.passes) + 1;
+    int warps = 4;
+    while (warps < 32 && warps * 4 < per) warps <<= 1;
+    e = launch_pdl(hill_window_combine_kernel, dim3(a.H, a.B), dim3(warps * 32), 0, st, 0, a, HC, nw);
+    ++*kernels;
+  }
   if (e != cudaSuccess || !a.accum) return e;
-  const int64_t tiles = std::min<int64_t>((a.cap + 31) / 32, ((int64_t)a.sinks + 31) / 32 + ((int64_t)a.window + 31) / 32 + 1);
-  *kernels = 3;
+  ++*kernels;
+  const int64_t tiles = tiles_at_most(a, 32);
   // the heads of a row are split over 2 or 8 warps while the tokens alone leave
   // more than three quarters (half) of the SMs' warps without work
   const int64_t quads = (tiles + 3) / 4 * (a.kvh ? a.B * a.Hkv : a.B), nh = a.kvh ? a.G : a.H;
