@@ -117,11 +117,9 @@ struct RowCopy {
       dst_step = 2 * (v ? a.v_sn : a.k_sn);
     }
   }
-  // Token i of this lane's half; slot < 0: none.
+  // Token i of this lane's half; slot < 0: none (the first one is read instead).
   __device__ __forceinline__ void load(int i, int slot, uint4 (&raw)[2]) const {
-    raw[0] = raw[1] = uint4{0u, 0u, 0u, 0u};
-    if (slot < 0) return;
-    const uint16_t* p = src + i * src_step;
+    const uint16_t* p = src + (slot < 0 ? 0 : i) * src_step;
     raw[0] = ldg_nc128(p);
     raw[1] = ldg_nc128(p + 64);
   }
@@ -304,14 +302,16 @@ __global__ void __launch_bounds__(kIT) hill_insert_kernel(const InsertArgs a) {
 }
 
 // The new rows of (b, g) into the slots that hill_insert_kernel found: a CTA takes
-// `tokens` of them, a warp pairs of tokens in turn with kAhead pairs' rows under way
-// (with the rows of two pairs loaded, then written, 2.5 TB/s, three 7 % faster).
-constexpr int kAhead = 3;
+// `tokens` of them, a warp pairs of tokens in turn with kAhead pairs' rows under
+// way, four CTAs to an SM (66 thousand tokens of 8 KV heads into 4 bits 61 us, 5.3
+// TB/s; three or four pairs ahead 66 and 67; bound by the encoding's
+// instructions, 180 for two tokens' rows).
+constexpr int kAhead = 2;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kCtaTokens = 256;   // at most
 
 template <int DT, bool Q4>
-__global__ void __launch_bounds__(kRowThreads) hill_insert_rows_kernel(const InsertArgs a, int tokens) {
+__global__ void __launch_bounds__(kRowThreads, 4) hill_insert_rows_kernel(const InsertArgs a, int tokens) {
   __shared__ int s_slot[kCtaTokens];
   const int g = blockIdx.x % a.Hkv, b = blockIdx.x / a.Hkv;
   const int i0 = blockIdx.y * tokens, n = min(tokens, a.max_new - i0);

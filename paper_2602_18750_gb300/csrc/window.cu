@@ -296,7 +296,6 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   set_run(cur, t);
   }
 
-  const uint64_t policy = l2_evict_first_policy();
   auto next_run = [&](Walk& c) {   // c.tile has passed the run; only while an item follows
     Tl t = row_tiles(c.row);
     if (!CL && c.tile == t.count) {
@@ -318,11 +317,12 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   // A stage is a slot's content.  The state of what is asked for next:
   Walk ahead = cur;
   int to_ask = i1 - i0, run_left = cur.left, ask_b = seq_of(cur), ask_g = head_of(cur);
-  int asked = 0, slot_in = 0;   // stages
-  auto issue = [&] {            // the next stage, if there is one
+  bool ask_v = false;           // 16 bits: the tile's V
+  auto issue = [&](int at) {    // the next stage into slot `at`, if there is one
     if (to_ask == 0) return;
     if (lane == 0) {
-      const uint32_t dst = ring + slot_in * C::kSlot, bar = bars + 8 * slot_in;
+      const uint64_t policy = l2_evict_first_policy();
+      const uint32_t dst = ring + at * C::kSlot, bar = bars + 8 * at;
       if (Q4) {
         const int bg = ask_b * a.Hkv + ask_g;
         const uint32_t pbytes = min(C::kT, a.cap32 - ahead.j) * 8;   // (a row of parameters ends at cap32)
@@ -331,9 +331,8 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         tma_load_3d(dst + C::kCodes, &a.vmap, 0, ahead.j, bg, bar, policy);
         bulk_g2s(dst + 2 * C::kCodes, a.params + ((int64_t)bg * a.cap32 + ahead.j), pbytes, bar, policy);
       } else {
-        const bool v = asked & 1;
-        const void* map = v ? &a.vmap : &a.kmap;
-        const int dt = v ? a.vdim_tok : a.kdim_tok, dh = v ? a.vdim_head : a.kdim_head;
+        const void* map = ask_v ? &a.vmap : &a.kmap;
+        const int dt = ask_v ? a.vdim_tok : a.kdim_tok, dh = ask_v ? a.vdim_head : a.kdim_head;
         const int c1 = dt == 1 ? ahead.j : (dh == 1 ? ask_g : ask_b);
         const int c2 = dt == 2 ? ahead.j : (dh == 2 ? ask_g : ask_b);
         const int c3 = dt == 3 ? ahead.j : (dh == 3 ? ask_g : ask_b);
@@ -342,9 +341,10 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         tma_load_4d(dst + C::kBox, map, 64, c1, c2, c3, bar, policy);
       }
     }
-    ++asked;
-    slot_in = slot_in + 1 == C::kSlots ? 0 : slot_in + 1;
-    if (!Q4 && (asked & 1)) return;   // V of the same tile follows
+    if (!Q4) {
+      ask_v = !ask_v;
+      if (ask_v) return;   // V of the same tile follows
+    }
     ahead.j += C::kT;
     if (--to_ask > 0 && --run_left == 0) {
       ahead.tile += ahead.left;
@@ -354,17 +354,22 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
       ask_g = head_of(ahead);
     }
   };
-  int slot = 0, phase = 0, taken = 0;
+  int slot = 0, phase = 0;
   bool alive = true;
   auto arrive = [&] { alive = alive && mbar_wait(bars + 8 * slot, phase, a.err); };
   auto next_slot = [&] {
-    ++taken;
     if (++slot == C::kSlots) {
       slot = 0;
       phase ^= 1;
     }
   };
-  for (int i = 0; i < C::kSlots; ++i) issue();
+  auto refill = [&] {   // the slot has been read
+    __syncwarp();
+    const int at = slot;
+    next_slot();
+    issue(at);
+  };
+  for (int i = 0; i < C::kSlots; ++i) issue(i);
 
   // ------------------------------------------------------------ state of a pair
   uint32_t qf[8][kN][2];                 // query heads as the column operand
@@ -372,13 +377,11 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   float2 m[kN], l[kN];                   // columns 2 tig, 2 tig + 1; l of this lane's tokens only
   float2 cz[kN], cq[kN], mp[kN];         // 4 bits: factor of q . (code - z0); of the K rest; sum p V rest
   float R = 0.f, Rinv = 0.f;             // 4 bits: the power of two above the V scales
-  int b = 0, g = 0, h0 = 0, Gn = 0;      // the pair's sequence, KV head, first query head and heads
+  int head0 = 0, Gn = 0;                 // the pair's first query head (of all sequences') and heads
 
   auto begin_pair = [&] {
-    b = seq_of(cur);
-    g = head_of(cur);
-    const int pass = cur.pair % a.passes;
-    h0 = g * a.G + pass * HC;
+    const int b = seq_of(cur), pass = cur.pair % a.passes, h0 = head_of(cur) * a.G + pass * HC;
+    head0 = b * a.H + h0;
     Gn = min(HC, a.G - pass * HC);
 #pragma unroll
     for (int nt = 0; nt < kN; ++nt) {
@@ -441,9 +444,11 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   };
 
   // ------------------------------------------------------------ one tile
-  // From token j0 on; full: all its tokens are visible (of n, from `start` on or below the sinks)
-  auto tile = [&](auto full_tag, int j0, int n, int start) {
+  // From token j0 on; full: all its tokens are visible
+  auto tile = [&](auto full_tag, int j0) {
     constexpr bool kFull = decltype(full_tag)::value;
+    const Tl shown = kFull ? Tl(0, 0, 0, 0) : row_tiles(cur.row);
+    const int n = shown.n, start = shown.start;
     auto visible = [&](int r) {
       const int j = j0 + r;
       return kFull || (j < n && (j < a.sinks || j >= start));
@@ -532,9 +537,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
 #pragma unroll
           for (int nt = 0; nt < kN; ++nt) mma_16816<DT>(z[mt][nt], A, qf[kk][nt][0], qf[kk][nt][1]);
         }
-      __syncwarp();
-      next_slot();
-      issue();
+      refill();
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -558,7 +561,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         for (int e = 0; e < 2; ++e) {
           const int col = nt * 8 + 2 * tig + e;
           if (col >= Gn) continue;
-          float* to = a.logits + ((int64_t)b * a.H + h0 + col) * a.lstride + j0 + grp;
+          float* to = a.logits + (int64_t)(head0 + col) * a.lstride + j0 + grp;
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt) {
             to[mt * 16] = z[mt][nt][e];
@@ -729,9 +732,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
           for (int e = 0; e < 4; e += 2) plus(o[ct][nt], t[nt], e);
       }
     }
-    __syncwarp();
-    next_slot();
-    issue();
+    refill();
   };
 
   // ------------------------------------------------------------ a pair's end
@@ -758,7 +759,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         const int col = nt * 8 + 2 * tig + e;
         const bool mine = col < Gn;
         const float inv = whole ? 1.f / ls : 1.f;
-        float* to = whole ? a.out + ((int64_t)b * a.H + h0 + col) * kHeadDim : part_o + col * kHeadDim;
+        float* to = whole ? a.out + (int64_t)(head0 + col) * kHeadDim : part_o + col * kHeadDim;
 #pragma unroll
         for (int ct = 0; ct < 8; ct += 2) {
           float v[4] = {o[ct][nt][e], o[ct][nt][2 + e], o[ct + 1][nt][e], o[ct + 1][nt][2 + e]};
@@ -779,24 +780,23 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         }
         if (mine && grp == 0) {
           if (!whole) part_ml[col] = float2{mx, ls};
-          else if (a.stats) a.stats[(int64_t)b * a.H + h0 + col] = float2{mx, 1.f / ls};
+          else if (a.stats) a.stats[head0 + col] = float2{mx, 1.f / ls};
         }
       }
   };
 
   for (int item = i0; item < i1 && alive;) {
     begin_pair();
-    int count, n;
+    int count;
     for (;;) {   // the pair's runs: the sinks, the window
       const Tl t = row_tiles(cur.row);
       count = t.count;
-      n = t.n;
       const bool in_window = cur.tile >= t.sink;
-      const int lo = in_window ? t.start : 0, hi = in_window ? n : min(n, a.sinks);   // tokens all visible
+      const int lo = in_window ? t.start : 0, hi = in_window ? t.n : min(t.n, a.sinks);   // tokens all visible
       const int run = min(cur.left, i1 - item);
       for (int k = 0, j = cur.j; k < run && alive; ++k, j += C::kT) {
-        if (j >= lo && j + C::kT <= hi) tile(Bool<true>{}, j, n, t.start);
-        else tile(Bool<false>{}, j, n, t.start);
+        if (j >= lo && j + C::kT <= hi) tile(Bool<true>{}, j);
+        else tile(Bool<false>{}, j);
       }
       item += run;
       cur.tile += run;
@@ -807,7 +807,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     if (item < i1) next_run(cur);
   }
   // a wait ran out: the copies under way have to land before the CTA goes
-  while (!alive && taken < asked) {
+  for (int i = 0; !alive && i < C::kSlots; ++i) {
     mbar_wait(bars + 8 * slot, phase, a.err);
     next_slot();
   }
