@@ -3,18 +3,19 @@
 // them), from 16-bit K/V or from a 4-bit cache, with the attention weights
 // optionally added to the running importance (Sec. 4.1 column sums).
 //
-// Three kernels, the last only with an importance:
-//  hill_window_attn_kernel   streams K and V once.  The work is a list of
-//    tiles of 32 tokens, ordered (sequence, KV head, pass of query heads, tile);
-//    every warp of the grid owns one contiguous part of it and brings its tiles
-//    into a ring of its own in shared memory by TMA.  A warp that holds all
-//    tiles of a (sequence, KV head, pass) writes the output; the others leave
-//    (max, sum, o) partials.
+//  hill_window_attn_kernel   streams K and V once.  Every warp brings the tiles
+//    that are its own into a ring of its own in shared memory by TMA.  The tiles
+//    are dealt out in one of two ways (launch_attn_t):
+//    a cluster of CTAs takes each (row of lens, KV head, pass of query heads),
+//    and its warps' sums are merged in shared memory; or all of them form one list
+//    that the warps of the grid share evenly, and a warp that holds all
+//    tiles of one writes its output, while the others leave (max, sum, o) partials.
 //  hill_window_combine_kernel merges those partials.
 //  hill_window_accum_kernel  adds sum_h 2^(z - m_h) / l_h to the importance,
-//    from the logits that the first kernel stored.
+//    from the logits that the first kernel stored (it reads them, 4 bytes per token and query head,
+//    mostly from L2).
 //
-// Mathematics of a tile, 32 tokens as two row blocks of 16 (mma m16n8k16):
+// Mathematics of a tile, row blocks of 16 tokens (mma m16n8k16):
 //  S = K q^T with the tokens as rows and the pass's query heads as columns.
 //  The weights p = 2^(z - m) of a running maximum m are then already laid out
 //  by column, and an 8x8 transpose of each block (movmatrix) makes them the
@@ -38,7 +39,14 @@
 // takes masks alone, lost 10 bits: mma aligns a subnormal's products by the
 // exponent of its unnormalised form, and the output was off by 1e-4.)
 //
-// Bound by HBM: 512 bytes per token and KV head in 16 bits, 136 in 4 bits.
+// In 16 bits bound by HBM, 512 bytes per token and KV head: 4 x 16-32K tokens of 32
+// heads with their weights 253 us, 6.7 TB/s; 1 x 128K of 8 KV heads and 64 query
+// heads 83 us, 6.5 TB/s.  In 4 bits, 136 bytes, the instructions that make fp16
+// of the codes keep it from there: a tile of 32 tokens takes 600, 290 of them for the
+// codes, of the 700 that fit its share of HBM's time: 8 x 64K tokens of 32 heads
+// 392 us, 5.8 TB/s (346 us with the codes passed on unconverted).  Tiles of 64
+// tokens and 12 warps: 32 tokens and 12 or 16 warps took 462 us at the time, 64
+// tokens and 8 warps 425 against 402.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -88,12 +96,22 @@ struct Tiles {
   __device__ __forceinline__ int token(int i) const { return (i < sink ? i : first + i - sink) * T; }
 };
 
-// The part of the list that warp w of nw (at most as many as tiles) owns, and
-// the warp that owns item x.
-__device__ __forceinline__ int first_item(int w, int total, int nw) { return (int)((int64_t)w * total / nw); }
-__device__ __forceinline__ int warp_of(int x, int total, int nw) {
-  return (int)((((int64_t)x + 1) * nw - 1) / total);
-}
+// A list of items dealt out to n warps (at most as many as items, n < 2^15) in
+// parts of equal length: where part w begins, floor(w items / n), and the warp that owns item x.
+struct Parts {
+  int n, each, rest;
+  float per;
+  __device__ __forceinline__ Parts(int items, int n_) : n(n_), each(items / n_), rest(items - items / n_ * n_) {
+    per = __fdividef((float)n_, (float)items);
+  }
+  __device__ __forceinline__ int begin(int w) const { return w * each + w * rest / n; }
+  __device__ __forceinline__ int of(int x) const {
+    int w = min((int)((float)x * per), n - 1);   // within 1
+    while (begin(w) > x) --w;
+    while (w + 1 < n && begin(w + 1) <= x) ++w;
+    return w;
+  }
+};
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t d;
@@ -245,8 +263,9 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     const int nw = min(size * NW, t.count);
     w = warp * size + cluster.block_rank();
     if (w < nw) {
-      i0 = first_item(w, t.count, nw);
-      i1 = first_item(w + 1, t.count, nw);
+      const Parts parts(t.count, nw);
+      i0 = parts.begin(w);
+      i1 = parts.begin(w + 1);
       cur.tile = i0;
       set_run(cur, t);
     }
@@ -280,8 +299,9 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   const int nw = min((int)gridDim.x * NW, total);
   w = warp * gridDim.x + blockIdx.x;
   if (w >= nw) return;
-  i0 = first_item(w, total, nw);
-  i1 = first_item(w + 1, total, nw);
+  const Parts parts(total, nw);
+  i0 = parts.begin(w);
+  i1 = parts.begin(w + 1);
   int lo = 0, hi = rows - 1;   // the last row that starts at or before i0
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -520,7 +540,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float2 v = fma2(mul2(float2{z[mt][nt][2 * e], z[mt][nt][2 * e + 1]}, both(ks[e])), cz[nt],
+            const float2 v = fma2(float2{z[mt][nt][2 * e], z[mt][nt][2 * e + 1]}, mul2(both(ks[e]), cz[nt]),
                                   mul2(both(kr[e]), cq[nt]));
             z[mt][nt][2 * e] = v.x;
             z[mt][nt][2 * e + 1] = v.y;
@@ -890,7 +910,8 @@ __global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps
     return;
   }
   const int x0 = start + pair * count, nw = min(warps_in_all, total);
-  const int w0 = warp_of(x0, total, nw), w1 = warp_of(x0 + count - 1, total, nw);
+  const Parts parts(total, nw);
+  const int w0 = parts.of(x0), w1 = parts.of(x0 + count - 1);
   if (w0 == w1) return;   // written by its warp
   Merged s;
   constexpr int kU = 4;
@@ -949,7 +970,7 @@ __global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const
   float4 sum{0.f, 0.f, 0.f, 0.f};
   if (there) {
     const int64_t at = (int64_t)b * a.H + h0;
-    constexpr int kU = 8;   // heads in flight
+    constexpr int kU = 4;   // heads in flight
     for (int h = part; h < nh; h += kSplit * kU) {
       float4 z[kU];
       float2 st[kU];

@@ -140,6 +140,38 @@ def test_split_and_joined(H, shape, q4):
     assert torch.equal(a, c.out) and torch.equal(b, accum)   # bit for bit, whatever the workspace held
 
 
+@pytest.mark.parametrize("q4", [False, True], ids=["16bit", "q4"])
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("heads", [(4, 4), (8, 2), (14, 2), (16, 2), (12, 1), (32, 1)], ids=lambda h: f"{h[0]}x{h[1]}")
+def test_both_forms(H, heads, dtype, q4):
+    """Short rows go to clusters, long ones to the list of tiles with its merge: the launches say so, and both are right."""
+    cap = 30000
+    c = Case(H, 3, *heads, cap, dtype, q4, seed=43)
+    for lens, sinks, window, form in [([1000, 700, 64], 0, 900, 1), ([cap, 12345, 1], 0, ALL, 2), ([cap, 20000, 0], 100, 25000, 2)]:
+        n0 = H.hill_kernel_launches()
+        got = c.attend(lens, sinks, window)
+        if not q4 and heads == (4, 4):
+            form = 1   # 12 clusters of 8 CTAs draw all of HBM's rate: they keep rows of up to 16 tiles a warp, these are 15
+        assert H.hill_kernel_launches() - n0 == form
+        ref, w, bound, wb = c.reference(lens, sinks, window)
+        check(got, ref, bound)
+        accum = torch.zeros(3, cap, device="cuda")
+        n0 = H.hill_kernel_launches()
+        check(c.attend(lens, sinks, window, accum), ref, bound)
+        assert H.hill_kernel_launches() - n0 == form + 1
+        check(accum.cpu().numpy().astype(np.float64), w, wb + 2.0 ** -23 * w)
+
+
+def test_values_far_from_one(H):
+    """4-bit rows of 2^100 under queries of 2^-100, and the reverse: the logits are ordinary, their factors are not."""
+    for scale in (2.0 ** 100, 2.0 ** -100):
+        c = Case(H, 1, 8, 2, 300, "bf16", True, seed=47, scale=scale)
+        c.q = (c.q.float() / scale / 8).bfloat16()
+        c.desc = H.make_desc_q4(c.q, c.k4)
+        ref, w, bound, _ = c.reference([300], 0, ALL)
+        check(c.attend([300], 0, ALL), ref, bound)
+
+
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), "lowest"])
 def test_hidden_slots_do_not_matter(H, bad, dtype):
