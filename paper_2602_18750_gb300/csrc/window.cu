@@ -967,6 +967,15 @@ __global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const
   const int i = quad * 4 + (lane >> 3);
   const bool there = i < t.count;
   const int j = there ? t.token(i) + (lane & 7) * 4 : 0;
+  // what is there already, asked for first (a token that is not visible has weight 0, and its place is not touched)
+  float* to = a.accum + (int64_t)row * a.cap + j;
+  float old[4];
+  bool see[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    see[e] = there && part == 0 && j + e < t.n && (j + e < a.sinks || j + e >= t.start);
+    old[e] = see[e] ? to[e] : 0.f;
+  }
   float4 sum{0.f, 0.f, 0.f, 0.f};
   if (there) {
     const int64_t at = (int64_t)b * a.H + h0;
@@ -1002,12 +1011,10 @@ __global__ void __launch_bounds__(kAccWarps * 32) hill_window_accum_kernel(const
       sum.w += v.w;
     }
   }
-  if (!there) return;
-  float* to = a.accum + (int64_t)row * a.cap + j;
   const float v[4] = {sum.x, sum.y, sum.z, sum.w};
 #pragma unroll
-  for (int e = 0; e < 4; ++e)   // (a token that is not visible has weight 0, and its place is not touched)
-    if (j + e < t.n && (j + e < a.sinks || j + e >= t.start)) to[e] += v[e];
+  for (int e = 0; e < 4; ++e)
+    if (see[e]) to[e] = old[e] + v[e];
 }
 
 template <int kSplit>

@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -63,6 +64,10 @@ class hill_new_rows(ctypes.Structure):
     ]
 
 
+# the same in one call (a fifth of the time that filling the fields takes)
+_pack_rows = struct.Struct("@PPqqqqqqiPP").pack
+assert struct.calcsize("@PPqqqqqqiPP") == ctypes.sizeof(hill_new_rows)
+
 _lib = None
 
 
@@ -99,9 +104,9 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.hill_window_workspace_bytes.restype = SZ
     lib.hill_window_attn.argtypes = [D, P, P, P, P, I32, I32, I32, P, P, P, SZ, P]
     lib.hill_window_attn_q4.argtypes = [D, P, P, P, P, P, I32, I32, I32, P, P, P, SZ, P]
-    N = ctypes.POINTER(hill_new_rows)
-    lib.hill_cache_insert.argtypes = [D, N, P, P, P, P, P, I32, I32, I32, P, P]
-    lib.hill_cache_insert_q4.argtypes = [D, N, P, P, P, P, P, P, I32, I32, I32, P, P]
+    # (the second: a hill_new_rows, by reference or packed)
+    lib.hill_cache_insert.argtypes = [D, P, P, P, P, P, P, I32, I32, I32, P, P]
+    lib.hill_cache_insert_q4.argtypes = [D, P, P, P, P, P, P, P, I32, I32, I32, P, P]
     lib.hill_cache_read_q4.argtypes = [D, P, P, P, P, P, I32, P, P, P]
     lib.hill_sync_status.argtypes = [P]
     lib.hill_status_string.argtypes = [I32]
@@ -128,11 +133,7 @@ def _check(status: int, where: str) -> None:
 
 
 def _ptr(t) -> int | None:
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
+    return t if t is None or isinstance(t, int) else t.data_ptr()
 
 
 # the handle of the current stream without a Stream object around it (2.5 us of a call)
@@ -362,7 +363,8 @@ def hill_window_attn_q4(desc, q, k4, v4, params, lens, sinks, window, out, accum
                                       _stream(stream)), "hill_window_attn_q4")
 
 
-def _new_rows(desc, k_new, v_new, n_new, w_new) -> hill_new_rows:
+def _new_rows(desc, k_new, v_new, n_new, w_new) -> bytes:
+    """The hill_new_rows of new tokens, packed."""
     shape, dtype = k_new.shape, torch.bfloat16 if desc.dtype else torch.float16
     if len(shape) != 4 or shape != v_new.shape or k_new.dtype != dtype or v_new.dtype != dtype:
         raise ValueError("new rows must be [B][Hkv][T][d], K and V alike, in the cache's type")
@@ -371,14 +373,14 @@ def _new_rows(desc, k_new, v_new, n_new, w_new) -> hill_new_rows:
     if B != desc.batch or Hkv != desc.num_kv_heads or d != desc.head_dim or k1 != 1 or v1 != 1:
         raise ValueError(f"new rows must be [{desc.batch}][{desc.num_kv_heads}][T][{desc.head_dim}], the last dimension "
                          f"contiguous; got {tuple(shape)}")
-    return hill_new_rows(k_new.data_ptr(), v_new.data_ptr(), kb, kh, kn, vb, vh, vn, T, _ptr(n_new), _ptr(w_new))
+    return _pack_rows(k_new.data_ptr(), v_new.data_ptr(), kb, kh, kn, vb, vh, vn, T, _ptr(n_new) or 0, _ptr(w_new) or 0)
 
 
 def hill_cache_insert(desc, k_new, v_new, k_cache, v_cache, seen, pos, accum, sinks, recent, slots, n_new=None,
                       w_new=None, kvh=False, stream=None) -> None:
     """New tokens [B][Hkv][T][d] into a cache of fixed size, in place; a full one evicts by accumulated weight."""
     rows = _new_rows(desc, k_new, v_new, n_new, w_new)
-    _check(load().hill_cache_insert(ctypes.byref(desc), ctypes.byref(rows), _ptr(k_cache), _ptr(v_cache), _ptr(seen),
+    _check(load().hill_cache_insert(ctypes.byref(desc), rows, _ptr(k_cache), _ptr(v_cache), _ptr(seen),
                                     _ptr(pos), _ptr(accum), int(sinks), int(recent), int(bool(kvh)), _ptr(slots),
                                     _stream(stream)), "hill_cache_insert")
 
@@ -387,7 +389,7 @@ def hill_cache_insert_q4(desc, k_new, v_new, k4, v4, params, seen, pos, accum, s
                          w_new=None, kvh=False, stream=None) -> None:
     """hill_cache_insert into a 4-bit cache."""
     rows = _new_rows(desc, k_new, v_new, n_new, w_new)
-    _check(load().hill_cache_insert_q4(ctypes.byref(desc), ctypes.byref(rows), _ptr(k4), _ptr(v4), _ptr(params),
+    _check(load().hill_cache_insert_q4(ctypes.byref(desc), rows, _ptr(k4), _ptr(v4), _ptr(params),
                                        _ptr(seen), _ptr(pos), _ptr(accum), int(sinks), int(recent), int(bool(kvh)),
                                        _ptr(slots), _stream(stream)), "hill_cache_insert_q4")
 
