@@ -1039,6 +1039,10 @@ cudaError_t launch_attn_cl(const WindowArgs& a, int grid, int cluster, cudaStrea
   static int cache[64] = {0};
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), C::kSmem, cache);
   if (e != cudaSuccess) return e;
+  if (count && cluster > 8) {   // the larger clusters have to be asked for, once
+    e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+  }
   if (!count) return launch_pdl(kern, dim3(grid), dim3(C::kNW * 32), C::kSmem, st, CL ? cluster : 0, a);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cluster);
@@ -1053,7 +1057,7 @@ cudaError_t launch_attn_cl(const WindowArgs& a, int grid, int cluster, cudaStrea
   return cudaOccupancyMaxActiveClusters(count, kern, &cfg);
 }
 
-constexpr int kSizes = 4;   // clusters of 1, 2, 4, 8 CTAs
+constexpr int kSizes = 5;   // clusters of 1, 2, 4, 8, 16 CTAs
 
 // One (row, KV head, pass) to a cluster, all of them at once, or the list over
 // all SMs with a second kernel that merges?  The list costs 2.5 us (and 2 us of the
@@ -1065,7 +1069,11 @@ constexpr int kSizes = 4;   // clusters of 1, 2, 4, 8 CTAs
 // In 16 bits 64 CTAs already draw all of HBM's rate, and what counts is that: 8 KV
 // heads 32768 tokens 25.7 / 23.9 (16 - 6.7), 4 KV heads 14.7 / 23.8 (16 - 3.4, 32
 // CTAs); longer rows keep the list, which evens out rows of different lengths.
-constexpr double kIdleRounds = 1.45;
+// With few units the merge has hundreds of partials to an output, and more idle rounds pay: 4 KV
+// heads 32768 tokens in 4 bits 17.1 / 15.3 (3 - 1.1), 4 sequences of one KV head 8192
+// tokens 13.8 / 13.0 (4 - 1.7).  Clusters of 16 over 8: 4 KV heads 8192 tokens 10.2 -> 7.9.
+constexpr double kIdleRounds = 1.45, kIdleRoundsFew = 2.4;
+constexpr int kFewUnits = 8;
 constexpr int kStreamCtas = 64, kStreamRounds = 16;
 
 // *whole: the outputs are complete, there is nothing to merge.
@@ -1095,7 +1103,7 @@ cudaError_t launch_attn_t(const WindowArgs& a, int sms, cudaStream_t st, bool* w
     if (size > 0) {
       const int64_t per = (int64_t)size * C::kNW, rounds = (tiles + per - 1) / per;
       const double share = (double)tiles * units / ((double)sms * C::kNW);
-      *whole = rounds - share <= kIdleRounds ||
+      *whole = rounds - share <= (units <= kFewUnits ? kIdleRoundsFew : kIdleRounds) ||
                (!Q4 && HC < 16 && units * size >= kStreamCtas && rounds <= kStreamRounds);
       if (*whole) return launch_attn_cl<DT, Q4, HC, true>(a, (int)units * size, size, st);
     }
