@@ -965,7 +965,6 @@ namespace {
 
 struct WindowLayout {
   size_t part_o, part_ml, table, stats, logits, total;
-  int passes, heads;   // of query heads per KV head; at most so many in one
 };
 
 int cdiv(int a, int b) { return (a + b - 1) / b; }
@@ -975,10 +974,11 @@ WindowLayout window_layout(const hill_desc* d, bool with_accum, int sms) {
   WindowLayout L{};
   const size_t B = d->batch, H = d->num_q_heads;
   const int G = d->num_q_heads / d->num_kv_heads;
-  L.heads = window_heads_per_pass(G);
-  L.passes = cdiv(G, L.heads);
-  // the same for both formats: the larger number of warps
-  const size_t parts = (size_t)sms * std::max(window_warps(true, L.heads), window_warps(false, L.heads)) * 2 * L.heads;
+  // the most that a call of either format and any window needs: every form of the kernel that may take it
+  size_t per_sm = 0;
+  for (const int heads : {window_heads_per_pass(G, 0), window_heads_per_pass(G, INT64_MAX)})
+    per_sm = std::max(per_sm, (size_t)std::max(window_warps(true, heads), window_warps(false, heads)) * 2 * heads);
+  const size_t parts = (size_t)sms * per_sm;
   size_t off = 0;
   L.part_o = off;
   off += align_up(parts * kHeadDim * sizeof(float));
@@ -1006,7 +1006,7 @@ hill_status window_attn(const hill_desc* desc, const void* q, const void* k, con
   if (kvh && (int64_t)desc->batch * desc->num_kv_heads > window_max_rows()) return HILL_ERR_UNSUPPORTED;
   // the list of tiles is numbered in 32 bits
   const int G = desc->num_q_heads / desc->num_kv_heads;
-  if ((int64_t)desc->batch * desc->num_kv_heads * cdiv(G, window_heads_per_pass(G)) * cdiv(desc->capacity, 32) >= INT32_MAX)
+  if ((int64_t)desc->batch * desc->num_kv_heads * cdiv(G, window_heads_per_pass(G, 0)) * cdiv(desc->capacity, 32) >= INT32_MAX)
     return HILL_ERR_UNSUPPORTED;
   DeviceInfo di;
   if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
@@ -1015,8 +1015,11 @@ hill_status window_attn(const hill_desc* desc, const void* q, const void* k, con
   if (desc->batch == 0) return HILL_OK;
   unsigned char* base = ws_base(ws);
   WindowArgs a{};
+  const int64_t shown = std::min<int64_t>(desc->capacity, (int64_t)sinks + window);
+  a.heads = window_heads_per_pass(G, shown * desc->batch * desc->num_kv_heads);
+  a.passes = cdiv(G, a.heads);
   if (params) {
-    const int tile = window_q4_tile(L.heads);
+    const int tile = window_q4_tile(a.heads);
     s = make_q4_map(desc, k, tile, &a.kmap);
     if (s == HILL_OK) s = make_q4_map(desc, v, tile, &a.vmap);
   } else {
@@ -1043,7 +1046,6 @@ hill_status window_attn(const hill_desc* desc, const void* q, const void* k, con
   a.kvh = kvh ? 1 : 0;
   a.sinks = sinks;
   a.window = window;
-  a.passes = L.passes;
   a.out = out;
   a.accum = accum;
   a.part_o = reinterpret_cast<float*>(base + L.part_o);

@@ -159,7 +159,7 @@ struct WindowArgs {
   const int32_t* lens;   // [B], kvh: [B][Hkv]
   int B, H, Hkv, G, cap, cap32, kvh;
   int sinks, window;
-  int passes;            // of at most window_heads_per_pass(G) query heads
+  int heads, passes;     // query heads of a KV head are taken in passes of at most `heads`: 4, 8 or 16
   float* out;            // [B][H][d]
   float* accum;          // [B][cap], kvh: [B][Hkv][cap], or NULL
   float* logits;         // [B][H][lstride] base-2 logits, or NULL (no accum)
@@ -307,7 +307,7 @@ cudaError_t launch_sparse_attn(const AttnArgs& a, int dtype, int G, int grid, bo
 
 
 // window.cu
-int window_heads_per_pass(int G);
+int window_heads_per_pass(int G, int64_t rows);   // rows: visible tokens x KV heads, at most
 int window_warps(bool q4, int heads_per_pass);   // per CTA, one CTA per SM
 int window_q4_tile(int heads_per_pass);           // tokens
 int window_max_rows();
