@@ -160,7 +160,9 @@ __device__ __forceinline__ void codes_to_half(uint32_t w, __half2 z1024, uint32_
 // would be right, this one leaves the smallest rest): 1024 + it, as a float that fp16 holds, and
 // the rest min + scale * zero point.
 __device__ __forceinline__ float zero_point(float2 p, float& rest) {
-  const float t = fminf(fmaxf(__fdividef(-p.y, p.x) + 1024.f, 1024.f), 1039.f);
+  float inv;   // (of 0: infinity, and the zero point one of the ends or, with a minimum of 0, 0)
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(p.x));
+  const float t = fminf(fmaxf(fmaf(-p.y, inv, 1024.f), 1024.f), 1039.f);
   const float z = __half2float(__float2half_rn(t));   // (fp16 steps by 1 there)
   rest = fmaf(p.x, z - 1024.f, p.y);
   return z;
@@ -241,6 +243,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     prefetch_tmap(&a.kmap);
     prefetch_tmap(&a.vmap);
   }
+  __syncwarp();
   const int rows = a.kvh ? a.B * a.Hkv : a.B;
   const int pairs = (a.kvh ? 1 : a.Hkv) * a.passes;   // (KV head, pass) of a row
 
@@ -270,50 +273,50 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
       set_run(cur, t);
     }
   } else {
-  // the list: every CTA scans the rows' tiles
-  int total = 0;
-  for (int r0 = 0; r0 < rows; r0 += NW * 32) {
-    const int r = r0 + (int)threadIdx.x;
-    const int mine = r < rows ? row_tiles(r).count * pairs : 0;
-    int inc = mine;
+    // the list: every CTA scans the rows' tiles
+    int total = 0;
+    for (int r0 = 0; r0 < rows; r0 += NW * 32) {
+      const int r = r0 + (int)threadIdx.x;
+      const int mine = r < rows ? row_tiles(r).count * pairs : 0;
+      int inc = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += y;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (lane == 31) s_sum[warp] = inc;
+      __syncthreads();
+      int before = total;
+      for (int w = 0; w < NW; ++w) {
+        if (w < warp) before += s_sum[w];
+        total += s_sum[w];
+      }
+      if (r < rows) s_start[r] = before + inc - mine;
+      __syncthreads();
     }
-    if (lane == 31) s_sum[warp] = inc;
+    if (threadIdx.x == 0) s_start[rows] = total;
     __syncthreads();
-    int before = total;
-    for (int w = 0; w < NW; ++w) {
-      if (w < warp) before += s_sum[w];
-      total += s_sum[w];
+    if (blockIdx.x == 0)
+      for (int r = threadIdx.x; r <= rows; r += NW * 32) a.table[r] = s_start[r];
+    // parts are numbered across the CTAs first, so that few tiles spread over all SMs
+    const int nw = min((int)gridDim.x * NW, total);
+    w = warp * gridDim.x + blockIdx.x;
+    if (w >= nw) return;
+    const Parts parts(total, nw);
+    i0 = parts.begin(w);
+    i1 = parts.begin(w + 1);
+    int lo = 0, hi = rows - 1;   // the last row that starts at or before i0
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (s_start[mid] <= i0) lo = mid;
+      else hi = mid - 1;
     }
-    if (r < rows) s_start[r] = before + inc - mine;
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) s_start[rows] = total;
-  __syncthreads();
-  if (blockIdx.x == 0)
-    for (int r = threadIdx.x; r <= rows; r += NW * 32) a.table[r] = s_start[r];
-  // parts are numbered across the CTAs first, so that few tiles spread over all SMs
-  const int nw = min((int)gridDim.x * NW, total);
-  w = warp * gridDim.x + blockIdx.x;
-  if (w >= nw) return;
-  const Parts parts(total, nw);
-  i0 = parts.begin(w);
-  i1 = parts.begin(w + 1);
-  int lo = 0, hi = rows - 1;   // the last row that starts at or before i0
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (s_start[mid] <= i0) lo = mid;
-    else hi = mid - 1;
-  }
-  const Tl t = row_tiles(lo);
-  const int x = i0 - s_start[lo];
-  cur.row = lo;
-  cur.pair = x / t.count;
-  cur.tile = x - cur.pair * t.count;
-  set_run(cur, t);
+    const Tl t = row_tiles(lo);
+    const int x = i0 - s_start[lo];
+    cur.row = lo;
+    cur.pair = x / t.count;
+    cur.tile = x - cur.pair * t.count;
+    set_run(cur, t);
   }
 
   auto next_run = [&](Walk& c) {   // c.tile has passed the run; only while an item follows
@@ -485,7 +488,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     const uint32_t base = ring + slot * C::kSlot;
     float smax = 0.f;            // 4 bits: the largest of this lane's V scales
     float vs[MT][2], vr[MT][2];  // V scale, rest of tokens 16 mt + grp (+ 8)
-    uint32_t vz[MT][2];          // 1024 + V zero points of tokens 16 mt (+ 8) + 2 tig, 2 tig + 1
+    [[maybe_unused]] uint32_t vz[MT][2];   // 1024 + V zero points of tokens 16 mt (+ 8) + 2 tig, 2 tig + 1
     if constexpr (Q4) {
       // each lane prepares the parameters of a few tokens and leaves notes of
       // them for the warp: zero point and scale of K (16 bits each), rest, the same of V
