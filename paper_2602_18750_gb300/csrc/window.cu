@@ -893,10 +893,15 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
 
 // ---------------------------------------------------------------- merge
 // One CTA per (sequence, query head): its warps take the partials in turn, a lane
-// four channels.
-__global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps_in_all) {
-  __shared__ float s_o[32][kHeadDim];
-  __shared__ float2 s_ml[32];
+// four channels, twelve partials under way.  Bound by latency, so all CTAs
+// are to be on the SMs at once (merge_warps).
+constexpr int kMergeWarps = 16;   // at most
+constexpr int kMergeWarpsPerSm = 20;   // of 96 registers a thread
+
+__global__ void __launch_bounds__(kMergeWarps * 32) hill_window_combine_kernel(const WindowArgs a, int HC,
+                                                                               int warps_in_all) {
+  __shared__ float s_o[kMergeWarps][kHeadDim];
+  __shared__ float2 s_ml[kMergeWarps];
   const int h = blockIdx.x, b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int warps = blockDim.x >> 5;
   const int g = h / a.G, hg = h - g * a.G, pass = hg / HC, col = hg - pass * HC;
@@ -917,7 +922,7 @@ __global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps
   const int w0 = parts.of(x0), w1 = parts.of(x0 + count - 1);
   if (w0 == w1) return;   // written by its warp
   Merged s;
-  constexpr int kU = 4;
+  constexpr int kU = 12;
   for (int w = w0 + warp; w <= w1; w += warps * kU) {
     float2 ml[kU];
     float4 v[kU];
@@ -939,7 +944,9 @@ __global__ void hill_window_combine_kernel(const WindowArgs a, int HC, int warps
   __syncthreads();
   if (threadIdx.x >= kHeadDim) return;
   float M = kNegHuge, L = 0.f, O = 0.f;
+#pragma unroll 4
   for (int i = 0; i < warps; ++i) M = fmaxf(M, s_ml[i].x);
+#pragma unroll 4
   for (int i = 0; i < warps; ++i) {
     const float s = ex2(s_ml[i].x - M);
     L = fmaf(s_ml[i].y, s, L);
@@ -1066,16 +1073,18 @@ constexpr int kSizes = 5;   // clusters of 1, 2, 4, 8, 16 CTAs
 // all SMs with a second kernel that merges?  The list costs 2.5 us (and 2 us of the
 // host's time) for the merge; the clusters leave SMs idle: the rounds of tiles
 // that a warp makes, less those that it would make if all SMs had an equal share.
-// Measured (us, list / clusters; rounds - share): 4 bits 32 heads 8192 tokens
-// 16.0 / 13.6 (3 - 2.25), 8 KV heads 8192 tokens 11.0 / 10.3 (2 - 0.56), 4 KV heads
-// 8192 tokens 10.2 / 11.0 (2 - 0.28), 32 heads 32768 tokens 34.6 / 37.0 (11 - 9.0).
+// Measured (us, list / clusters; rounds - share): 4 bits 2 x 5000 tokens of 32 heads
+// 17.9 / 16.6 (4 - 2.8), 13000 tokens of 4 KV heads 11.7 / 13.0 (2 - 0.45), 24000 of 8 16.1 / 17.3
+// (4 - 1.6), 2 x 13000 of 32 30.8 / 32.0 (9 - 7.2).  Clusters of 16 over 8: 8192 of 4 KV heads 10.2 -> 7.9.
 // In 16 bits 64 CTAs already draw all of HBM's rate, and what counts is that: 8 KV
 // heads 32768 tokens 25.7 / 23.9 (16 - 6.7), 4 KV heads 14.7 / 23.8 (16 - 3.4, 32
-// CTAs); longer rows keep the list, which evens out rows of different lengths.
-// With few units the merge has hundreds of partials to an output, and more idle rounds pay: 4 KV
-// heads 32768 tokens in 4 bits 17.1 / 15.3 (3 - 1.1), 4 sequences of one KV head 8192
-// tokens 13.8 / 13.0 (4 - 1.7).  Clusters of 16 over 8: 4 KV heads 8192 tokens 10.2 -> 7.9.
-constexpr double kIdleRounds = 1.45, kIdleRoundsFew = 2.4;
+// CTAs); longer rows keep the list, which evens out rows of different lengths.  With few units the
+// merge has hundreds of partials to an output: 1 KV head 13000 tokens 10.5 / 9.5 (4 - 0.3), 2 x 24000
+// 14.2 / 12.0 (6 - 1.2); in 4 bits, once every warp has one, 4 KV heads 32768 tokens 16.7 / 15.3 (3 - 1.1).
+// Passes of 16 heads have four times the partials of ones of 4: in 4 bits 5 x 5000 tokens of 32 heads
+// and one KV head 16.2 / 12.1 (3 - 1.3), 6 x 8192 of 48 and 4 20.6 / 21.2 (8 - 5.0); in 16 bits 15.7 / 11.2
+// there, 4 x 12000 of one KV head 14.7 / 16.5 (6 - 2.5).
+constexpr double kIdleRounds = 1.45, kIdleRounds16 = 2.4, kIdleRoundsFew = 5.5, kIdleRoundsFewQ4 = 2.0;
 constexpr int kFewUnits = 8;
 constexpr int kStreamCtas = 64, kStreamRounds = 16;
 
@@ -1106,7 +1115,11 @@ cudaError_t launch_attn_t(const WindowArgs& a, int sms, cudaStream_t st, bool* w
     if (size > 0) {
       const int64_t per = (int64_t)size * C::kNW, rounds = (tiles + per - 1) / per;
       const double share = (double)tiles * units / ((double)sms * C::kNW);
-      *whole = rounds - share <= (units <= kFewUnits ? kIdleRoundsFew : kIdleRounds) ||
+      double idle = kIdleRounds;
+      if (HC == 16) idle = kIdleRounds16;
+      else if (units <= kFewUnits && !Q4) idle = kIdleRoundsFew;
+      else if (units <= kFewUnits && share >= 1) idle = kIdleRoundsFewQ4;
+      *whole = rounds - share <= idle ||
                (!Q4 && HC < 16 && units * size >= kStreamCtas && rounds <= kStreamRounds);
       if (*whole) return launch_attn_cl<DT, Q4, HC, true>(a, (int)units * size, size, st);
     }
@@ -1130,6 +1143,20 @@ int window_heads_per_pass(int G, int64_t rows) {
   if (G <= 8) return G <= 4 ? 4 : 8;
   return rows <= (G <= 16 ? 32768 : 16384) ? 8 : 16;
 }
+// Warps of a merging CTA: about twelve partials each, but no more than let all CTAs
+// run at once.  (32 warps with four partials each took a second wave where there were more
+// outputs than SMs; before / now, us: 32 heads of one KV head 6 x 10000 tokens 22.9 / 19.5,
+// 9 x 40000 in 4 bits 49.7 / 45.8; 32 heads of four, 6 x 40000 in 4 bits 42.8 / 38.9, 1 x
+// 40000 17.9 / 17.3; 16 heads of one, 1 x 40000 20.0 / 20.2.)
+static int merge_warps(const WindowArgs& a, int nw, int sms) {
+  const int64_t per = nw / std::max<int64_t>(1, (int64_t)a.B * a.Hkv * a.passes) + 1;
+  int warps = 4;
+  while (warps < kMergeWarps && warps * 12 < per &&
+         (int64_t)a.B * a.H <= (int64_t)sms * (kMergeWarpsPerSm / (2 * warps)))
+    warps <<= 1;
+  return warps;
+}
+
 int window_warps(bool q4, int HC) { return q4 ? warps_for<true>(HC) : warps_for<false>(HC); }
 int window_q4_tile(int HC) { return HC == 16 ? Cfg<true, 16>::kT : Cfg<true, 4>::kT; }
 int window_max_rows() { return kMaxRows; }
@@ -1151,10 +1178,7 @@ cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms,
   *kernels = 1;
   if (!whole) {
     const int nw = sms * window_warps(q4, HC);
-    // about four partials to a warp
-    const int64_t per = nw / std::max<int64_t>(1, (int64_t)a.B * a.Hkv * a.passes) + 1;
-    int warps = 4;
-    while (warps < 32 && warps * 4 < per) warps <<= 1;
+    const int warps = merge_warps(a, nw, sms);
     e = launch_pdl(hill_window_combine_kernel, dim3(a.H, a.B), dim3(warps * 32), 0, st, 0, a, HC, nw);
     ++*kernels;
   }
