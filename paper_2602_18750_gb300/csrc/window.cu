@@ -41,7 +41,7 @@
 //
 // In 16 bits bound by HBM, 512 bytes per token and KV head: 4 x 16-32K tokens of 32
 // heads with their weights 250-260 us, 6.6 TB/s; 1 x 128K of 8 KV heads and 64 query
-// heads 84 us, 6.4 TB/s.  In 4 bits, 136 bytes, the instructions that make fp16
+// heads 83 us, 6.5 TB/s.  In 4 bits, 136 bytes, the instructions that make fp16
 // of the codes keep it from there: a tile of 32 tokens takes 600, 290 of them for the
 // codes, of the 700 that fit its share of HBM's time: 8 x 64K tokens of 32 heads
 // 388 us, 5.9 TB/s (346 us with the codes passed on unconverted).  Tiles of 64
