@@ -166,6 +166,19 @@ def test_both_forms(H, heads, dtype, q4):
     run(c, np.random.RandomState(5).randint(0, 151, 160), 3, 130, (2,))
 
 
+@pytest.mark.parametrize("q4", [False, True], ids=["16bit", "q4"])
+@pytest.mark.parametrize("shape", [(12, 32, 1, 9000), (6, 32, 1, 20000), (1, 20, 1, 40000), (5, 64, 2, 5000)])
+def test_merges_of_many_partials(H, shape, q4):
+    """Long rows of large groups: merging CTAs of every size, more outputs than SMs, rows without a partial among them."""
+    B, heads, Hkv, n = shape
+    c = Case(H, B, heads, Hkv, n, "bf16", q4, seed=59)
+    for lens in ([n] * B, [n if b % 3 == 0 else (n // 7 if b % 3 == 1 else 0) for b in range(B)]):
+        ref, w, bound, wb = c.reference(lens, 0, ALL)
+        accum = torch.zeros(w.shape, device="cuda")
+        check(c.attend(lens, 0, ALL, accum), ref, bound)
+        check(accum.cpu().numpy().astype(np.float64), w, wb + 2.0 ** -23 * w)
+
+
 def test_values_far_from_one(H):
     """4-bit rows of 2^100 under queries of 2^-100, and the reverse: the logits are ordinary, their factors are not."""
     for scale in (2.0 ** 100, 2.0 ** -100):
