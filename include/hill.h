@@ -357,7 +357,9 @@ size_t hill_window_workspace_bytes(const hill_desc* desc, int32_t with_accum);
  * sum of p_j over the row's query heads, for visible j only.
  * lens and accum: [B] and [B][cap], kvh != 0: [B][Hkv] and [B][Hkv][cap] (B * Hkv
  * <= 2048).  What lies in slots that are not visible does not matter, NaN
- * included.  q, K, V as in the calls above; out 16-byte aligned. */
+ * included; a query, key or value that is seen and not finite leaves the
+ * outputs (and weights) that it enters not finite, as the formula has it.
+ * q, K, V as in the calls above; out 16-byte aligned. */
 hill_status hill_window_attn(const hill_desc* desc, const void* q, const void* k_cache, const void* v_cache,
                              const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh, float* accum,
                              float* out, void* ws, size_t ws_bytes, void* stream);

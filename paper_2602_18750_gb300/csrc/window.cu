@@ -839,7 +839,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
     // place, and these by the cluster, its CTAs taking the heads in turn
     cg::cluster_group cluster = cg::this_cluster();
     const int size = cluster.num_blocks(), rank = cluster.block_rank();
-    if (i0 >= i1 && lane < HC) ring_ml[lane] = float2{kNegHuge, 0.f};   // nothing of this warp
+    if (i0 >= i1 && lane < HC) ring_ml[lane] = float2{kNegHuge, -1.f};   // nothing of this warp
     pdl_launch_dependents();
     __syncthreads();
     const int b = seq_of(cur), pass = cur.pair % a.passes, h0 = head_of(cur) * a.G + pass * HC;
@@ -857,7 +857,12 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         for (int u = 0; u < kU; ++u) {
           const float* from = first + (u0 + u) * kStride;
           ml[u] = reinterpret_cast<const float2*>(from + HC * kHeadDim)[col];
-          v[u] = ml[u].y > 0.f ? *reinterpret_cast<const float4*>(from + col * kHeadDim + 4 * lane) : float4{0.f, 0.f, 0.f, 0.f};
+          if (ml[u].y < 0.f) {   // (a sum that is not a number counts)
+            ml[u].y = 0.f;
+            v[u] = float4{0.f, 0.f, 0.f, 0.f};
+          } else {
+            v[u] = *reinterpret_cast<const float4*>(from + col * kHeadDim + 4 * lane);
+          }
         }
         s.add(ml, v);
       }
@@ -880,11 +885,11 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         }
         s.add(ml, v);
       }
-      // (nothing visible: no sum, zeros)
-      const float inv = s.l > 0.f ? 1.f / s.l : 0.f;
+      // zeros where nothing is visible; a sum that is not a number shows in the output
+      const float inv = s.l == 0.f && row_tiles(cur.row).count == 0 ? 0.f : 1.f / s.l;
       const int64_t at = (int64_t)b * a.H + h0 + col;
-      const float4 out{s.o.x * inv, s.o.y * inv, s.o.z * inv, s.o.w * inv};
-      *reinterpret_cast<float4*>(a.out + at * kHeadDim + 4 * lane) = s.l > 0.f ? out : float4{0.f, 0.f, 0.f, 0.f};
+      *reinterpret_cast<float4*>(a.out + at * kHeadDim + 4 * lane) =
+          float4{s.o.x * inv, s.o.y * inv, s.o.z * inv, s.o.w * inv};
       if (a.stats && lane == 0) a.stats[at] = float2{s.m, inv};
     }
     cluster.sync();   // no CTA leaves while another reads its sums
