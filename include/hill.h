@@ -365,7 +365,9 @@ hill_status hill_window_attn(const hill_desc* desc, const void* q, const void* k
                              float* out, void* ws, size_t ws_bytes, void* stream);
 
 /* hill_window_attn over a 4-bit cache: K and V are the values that the rows
- * stand for (not rounded to 16 bits). */
+ * stand for (not rounded to 16 bits).  A token's weight times its V scale
+ * enters with a relative error of 2^-22 and one of 2^-32 of a head's largest
+ * such product; scales and minima of up to 2^100 are summed without overflow. */
 hill_status hill_window_attn_q4(const hill_desc* desc, const void* q, const uint8_t* k4, const uint8_t* v4,
                                 const void* params, const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh,
                                 float* accum, float* out, void* ws, size_t ws_bytes, void* stream);

@@ -32,8 +32,13 @@
 // near -min / scale this is scale * (code - z0) + rest, the rest below half a
 // scale where the row has both signs: nothing large cancels.  code - z0 enters
 // mma as fp16 integers, the scale and rest in float32: z = scale (q . (code -
-// z0)) + rest sum(q), and o = sum p scale (code - z0) + sum p rest, where p scale / R
-// is the 16-bit operand and R a power of two at or above every scale so far.
+// z0)) + rest sum(q), and o = sum p scale (code - z0) + sum p rest.  The 16-bit
+// operand of the former is F p scale, again a high part and a residual, F a power of two
+// of each head that put its largest product p scale at 2^7 when it was set, and is set
+// again when one passes 2^15: a product is off by at most 2^-22 of itself plus 2^-32 of
+// the largest.  (With F from the largest scale alone a row of large values and no weight,
+// or one of all the weight and no value, left the others' products as fp16 subnormals: the output off
+// by 2 % at 2^20 times the other scales, by 4 % beside a token of 2^20 times their weight.)
 // The query is multiplied by a power of two that puts its largest element at 2^14
 // (bf16 queries fit fp16 that way).  (Codes left as fp16 subnormals, which
 // takes masks alone, lost 10 bits: mma aligns a subnormal's products by the
@@ -183,11 +188,19 @@ __device__ __forceinline__ uint2 lds64(uint32_t addr) {
   return v;
 }
 
-// A power of two at or above s >= 0 (at least 2^-125, at most 2^127).
-__device__ __forceinline__ float pow2_above(float s) {
-  const uint32_t e = __float_as_uint(s) >> 23;
-  return __uint_as_float(min(max(e + 1, 2u), 254u) << 23);
+// Powers of two as floats, from 2^-121 to kMaxFactor = 2^126.  fit_below: the factor that puts
+// the largest of some products, t, at 2^7 if f takes it past 2^12, else f.
+constexpr float kMaxFactor = 8.507059173e37f;
+__device__ __forceinline__ float fit_below(float f, float t) {
+  return t * f > 4096.f ? __uint_as_float((261u - (__float_as_uint(t) >> 23)) << 23) : f;
 }
+// f times 2^k, k >= 0, or as much of it as there is room for: `taken`.
+__device__ __forceinline__ float times_pow2(float f, int k, int& taken) {
+  const uint32_t e = __float_as_uint(f) >> 23;
+  taken = min(k, 253 - (int)e);
+  return __uint_as_float((e + taken) << 23);
+}
+__device__ __forceinline__ float inverse_pow2(float f) { return __uint_as_float((254u << 23) - __float_as_uint(f)); }
 
 template <int I> using Int = std::integral_constant<int, I>;
 template <bool I> using Bool = std::integral_constant<bool, I>;
@@ -399,7 +412,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
   float o[8][kN][4];                     // O^T: channels x heads
   float2 m[kN], l[kN];                   // columns 2 tig, 2 tig + 1; l of this lane's tokens only
   float2 cz[kN], cq[kN], mp[kN];         // 4 bits: factor of q . (code - z0); of the K rest; sum p V rest
-  float R = 0.f, Rinv = 0.f;             // 4 bits: the power of two above the V scales
+  float2 vf[kN];                         // 4 bits: the power of two that p V scale is multiplied by in o
   int head0 = 0, Gn = 0;                 // the pair's first query head (of all sequences') and heads
 
   auto begin_pair = [&] {
@@ -458,12 +471,12 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
       }
       m[nt] = both(kNegHuge);
       l[nt] = mp[nt] = both(0.f);
+      vf[nt] = both(kMaxFactor);
 #pragma unroll
       for (int ct = 0; ct < 8; ++ct)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[ct][nt][e] = 0.f;
     }
-    R = Rinv = 0.f;
   };
 
   // ------------------------------------------------------------ one tile
@@ -486,15 +499,14 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
 
     arrive();
     const uint32_t base = ring + slot * C::kSlot;
-    float smax = 0.f;            // 4 bits: the largest of this lane's V scales
-    float vs[MT][2], vr[MT][2];  // V scale, rest of tokens 16 mt + grp (+ 8)
+    [[maybe_unused]] float vs[MT][2], vr[MT][2];  // V scale, rest of tokens 16 mt + grp (+ 8)
     [[maybe_unused]] uint32_t vz[MT][2];   // 1024 + V zero points of tokens 16 mt (+ 8) + 2 tig, 2 tig + 1
+    constexpr int kPer = C::kT / 2;   // notes per slot
+    static_assert(!Q4 || C::kSlots * kPer >= C::kT, "room for the notes");
+    [[maybe_unused]] auto note = [&](int r) { return ring + (r / kPer) * C::kSlot + C::kNotes + (r % kPer) * 16; };
     if constexpr (Q4) {
       // each lane prepares the parameters of a few tokens and leaves notes of
       // them for the warp: zero point and scale of K (16 bits each), rest, the same of V
-      constexpr int kPer = C::kT / 2;   // notes per slot
-      static_assert(C::kSlots * kPer >= C::kT, "room for the notes");
-      auto note = [&](int r) { return ring + (r / kPer) * C::kSlot + C::kNotes + (r % kPer) * 16; };
 #pragma unroll
       for (int i = 0; i < C::kT / 32; ++i) {
         const int r = i * 32 + lane;
@@ -505,7 +517,6 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         const uint32_t zz = pack2<0>(zero_point(unpack2<DT>(pr.x), kr), zero_point(vp, vrest));
         sts128(note(r), uint4{__byte_perm(pr.x, zz, 0x5410), __float_as_uint(kr), __byte_perm(pr.y, zz, 0x7610),
                               __float_as_uint(vrest)});
-        smax = fmaxf(smax, vp.x);
       }
       __syncwarp();
 #pragma unroll
@@ -593,77 +604,142 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         }
     }
 
-    // the running maximum (and R) where a logit (a scale) has passed it
-    auto top = [&](int nt, int e) {
-      float t = fmaxf(z[0][nt][e], z[0][nt][2 + e]);
+    // the largest of each column's values in this lane's rows, or in all of the tile's
+    auto top = [](const float (&x)[MT][kN][4], int nt, int e) {
+      float t = fmaxf(x[0][nt][e], x[0][nt][2 + e]);
 #pragma unroll
-      for (int mt = 1; mt < MT; ++mt) t = fmaxf(t, fmaxf(z[mt][nt][e], z[mt][nt][2 + e]));
+      for (int mt = 1; mt < MT; ++mt) t = fmaxf(t, fmaxf(x[mt][nt][e], x[mt][nt][2 + e]));
       return t;
     };
-    bool over = Q4 && smax > R;
+    auto tile_top = [&](const float (&x)[MT][kN][4], int nt) {
+      float2 t{top(x, nt, 0), top(x, nt, 1)};
 #pragma unroll
-    for (int nt = 0; nt < kN; ++nt)
-      over = over || top(nt, 0) > m[nt].x + 15.f || top(nt, 1) > m[nt].y + 15.f;
-    if (__any_sync(0xffffffffu, over)) {
-      float shrink = 1.f;
-      if (Q4) {
-        smax = warp_max(smax);
-        if (smax > R || R == 0.f) {
-          const float Rn = pow2_above(smax);
-          shrink = R * (1.f / Rn);
-          R = Rn;
-          Rinv = 1.f / Rn;
-        }
+      for (int s = 4; s < 32; s <<= 1) {
+        t.x = fmaxf(t.x, __shfl_xor_sync(0xffffffffu, t.x, s));
+        t.y = fmaxf(t.y, __shfl_xor_sync(0xffffffffu, t.y, s));
       }
+      return t;
+    };
+    auto scale_o = [&](int nt, float2 f) {
+#pragma unroll
+      for (int ct = 0; ct < 8; ++ct)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[ct][nt][e] *= e & 1 ? f.y : f.x;
+    };
+    // the running maximum, where a logit has passed it
+    auto raise = [&] {
 #pragma unroll
       for (int nt = 0; nt < kN; ++nt) {
-        float2 t{top(nt, 0), top(nt, 1)};
-#pragma unroll
-        for (int s = 4; s < 32; s <<= 1) {
-          t.x = fmaxf(t.x, __shfl_xor_sync(0xffffffffu, t.x, s));
-          t.y = fmaxf(t.y, __shfl_xor_sync(0xffffffffu, t.y, s));
-        }
+        const float2 t = tile_top(z, nt);
         const float2 mn{fmaxf(m[nt].x, t.x - 7.f), fmaxf(m[nt].y, t.y - 7.f)};
-        float2 f{ex2(m[nt].x - mn.x), ex2(m[nt].y - mn.y)};
+        const float2 up{mn.x - m[nt].x, mn.y - m[nt].y};
+        float2 f{ex2(-up.x), ex2(-up.y)};
         m[nt] = mn;
         l[nt] = mul2(l[nt], f);
-        if (Q4) mp[nt] = mul2(mp[nt], f);
-        f = mul2(f, both(shrink));
-#pragma unroll
-        for (int ct = 0; ct < 8; ++ct)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[ct][nt][e] *= e & 1 ? f.y : f.x;
+        if (Q4) {   // o keeps its size where vf can make up for it
+          mp[nt] = mul2(mp[nt], f);
+          int kx, ky;
+          vf[nt].x = times_pow2(vf[nt].x, (int)fminf(up.x, 252.f), kx);
+          vf[nt].y = times_pow2(vf[nt].y, (int)fminf(up.y, 252.f), ky);
+          f = float2{ex2((float)kx - up.x), ex2((float)ky - up.y)};
+        }
+        scale_o(nt, f);
       }
-    }
+    };
+    auto weight = [&](int mt, int t8, int nt) {
+      const float2 d = add2(float2{z[mt][nt][2 * t8], z[mt][nt][2 * t8 + 1]}, float2{-m[nt].x, -m[nt].y});
+      return float2{ex2(d.x), ex2(d.y)};
+    };
 
     // weights, and the column operand: high parts and residuals
     constexpr int PT = Q4 ? 0 : DT;
     uint32_t ph[MT][kN][2], pl[MT][kN][2];
+    auto operand = [&](float2 p, int mt, int t8, int nt) {
+      const uint32_t hi = pack2<PT>(p.x, p.y);
+      const float2 hf = unpack2<PT>(hi), rest = add2(p, float2{-hf.x, -hf.y});
+      const uint32_t lo = pack2<PT>(rest.x, rest.y);
+      if (kFold) {
+        ph[mt][nt][t8] = transpose8(tig < 2 ? hi : lo);
+      } else {
+        ph[mt][nt][t8] = transpose8(hi);
+        pl[mt][nt][t8] = transpose8(lo);
+      }
+    };
+    if constexpr (Q4) {
+      float pv[MT][kN][4];                // p V scale
+      float2 ls[kN], ms[kN], ts[kN];      // sums of p, of p V rest and of pv
+      auto clear = [&] {
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int t8 = 0; t8 < 2; ++t8) {
-        const float f = Q4 ? vs[mt][t8] * Rinv : 1.f;
+        for (int nt = 0; nt < kN; ++nt) ls[nt] = ms[nt] = ts[nt] = both(0.f);
+      };
+      auto weigh = [&](int mt, int t8, float scale, float rest) {
 #pragma unroll
         for (int nt = 0; nt < kN; ++nt) {
-          const float2 d = add2(float2{z[mt][nt][2 * t8], z[mt][nt][2 * t8 + 1]}, float2{-m[nt].x, -m[nt].y});
-          float2 p{ex2(d.x), ex2(d.y)};
-          l[nt] = add2(l[nt], p);
-          if (Q4) {
-            mp[nt] = fma2(p, both(vr[mt][t8]), mp[nt]);
-            p = mul2(p, both(f));
+          const float2 p = weight(mt, t8, nt), v = mul2(p, both(scale));
+          ls[nt] = add2(ls[nt], p);
+          ms[nt] = fma2(p, both(rest), ms[nt]);
+          ts[nt] = add2(ts[nt], v);
+          pv[mt][nt][2 * t8] = v.x;
+          pv[mt][nt][2 * t8 + 1] = v.y;
+        }
+      };
+      clear();
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int t8 = 0; t8 < 2; ++t8) weigh(mt, t8, vs[mt][t8], vr[mt][t8]);
+      // A weight past 2^15, or a product past what vf allows for?  (The sums of the lane's tokens, at most
+      // eight, are looked at: where they are within, none is past.)
+      bool over = false;
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt) {
+        const float2 t = mul2(ts[nt], vf[nt]);
+        over = over || ls[nt].x > 32768.f || ls[nt].y > 32768.f || t.x > 32768.f || t.y > 32768.f;
+      }
+      if (__any_sync(0xffffffffu, over)) {   // once more, with the scales from the notes
+        raise();
+        clear();
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int t8 = 0; t8 < 2; ++t8) {
+            const uint4 n4 = lds128(note(mt * 16 + t8 * 8 + grp));
+            weigh(mt, t8, unpack2<DT>(n4.z).x, __uint_as_float(n4.w));
           }
-          const uint32_t hi = pack2<PT>(p.x, p.y);
-          const float2 hf = unpack2<PT>(hi), rest = add2(p, float2{-hf.x, -hf.y});
-          const uint32_t lo = pack2<PT>(rest.x, rest.y);
-          if (kFold) {
-            ph[mt][nt][t8] = transpose8(tig < 2 ? hi : lo);
-          } else {
-            ph[mt][nt][t8] = transpose8(hi);
-            pl[mt][nt][t8] = transpose8(lo);
-          }
+#pragma unroll
+        for (int nt = 0; nt < kN; ++nt) {
+          const float2 t = tile_top(pv, nt);
+          const float2 to{fit_below(vf[nt].x, t.x), fit_below(vf[nt].y, t.y)};
+          scale_o(nt, float2{to.x * inverse_pow2(vf[nt].x), to.y * inverse_pow2(vf[nt].y)});
+          vf[nt] = to;
         }
       }
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt) {
+        l[nt] = add2(l[nt], ls[nt]);
+        mp[nt] = add2(mp[nt], ms[nt]);
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+          for (int t8 = 0; t8 < 2; ++t8)
+            operand(mul2(float2{pv[mt][nt][2 * t8], pv[mt][nt][2 * t8 + 1]}, vf[nt]), mt, t8, nt);
+      }
+    } else {
+      bool over = false;
+#pragma unroll
+      for (int nt = 0; nt < kN; ++nt) over = over || top(z, nt, 0) > m[nt].x + 15.f || top(z, nt, 1) > m[nt].y + 15.f;
+      if (__any_sync(0xffffffffu, over)) raise();
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int t8 = 0; t8 < 2; ++t8)
+#pragma unroll
+          for (int nt = 0; nt < kN; ++nt) {
+            const float2 p = weight(mt, t8, nt);
+            l[nt] = add2(l[nt], p);
+            operand(p, mt, t8, nt);
+          }
+    }
 
     // O^T += V^T p.  mma rounds its sums towards zero, which over the thousands
     // of tiles of a long row adds up (to 2e-5 of the output); so a tile is
@@ -782,6 +858,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
         const int col = nt * 8 + 2 * tig + e;
         const bool mine = col < Gn;
         const float inv = whole ? 1.f / ls : 1.f;
+        [[maybe_unused]] const float back = Q4 ? inverse_pow2(e ? vf[nt].y : vf[nt].x) : 1.f;
         float* to = whole ? a.out + (int64_t)(head0 + col) * kHeadDim : part_o + col * kHeadDim;
 #pragma unroll
         for (int ct = 0; ct < 8; ct += 2) {
@@ -793,7 +870,7 @@ __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_ker
           if (!mine) continue;
           if (Q4) {
             *reinterpret_cast<float4*>(to + ct * 16 + 4 * grp) =
-                float4{fmaf(v[0], R, ms) * inv, fmaf(v[1], R, ms) * inv, fmaf(v[2], R, ms) * inv, fmaf(v[3], R, ms) * inv};
+                float4{fmaf(v[0], back, ms) * inv, fmaf(v[1], back, ms) * inv, fmaf(v[2], back, ms) * inv, fmaf(v[3], back, ms) * inv};
           } else {
             to[ct * 16 + grp] = v[0] * inv;
             to[ct * 16 + 8 + grp] = v[1] * inv;
