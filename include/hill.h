@@ -395,8 +395,9 @@ typedef struct {
  * them, stay.  slots [B][max_new] (kvh: [B][Hkv][max_new]) receives every new
  * token's slot, -1 past a sequence's own.
  * sinks + max(recent, max_new) must not exceed cap.  If pos names fewer slots
- * that may go than are needed (positions that no insert made), the remaining
- * tokens are dropped (slot -1) and HILL_ERR_DEVICE is recorded.  -0.0 ranks
+ * that may go than are needed (positions that no insert made), none of them is
+ * given up: the tokens that found no free slot are dropped (slot -1) and
+ * HILL_ERR_DEVICE is recorded.  -0.0 ranks
  * equal to +0.0; weights must be finite. */
 hill_status hill_cache_insert(const hill_desc* desc, const hill_new_rows* rows, void* k_cache, void* v_cache,
                               int32_t* seen, int32_t* pos, float* accum, int32_t sinks, int32_t recent, int32_t kvh,
