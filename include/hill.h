@@ -337,7 +337,8 @@ hill_status hill_score_noalloc(const hill_desc* desc, const void* q, const void*
  *           cap rounded up to 32, dense, 16-byte aligned.
  * Finite rows give scale = (max - min) / 15 rounded to the 16-bit type and
  * code = (x - min) / scale rounded to nearest even, clamped to [0, 15] (0 when
- * the scale rounds to 0).  desc gives the sizes and the type; its K and V
+ * the scale rounds to 0).  A row with a NaN or an infinity, or whose max - min
+ * float32 does not hold, stands for no finite value.  desc gives the sizes and the type; its K and V
  * strides are not used for 4-bit caches.
  *
  * These calls read all their inputs after the dependency wait (see above). */

@@ -55,13 +55,13 @@ __device__ __forceinline__ uint2 encode_row(const uint4 (&raw)[2], uint32_t& par
   uint32_t lo = w[0], hi = w[0];
 #pragma unroll
   for (int i = 1; i < 8; ++i) {
-    lo = un(__hmin2(pr(lo), pr(w[i])));
-    hi = un(__hmax2(pr(hi), pr(w[i])));
+    lo = un(__hmin2_nan(pr(lo), pr(w[i])));   // (a NaN stays one: the row then stands for NaN)
+    hi = un(__hmax2_nan(pr(hi), pr(w[i])));
   }
   // (min, -max) side by side: halves 0 and 1 of each, joined
-  uint32_t v = un(__hmin2(pr(__byte_perm(lo, hi, 0x5410) ^ 0x80000000u), pr(__byte_perm(lo, hi, 0x7632) ^ 0x80000000u)));
+  uint32_t v = un(__hmin2_nan(pr(__byte_perm(lo, hi, 0x5410) ^ 0x80000000u), pr(__byte_perm(lo, hi, 0x7632) ^ 0x80000000u)));
 #pragma unroll
-  for (int s = 1; s < 8; s <<= 1) v = un(__hmin2(pr(v), pr(__shfl_xor_sync(0xffffffffu, v, s))));
+  for (int s = 1; s < 8; s <<= 1) v = un(__hmin2_nan(pr(v), pr(__shfl_xor_sync(0xffffffffu, v, s))));
   const float2 ends = unpack2<DT>(v);
   const float mn = ends.x, mx = -ends.y;
   param = pack2<DT>(__fdiv_rn(mx - mn, 15.f), mn);

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from bounded_util import ALL
-from test_gpu_bounded import H, Case, check  # noqa: F401 (H: the fixture)
+from test_gpu_bounded import H, Case, Store, check, gen  # noqa: F401 (H: the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,33 @@ def test_rows_with_nothing_to_see_stay_zero(H, q4, B):  # noqa: F811
             assert np.isnan(got[1::2, 0]).all() and np.isfinite(got[1::2, 1:]).all() and torch.isnan(accum[1::2]).all()
         else:
             assert (got == 0).all() and torch.all(accum == 0.25)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf"), 3.3e38], ids=["nan", "inf", "-inf", "far"])
+def test_new_rows_that_are_not_finite(H, bad, dtype):  # noqa: F811
+    """In 4 bits such a row stands for no finite value, whichever channel was not; the others are as ever.  So does one
+    whose max - min float32 does not hold."""
+    T = 40
+    for at in (0, 77, 127):
+        s = Store(H, 1, 2, T, q4=True, dtype=dtype, seed=113)
+        k, v = (torch.randn(1, 2, T, 128, device="cuda", generator=gen(114)).to(s.dt) for _ in range(2))
+        s.insert(T, 0, 0, new=(k, v))
+        clean = [x.clone() for x in (s.k4, s.v4, s.params)]
+        k[0, 0, 3, at] = v[0, 1, 8, at] = bad
+        if bad == 3.3e38:
+            k[0, 0, 3, at ^ 1] = v[0, 1, 8, at ^ 1] = -bad
+        s.seen.zero_()
+        slots = torch.zeros(1, T, dtype=torch.int32, device="cuda")
+        H.hill_cache_insert_q4(s.desc, k, v, s.k4, s.v4, s.params, s.seen, s.pos, s.accum, 0, 0, slots)
+        H.hill_sync_status()
+        K, V = torch.zeros_like(k), torch.zeros_like(v)
+        lo, hi = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (0, T))
+        desc = H.make_desc(torch.zeros(1, 2, 128, dtype=s.dt, device="cuda"), K, V)
+        H.hill_cache_read_q4(desc, s.k4, s.v4, s.params, lo, hi, T, K, V)
+        H.hill_sync_status()
+        assert not torch.isfinite(K[0, 0, 3]).any() and not torch.isfinite(V[0, 1, 8]).any()
+        rest = torch.ones(2, T, dtype=torch.bool, device="cuda")
+        rest[0, 3] = rest[1, 8] = False
+        assert all(torch.equal(a[0, :, :T][rest], b[0, :, :T][rest]) for a, b in zip((s.k4, s.v4, s.params), clean))
+        assert torch.isfinite(K[0][rest]).all() and torch.isfinite(V[0][rest]).all()
