@@ -136,6 +136,18 @@ def _ptr(t) -> int | None:
     return t if t is None or isinstance(t, int) else t.data_ptr()
 
 
+_I32, _F32 = torch.int32, torch.float32
+
+
+def _typed(t, dtype, what: str) -> int | None:
+    """The pointer of a tensor that the kernels read or write as dense elements of dtype."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous, of {dtype}; got {t.dtype}, strides {t.stride()}")
+    return t.data_ptr()
+
+
 # the handle of the current stream without a Stream object around it (2.5 us of a call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -314,6 +326,8 @@ def make_desc_q4(q: torch.Tensor, k4: torch.Tensor) -> hill_desc:
     Bk, Hkv, cap, half = k4.shape
     if Bk != B or 2 * half != d:
         raise ValueError(f"shape mismatch q {tuple(q.shape)} vs codes {tuple(k4.shape)}")
+    if k4.element_size() != 1 or not k4.is_contiguous():
+        raise ValueError("codes must be bytes, contiguous")
     if q.stride(-1) != 1:
         raise ValueError("head dimension must be contiguous")
     dt = {torch.float16: HILL_F16, torch.bfloat16: HILL_BF16}.get(q.dtype)
@@ -349,21 +363,23 @@ def hill_window_attn(desc, q, k_cache, v_cache, lens, sinks, window, out, accum=
                      stream=None) -> None:
     """Attention over the first `sinks` and the newest `window` tokens; accum += the weights."""
     wp, wn = _ws(ws)
-    _check(load().hill_window_attn(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(lens), int(sinks),
-                                   int(window), int(bool(kvh)), _ptr(accum), _ptr(out), wp, wn, _stream(stream)),
-           "hill_window_attn")
+    _check(load().hill_window_attn(ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache),
+                                   _typed(lens, _I32, "lens"), int(sinks), int(window), int(bool(kvh)),
+                                   _typed(accum, _F32, "accum"), _typed(out, _F32, "out"), wp, wn,
+                                   _stream(stream)), "hill_window_attn")
 
 
 def hill_window_attn_q4(desc, q, k4, v4, params, lens, sinks, window, out, accum=None, kvh=False, ws=None,
                         stream=None) -> None:
     """hill_window_attn over a cache held in 4 bits."""
     wp, wn = _ws(ws)
-    _check(load().hill_window_attn_q4(ctypes.byref(desc), _ptr(q), _ptr(k4), _ptr(v4), _ptr(params), _ptr(lens),
-                                      int(sinks), int(window), int(bool(kvh)), _ptr(accum), _ptr(out), wp, wn,
+    _check(load().hill_window_attn_q4(ctypes.byref(desc), _ptr(q), _ptr(k4), _ptr(v4), _ptr(params),
+                                      _typed(lens, _I32, "lens"), int(sinks), int(window), int(bool(kvh)),
+                                      _typed(accum, _F32, "accum"), _typed(out, _F32, "out"), wp, wn,
                                       _stream(stream)), "hill_window_attn_q4")
 
 
-def _new_rows(desc, k_new, v_new, n_new, w_new) -> bytes:
+def _new_rows(desc, k_new, v_new, n_new, w_new, kvh) -> bytes:
     """The hill_new_rows of new tokens, packed."""
     shape, dtype = k_new.shape, torch.bfloat16 if desc.dtype else torch.float16
     if len(shape) != 4 or shape != v_new.shape or k_new.dtype != dtype or v_new.dtype != dtype:
@@ -373,32 +389,55 @@ def _new_rows(desc, k_new, v_new, n_new, w_new) -> bytes:
     if B != desc.batch or Hkv != desc.num_kv_heads or d != desc.head_dim or k1 != 1 or v1 != 1:
         raise ValueError(f"new rows must be [{desc.batch}][{desc.num_kv_heads}][T][{desc.head_dim}], the last dimension "
                          f"contiguous; got {tuple(shape)}")
-    return _pack_rows(k_new.data_ptr(), v_new.data_ptr(), kb, kh, kn, vb, vh, vn, T, _ptr(n_new) or 0, _ptr(w_new) or 0)
+    n = w = 0
+    if n_new is not None:
+        n = _typed(n_new, _I32, "n_new")
+        if n_new is not n and n_new.numel() < B:
+            raise ValueError(f"n_new must be [{B}], got {tuple(n_new.shape)}")
+    if w_new is not None:
+        w = _typed(w_new, _F32, "w_new")
+        if w_new is not w and w_new.numel() != B * (Hkv if kvh else 1) * T:
+            raise ValueError(f"w_new must be [{B}]{[Hkv] if kvh else ''}[{T}], got {tuple(w_new.shape)}")
+    return _pack_rows(k_new.data_ptr(), v_new.data_ptr(), kb, kh, kn, vb, vh, vn, T, n, w)
+
+
+def _state(seen, pos, accum, slots):
+    """Their pointers; the usual case without a call for each (1 us of an insert's host time)."""
+    try:
+        if (seen.dtype is _I32 and pos.dtype is _I32 and slots.dtype is _I32 and accum.dtype is _F32
+                and seen.is_contiguous() and pos.is_contiguous() and slots.is_contiguous() and accum.is_contiguous()):
+            return seen.data_ptr(), pos.data_ptr(), accum.data_ptr(), slots.data_ptr()
+    except AttributeError:   # pointers among them
+        pass
+    return _typed(seen, _I32, "seen"), _typed(pos, _I32, "pos"), _typed(accum, _F32, "accum"), _typed(slots, _I32, "slots")
 
 
 def hill_cache_insert(desc, k_new, v_new, k_cache, v_cache, seen, pos, accum, sinks, recent, slots, n_new=None,
                       w_new=None, kvh=False, stream=None) -> None:
     """New tokens [B][Hkv][T][d] into a cache of fixed size, in place; a full one evicts by accumulated weight."""
-    rows = _new_rows(desc, k_new, v_new, n_new, w_new)
-    _check(load().hill_cache_insert(ctypes.byref(desc), rows, _ptr(k_cache), _ptr(v_cache), _ptr(seen),
-                                    _ptr(pos), _ptr(accum), int(sinks), int(recent), int(bool(kvh)), _ptr(slots),
-                                    _stream(stream)), "hill_cache_insert")
+    rows = _new_rows(desc, k_new, v_new, n_new, w_new, kvh)
+    seen, pos, accum, slots = _state(seen, pos, accum, slots)
+    _check(load().hill_cache_insert(ctypes.byref(desc), rows, _ptr(k_cache), _ptr(v_cache), seen, pos, accum,
+                                    int(sinks), int(recent), 1 if kvh else 0, slots, _stream(stream)),
+           "hill_cache_insert")
 
 
 def hill_cache_insert_q4(desc, k_new, v_new, k4, v4, params, seen, pos, accum, sinks, recent, slots, n_new=None,
                          w_new=None, kvh=False, stream=None) -> None:
     """hill_cache_insert into a 4-bit cache."""
-    rows = _new_rows(desc, k_new, v_new, n_new, w_new)
-    _check(load().hill_cache_insert_q4(ctypes.byref(desc), rows, _ptr(k4), _ptr(v4), _ptr(params),
-                                       _ptr(seen), _ptr(pos), _ptr(accum), int(sinks), int(recent), int(bool(kvh)),
-                                       _ptr(slots), _stream(stream)), "hill_cache_insert_q4")
+    rows = _new_rows(desc, k_new, v_new, n_new, w_new, kvh)
+    seen, pos, accum, slots = _state(seen, pos, accum, slots)
+    _check(load().hill_cache_insert_q4(ctypes.byref(desc), rows, _ptr(k4), _ptr(v4), _ptr(params), seen, pos, accum,
+                                       int(sinks), int(recent), 1 if kvh else 0, slots, _stream(stream)),
+           "hill_cache_insert_q4")
 
 
 def hill_cache_read_q4(desc, k4, v4, params, row_begin, row_end, max_rows, k_cache, v_cache, stream=None) -> None:
     """What slots [row_begin, row_end) of a 4-bit cache stand for, into 16-bit caches."""
-    _check(load().hill_cache_read_q4(ctypes.byref(desc), _ptr(k4), _ptr(v4), _ptr(params), _ptr(row_begin),
-                                     _ptr(row_end), int(max_rows), _ptr(k_cache), _ptr(v_cache), _stream(stream)),
-           "hill_cache_read_q4")
+    _check(load().hill_cache_read_q4(ctypes.byref(desc), _ptr(k4), _ptr(v4), _ptr(params),
+                                     _typed(row_begin, _I32, "row_begin"),
+                                     _typed(row_end, _I32, "row_end"), int(max_rows), _ptr(k_cache),
+                                     _ptr(v_cache), _stream(stream)), "hill_cache_read_q4")
 
 
 def hill_selftest_wait(limit_us: int, stream=None) -> None:
@@ -454,6 +493,7 @@ class BoundedCache:
         if bits not in (4, 16):
             raise ValueError("bits must be 16 or 4")
         self.bits, self.sinks, self.recent, self.kvh, self.max_new = bits, int(sinks), int(recent), bool(kvh), int(max_new)
+        self.dtype = dtype
         rows = (batch, kv_heads) if kvh else (batch,)
         q = torch.empty(batch, heads, 128, dtype=dtype, device=device)
         if bits == 4:
@@ -485,8 +525,8 @@ class BoundedCache:
 
     def attend(self, q, stream=None):
         """Attention of q [B][H][d] over the held tokens; their weights are added to accum."""
-        if q.shape != self.out.shape or q.stride(-1) != 1:
-            raise ValueError(f"q must be {tuple(self.out.shape)} with the last dimension contiguous")
+        if q.shape != self.out.shape or q.stride(-1) != 1 or q.dtype is not self.dtype:
+            raise ValueError(f"q must be {tuple(self.out.shape)} of {self.dtype}, the last dimension contiguous")
         self.desc.q_sb, self.desc.q_sh = q.stride(0), q.stride(1)
         everything = self.desc.capacity
         if self.bits == 4:
