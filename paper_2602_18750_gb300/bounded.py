@@ -25,7 +25,9 @@ def run(bits: int, slots: int, prompt: int, steps: int, batch: int, heads: int =
         dtype=torch.float16, chunk: int = 512, seed: int = 0):
     """Returns (microseconds of a decode step, the last output, the cache)."""
     g = torch.Generator(device="cuda").manual_seed(seed)
-    cache = hill.BoundedCache(batch, heads, kv_heads, slots, dtype, bits, sinks=4, recent=slots // 8, max_new=chunk)
+    sinks = 4
+    chunk = max(1, min(chunk, slots - sinks))   # a full cache has to have room for a chunk
+    cache = hill.BoundedCache(batch, heads, kv_heads, slots, dtype, bits, sinks, recent=slots // 8, max_new=chunk)
     q = torch.randn(batch, heads, 128, generator=g, device="cuda").to(dtype)
     for start in range(0, prompt, chunk):
         cache.insert(*rows(g, batch, kv_heads, min(chunk, prompt - start), dtype))

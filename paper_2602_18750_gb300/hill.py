@@ -485,13 +485,16 @@ class BoundedCache:
 
     ``insert`` puts new tokens in (a full cache evicts by accumulated weight), ``attend`` runs the attention over
     what is held and adds the weights; ``step`` does both.  ``bits`` is 16 or 4.  With ``kvh`` every KV head keeps
-    tokens of its own.
+    tokens of its own.  ``sinks`` + max(``recent``, ``max_new``) slots are needed.  With ``recent`` = ``capacity`` -
+    ``sinks`` the oldest tokens after the sinks go first, whatever their weights: a sliding window.
     """
 
     def __init__(self, batch: int, heads: int, kv_heads: int, capacity: int, dtype=torch.float16, bits: int = 16,
                  sinks: int = 4, recent: int = 0, kvh: bool = False, max_new: int = 1, device="cuda"):
         if bits not in (4, 16):
             raise ValueError("bits must be 16 or 4")
+        if min(sinks, recent, max_new) < 0 or sinks + max(recent, max_new) > capacity:
+            raise ValueError(f"{capacity} slots do not hold {sinks} sinks and {max(recent, max_new)} tokens that stay")
         self.bits, self.sinks, self.recent, self.kvh, self.max_new = bits, int(sinks), int(recent), bool(kvh), int(max_new)
         self.dtype = dtype
         rows = (batch, kv_heads) if kvh else (batch,)

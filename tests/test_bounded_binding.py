@@ -108,3 +108,13 @@ def test_queries_of_another_type(monkeypatch):
                 refused(lambda: cache.attend(x))
             with monkeypatch.context() as m:
                 reaches_the_library(m, lambda: cache.attend(q, stream=1))
+
+
+def test_a_cache_without_room_for_what_is_to_stay(monkeypatch):
+    """sinks + max(recent, max_new) slots are needed: said when the cache is made, not by its first insert."""
+    monkeypatch.setattr(hill, "alloc_window_workspace", lambda *a: torch.zeros(1, dtype=torch.uint8))
+    for bits in (16, 4):
+        make = lambda **kw: hill.BoundedCache(B, HQ, HKV, 32, bits=bits, device="cpu", **kw)
+        make(sinks=4, recent=28, max_new=28)
+        for bad in (dict(max_new=29), dict(recent=29), dict(sinks=32), dict(sinks=-1), dict(recent=-1), dict(max_new=-1)):
+            refused(lambda: make(**bad))
