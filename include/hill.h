@@ -360,15 +360,18 @@ size_t hill_window_workspace_bytes(const hill_desc* desc, int32_t with_accum);
  * <= 2048).  What lies in slots that are not visible does not matter, NaN
  * included; a query, key or value that is seen and not finite leaves the
  * outputs (and weights) that it enters not finite, as the formula has it.
+ * Logits and sums are float32.  A weight meets V as the sum of two numbers of
+ * the cache's type: in bf16 it is off by at most 2^-16 of itself, in fp16 by
+ * 2^-22 of itself and 2^-32 of the head's largest weight.
  * q, K, V as in the calls above; out 16-byte aligned. */
 hill_status hill_window_attn(const hill_desc* desc, const void* q, const void* k_cache, const void* v_cache,
                              const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh, float* accum,
                              float* out, void* ws, size_t ws_bytes, void* stream);
 
 /* hill_window_attn over a 4-bit cache: K and V are the values that the rows
- * stand for (not rounded to 16 bits).  A token's weight times its V scale
- * enters with a relative error of 2^-22 and one of 2^-32 of a head's largest
- * such product; scales and minima of up to 2^100 are summed without overflow. */
+ * stand for (not rounded to 16 bits).  A token's weight times its V scale is
+ * off by at most 2^-21 of itself and 2^-32 of the head's largest such product.
+ * Scales are at least 0; with scales and minima up to 2^90 no sum overflows. */
 hill_status hill_window_attn_q4(const hill_desc* desc, const void* q, const uint8_t* k4, const uint8_t* v4,
                                 const void* params, const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh,
                                 float* accum, float* out, void* ws, size_t ws_bytes, void* stream);

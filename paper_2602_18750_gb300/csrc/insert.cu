@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kIT) hill_insert_kernel(const InsertArgs a) {
 
 // The new rows of (b, g) into the slots that hill_insert_kernel found: a CTA takes
 // `tokens` of them, a warp pairs of tokens in turn with kAhead pairs' rows under
-// way, four CTAs to an SM (66 thousand tokens of 8 KV heads into 4 bits 61 us, 5.3
+// way, four CTAs to an SM (66 thousand tokens of 8 KV heads into 4 bits 60 us, 5.3
 // TB/s; three or four pairs ahead 66 and 67; bound by the encoding's
 // instructions, 180 for two tokens' rows).
 constexpr int kAhead = 2;

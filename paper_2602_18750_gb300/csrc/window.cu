@@ -19,14 +19,15 @@
 //  S = K q^T with the tokens as rows and the pass's query heads as columns.
 //  The weights p = 2^(z - m) of a running maximum m are then already laid out
 //  by column, and an 8x8 transpose of each block (movmatrix) makes them the
-//  column operand of O^T += V^T p, whose rows are the 128 channels.  m is
-//  raised only when a logit passes it by 2^8 (the accumulators then shrink by
-//  the same factor), so the usual tile takes one vote and no shuffles.
-//  p enters as a 16-bit high part plus its 16-bit residual, so that the output
-//  keeps float32-like accuracy; m sits 2^7 below the maximum at which it was set, so that
-//  fp16 holds both parts without underflow for weights down to 2^-32 of the
-//  largest.  With at most 4 query heads the residuals are columns 4 to 7 of
-//  the same product; with more they are a second one.
+//  column operand of O^T += V^T p, whose rows are the 128 channels.  m is set 7
+//  below the largest logit (base 2) and raised only when a weight passes 2^15 (the
+//  accumulators then shrink by the same factor), so the usual tile takes one vote and
+//  no shuffles.
+//  p enters as a 16-bit high part plus its 16-bit residual: in bf16 16 bits of it; in
+//  fp16 22 bits, down to an absolute 2^-25, which is 2^-32 of the largest weight or less: the
+//  tokens beside one of nearly all the weight keep fewer bits, those below 2^-32 of it
+//  may count in the sum of the weights and not in the output.  With at most 4 query heads
+//  the residuals are columns 4 to 7 of the same product; with more they are a second one.
 //
 // 4-bit rows hold value = min + scale * code.  With an integer zero point z0
 // near -min / scale this is scale * (code - z0) + rest, the rest below half a
@@ -35,10 +36,10 @@
 // z0)) + rest sum(q), and o = sum p scale (code - z0) + sum p rest.  The 16-bit
 // operand of the former is F p scale, again a high part and a residual, F a power of two
 // of each head that put its largest product p scale at 2^7 when it was set, and is set
-// again when one passes 2^15: a product is off by at most 2^-22 of itself plus 2^-32 of
+// again when one passes 2^15: a product is off by at most 2^-21 of itself plus 2^-32 of
 // the largest.  (With F from the largest scale alone a row of large values and no weight,
 // or one of all the weight and no value, left the others' products as fp16 subnormals: the output off
-// by 2 % at 2^20 times the other scales, by 4 % beside a token of 2^20 times their weight.)
+// by 2 % at 2^24 times the other scales, by 4 % beside a token of 2^21 times all their weight.)
 // The query is multiplied by a power of two that puts its largest element at 2^14
 // (bf16 queries fit fp16 that way).  (Codes left as fp16 subnormals, which
 // takes masks alone, lost 10 bits: mma aligns a subnormal's products by the
@@ -46,11 +47,12 @@
 //
 // In 16 bits bound by HBM, 512 bytes per token and KV head: 4 x 16-32K tokens of 32
 // heads with their weights 250-260 us, 6.6 TB/s; 1 x 128K of 8 KV heads and 64 query
-// heads 83 us, 6.5 TB/s.  In 4 bits, 136 bytes, the instructions that make fp16
-// of the codes keep it from there: a tile of 32 tokens takes 600, 290 of them for the
-// codes, of the 700 that fit its share of HBM's time: 8 x 64K tokens of 32 heads
-// 388 us, 5.9 TB/s (346 us with the codes passed on unconverted).  Tiles of 64
-// tokens and 12 warps: 32 tokens and 12 or 16 warps took 462 us at the time, 64
+// heads 82 us, 6.5 TB/s.  In 4 bits, 136 bytes, the chain from codes to fp16 to
+// products keeps it from there: a tile of 32 tokens takes 570 instructions, half of them for
+// the codes, three warps to a scheduler, 61 % of the issue slots used, and the forms of
+// 12 warps spill (21 to 29 words loaded): 8 x 64K tokens of 32 heads 391 us,
+// 5.8 TB/s (346 us with the codes passed on unconverted, against 393 then).  Tiles of
+// 64 tokens and 12 warps: 32 tokens and 12 or 16 warps took 462 us at the time, 64
 // tokens and 8 warps 425 against 402.
 #include <cooperative_groups.h>
 

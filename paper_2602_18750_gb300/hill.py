@@ -486,7 +486,8 @@ class BoundedCache:
     ``insert`` puts new tokens in (a full cache evicts by accumulated weight), ``attend`` runs the attention over
     what is held and adds the weights; ``step`` does both.  ``bits`` is 16 or 4.  With ``kvh`` every KV head keeps
     tokens of its own.  ``sinks`` + max(``recent``, ``max_new``) slots are needed.  With ``recent`` = ``capacity`` -
-    ``sinks`` the oldest tokens after the sinks go first, whatever their weights: a sliding window.
+    ``sinks`` the oldest tokens after the sinks go first, whatever their weights: a sliding window (whose attention
+    needs no weights: ``hill_window_attn`` on the same buffers without an accum leaves them out).
     """
 
     def __init__(self, batch: int, heads: int, kv_heads: int, capacity: int, dtype=torch.float16, bits: int = 16,
