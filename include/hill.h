@@ -419,6 +419,110 @@ hill_status hill_cache_read_q4(const hill_desc* desc, const uint8_t* k4, const u
                                const int32_t* row_begin, const int32_t* row_end, int32_t max_rows, void* k_cache,
                                void* v_cache, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Prompts.  Before the decode steps a program runs its prompts through the same
+ * cache: attention of all their queries, and the importance (Sec. 4.1) that
+ * their tokens start with.  Rows of several sequences are packed: sequence b has
+ * the query rows [q_start[b], q_start[b+1]) of q and the key rows [k_start[b],
+ * k_start[b+1]) of k and v (device arrays [B + 1], int32, ascending).  With n
+ * queries and m keys, query i of a sequence is at position i + m - n: the keys
+ * before its prompt are its context, and a query sees key j where
+ *   j <= pos  and  (j < sinks or j > pos - window).
+ * Rows that belong to no sequence are neither read into a result nor written;
+ * offsets that descend or leave the tensors are clamped and recorded as
+ * HILL_ERR_DEVICE.
+ *     q [q_rows][H][d], k and v [k_rows][Hkv][d], strides *_st (row), *_sh (head)
+ * in elements, multiples of 8; 16-byte aligned; d contiguous.  At most 2^30 rows, 512 sequences.
+ * These calls read all their inputs after the dependency wait (see above). */
+typedef struct {
+  int32_t batch;         /* B >= 0, at most 512                       */
+  int32_t num_q_heads;   /* H >= 1                                    */
+  int32_t num_kv_heads;  /* Hkv >= 1, H % Hkv == 0                    */
+  int32_t head_dim;      /* d (128)                                   */
+  int32_t dtype;         /* hill_dtype of q, k, v and out             */
+  int32_t q_rows, k_rows;
+  int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh;
+} hill_packed;
+
+/* Attention of every query over the keys that it sees (Eq. 1):
+ *   out[i][h] = sum_j p_ij v_j,  p_ij = exp(z_ij - lse[i][h]),
+ *   z_ij = q_i . k_j / sqrt(d),  lse[i][h] = ln sum_j exp(z_ij).
+ * out [q_rows][H][d] in desc's type, dense, 16-byte aligned; lse [q_rows][H]
+ * float32, dense, or NULL.  A query that sees nothing has zeros and -infinity.  What lies in keys and
+ * values that a query does not see does not matter to it, NaN included.
+ * Logits, sums and outputs are held in float32; a weight meets v rounded to the
+ * type of v (half a step of that type), and the output is rounded once. */
+hill_status hill_prompt_attn(const hill_packed* desc, const void* q, const void* k, const void* v,
+                             const int32_t* q_start, const int32_t* k_start, int32_t sinks, int32_t window,
+                             void* out, float* lse, void* stream);
+
+/* Bytes of workspace of hill_prompt_importance.  Returns 0 for an invalid descriptor. */
+size_t hill_prompt_workspace_bytes(const hill_packed* desc);
+
+/* The weights of those queries summed for each key, added to a running importance:
+ *   accum[b][j] += sum_h sum_i exp(z_ij - lse[i][h])
+ * over the `newest` last queries of sequence b (all, if it has no more) that
+ * see key j.  lse is that of hill_prompt_attn.  accum [B][cap] (kvh: [B][Hkv][cap], each KV
+ * head the sum over its own query heads), float32, dense.  Keys past cap are left out
+ * and recorded as HILL_ERR_DEVICE.  Sums are float32, in a fixed order. */
+hill_status hill_prompt_importance(const hill_packed* desc, const void* q, const void* k, const float* lse,
+                                   const int32_t* q_start, const int32_t* k_start, int32_t sinks, int32_t window,
+                                   int32_t newest, int32_t kvh, float* accum, int32_t cap, void* ws,
+                                   size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * A cache in pages.  Position p of sequence b lies in page table[b][p / page],
+ * slot p % page of the pools
+ *   k, v    [pages][Hkv][page][d], dense, 16-byte aligned, in desc's type, or (scales
+ *           given) as E4M3 codes, one byte each;
+ *   scales  [pages][Hkv][page][2] float32 (K scale, V scale), dense, 16-byte aligned, or NULL.
+ * A row of codes is e4m3(x * (448 * (1 / amax))) with amax = max |x|, its scale amax * (1 / 448)
+ * (float32 steps, round to nearest even), and it stands for code * scale; rows with amax below
+ * 2^-119 stand for zeros.  `page` is a multiple of 16; table [B][cols] covers cols * page
+ * positions.  A page number outside [0, pages) stands for nothing: entries of
+ * positions that a call does not touch may hold any; one that it
+ * touches is recorded as HILL_ERR_DEVICE, reads as zeros and is not written.
+ * These calls read all their inputs after the dependency wait (see above). */
+typedef struct {
+  void* k;
+  void* v;
+  float* scales;
+  const int32_t* table;
+  int32_t pages, page, cols;
+} hill_pages;
+
+/* hill_window_attn over a cache in pages: the same visible positions, outputs,
+ * importance and workspace (hill_window_workspace_bytes).  desc->capacity =
+ * cols * page; its K and V strides are not used.  E4M3: K and V are the values that the rows stand for; a
+ * token's weight times its V scale is off by at most 2^-21 of itself and 2^-32
+ * of the head's largest such product. */
+hill_status hill_paged_attn(const hill_desc* desc, const void* q, const hill_pages* pages, const int32_t* lens,
+                            int32_t sinks, int32_t window, int32_t kvh, float* accum, float* out, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/* New rows of several sequences, packed: [rows][Hkv][d] in desc's type, strides in
+ * elements, multiples of 8; 16-byte aligned; d contiguous. */
+typedef struct {
+  const void* k;
+  const void* v;
+  int64_t k_st, k_sh, v_st, v_sh;
+  int32_t rows;
+} hill_rows;
+
+/* New rows into their pages, quantised where the pools hold codes: row t of sequence b
+ * (starts[b] <= t < starts[b+1], device array [B + 1]) becomes position begin[b] + t - starts[b].
+ * Rows before the first sequence or behind the last go nowhere.  Positions below 0 or past the
+ * table are dropped and recorded as HILL_ERR_DEVICE.  No two rows of a call may
+ * have the same place.  desc gives batch, num_kv_heads and dtype. */
+hill_status hill_paged_write(const hill_desc* desc, const hill_pages* pages, const hill_rows* rows,
+                             const int32_t* starts, const int32_t* begin, void* stream);
+
+/* Positions [row_begin[b], row_end[b]) (clamped to the table and to desc's capacity) of every KV
+ * head into 16-bit caches of desc's strides, for the calls that read those: copied, or
+ * code * scale rounded to desc's type.  max_rows bounds row_end - row_begin over b. */
+hill_status hill_paged_read(const hill_desc* desc, const hill_pages* pages, const int32_t* row_begin,
+                            const int32_t* row_end, int32_t max_rows, void* k_cache, void* v_cache, void* stream);
+
 /* Number of kernels this library has launched (or recorded into a CUDA graph
  * under stream capture) in this process so far, over all devices.  Lets a
  * caller count the kernels one call or one captured graph contains. */

@@ -994,45 +994,24 @@ WindowLayout window_layout(const hill_desc* d, bool with_accum, int sms) {
   return L;
 }
 
-// What hill_window_attn and its 4-bit form share.
-hill_status window_attn(const hill_desc* desc, const void* q, const void* k, const void* v, const void* params,
-                        const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh, float* accum, float* out,
-                        void* ws, size_t ws_bytes, void* stream) {
-  hill_status s = check_desc(desc);
-  if (s != HILL_OK) return s;
-  if (!q || !k || !v || !lens || !out || sinks < 0 || window < 0) return HILL_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (params && !aligned16(params)))
-    return HILL_ERR_INVALID_ARG;
+// The checks and arguments that the attention calls over a visible part share, but for the cache itself.
+hill_status plan_window(const hill_desc* desc, const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh,
+                        float* accum, float* out, const void* q, void* ws, size_t ws_bytes, DeviceInfo* di,
+                        WindowArgs* plan) {
   if (kvh && (int64_t)desc->batch * desc->num_kv_heads > window_max_rows()) return HILL_ERR_UNSUPPORTED;
   // the list of tiles is numbered in 32 bits
   const int G = desc->num_q_heads / desc->num_kv_heads;
   if ((int64_t)desc->batch * desc->num_kv_heads * cdiv(G, window_heads_per_pass(G, 0)) * cdiv(desc->capacity, 32) >= INT32_MAX)
     return HILL_ERR_UNSUPPORTED;
-  DeviceInfo di;
-  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
-  const WindowLayout L = window_layout(desc, accum != nullptr, di.sms);
+  if (device_info(di) != cudaSuccess) return HILL_ERR_CUDA;
+  const WindowLayout L = window_layout(desc, accum != nullptr, di->sms);
   if (!ws || ws_bytes < L.total) return HILL_ERR_WORKSPACE;
-  if (desc->batch == 0) return HILL_OK;
   unsigned char* base = ws_base(ws);
-  WindowArgs a{};
+  WindowArgs& a = *plan;
+  a = WindowArgs{};
   const int64_t shown = std::min<int64_t>(desc->capacity, (int64_t)sinks + window);
   a.heads = window_heads_per_pass(G, shown * desc->batch * desc->num_kv_heads);
   a.passes = cdiv(G, a.heads);
-  if (params) {
-    const int tile = window_q4_tile(a.heads);
-    s = make_q4_map(desc, k, tile, &a.kmap);
-    if (s == HILL_OK) s = make_q4_map(desc, v, tile, &a.vmap);
-  } else {
-    int where[3];
-    s = make_cache_map(desc, k, desc->k_sb, desc->k_sh, desc->k_sn, &a.kmap, where);
-    a.kdim_tok = where[0];
-    a.kdim_head = where[1];
-    if (s == HILL_OK) s = make_cache_map(desc, v, desc->v_sb, desc->v_sh, desc->v_sn, &a.vmap, where);
-    a.vdim_tok = where[0];
-    a.vdim_head = where[1];
-  }
-  if (s != HILL_OK) return s;
-  a.params = static_cast<const uint2*>(params);
   a.q = q;
   a.q_sb = desc->q_sb;
   a.q_sh = desc->q_sh;
@@ -1056,7 +1035,38 @@ hill_status window_attn(const hill_desc* desc, const void* q, const void* k, con
     a.logits = reinterpret_cast<float*>(base + L.logits);
     a.lstride = (desc->capacity + 63) & ~63;
   }
-  a.err = di.err;
+  a.err = di->err;
+  return HILL_OK;
+}
+
+// What hill_window_attn and its 4-bit form share.
+hill_status window_attn(const hill_desc* desc, const void* q, const void* k, const void* v, const void* params,
+                        const int32_t* lens, int32_t sinks, int32_t window, int32_t kvh, float* accum, float* out,
+                        void* ws, size_t ws_bytes, void* stream) {
+  hill_status s = check_desc(desc);
+  if (s != HILL_OK) return s;
+  if (!q || !k || !v || !lens || !out || sinks < 0 || window < 0) return HILL_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || (params && !aligned16(params)))
+    return HILL_ERR_INVALID_ARG;
+  DeviceInfo di;
+  WindowArgs a;
+  s = plan_window(desc, lens, sinks, window, kvh, accum, out, q, ws, ws_bytes, &di, &a);
+  if (s != HILL_OK || desc->batch == 0) return s;
+  if (params) {
+    const int tile = window_q4_tile(a.heads);
+    s = make_q4_map(desc, k, tile, &a.kmap);
+    if (s == HILL_OK) s = make_q4_map(desc, v, tile, &a.vmap);
+  } else {
+    int where[3];
+    s = make_cache_map(desc, k, desc->k_sb, desc->k_sh, desc->k_sn, &a.kmap, where);
+    a.kdim_tok = where[0];
+    a.kdim_head = where[1];
+    if (s == HILL_OK) s = make_cache_map(desc, v, desc->v_sb, desc->v_sh, desc->v_sn, &a.vmap, where);
+    a.vdim_tok = where[0];
+    a.vdim_head = where[1];
+  }
+  if (s != HILL_OK) return s;
+  a.params = static_cast<const uint2*>(params);
   int kernels = 0;
   const cudaError_t e =
       launch_window_attn(a, desc->dtype, params != nullptr, di.sms, static_cast<cudaStream_t>(stream), &kernels);
@@ -1191,6 +1201,296 @@ hill_status hill_cache_read_q4(const hill_desc* desc, const uint8_t* k4, const u
   a.cap32 = cap32_of(desc);
   return from_cuda(counted(launch_read_q4(a, desc->dtype, std::min(max_rows, desc->capacity),
                                           static_cast<cudaStream_t>(stream)), 1));
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Prompts and caches in pages (prompt.cu, importance.cu, paged.cu, pages.cu).
+namespace hill {
+namespace {
+
+constexpr int kRowsMax = 1 << 30;     // positions and sums of positions and windows stay in 32 bits
+constexpr int kTileRows = 128;        // query rows of a tile (query heads x tokens), keys of a tile
+
+hill_status check_packed(const hill_packed* d) {
+  if (!d) return HILL_ERR_INVALID_ARG;
+  if (d->batch < 0 || d->num_q_heads <= 0 || d->num_kv_heads <= 0 || d->head_dim <= 0 || d->q_rows < 0 || d->k_rows < 0)
+    return HILL_ERR_INVALID_ARG;
+  if (d->num_q_heads % d->num_kv_heads) return HILL_ERR_INVALID_ARG;
+  if (d->dtype != HILL_F16 && d->dtype != HILL_BF16) return HILL_ERR_INVALID_ARG;
+  if (!stride_ok(d->q_st) || !stride_ok(d->q_sh) || !stride_ok(d->k_st) || !stride_ok(d->k_sh) ||
+      !stride_ok(d->v_st) || !stride_ok(d->v_sh))
+    return HILL_ERR_INVALID_ARG;
+  if (d->head_dim != kHeadDim || d->batch > score_max_batch()) return HILL_ERR_UNSUPPORTED;
+  if (d->q_rows > kRowsMax || d->k_rows > kRowsMax) return HILL_ERR_UNSUPPORTED;
+  // tiles are numbered in 32 bits, with 16 to spare for parts of them
+  if ((int64_t)d->num_q_heads * ((int64_t)d->q_rows / kTileRows + d->batch + 1) > kRowsMax ||
+      (int64_t)d->num_kv_heads * ((int64_t)d->k_rows / kTileRows + d->batch + 1) * 16 > kRowsMax)
+    return HILL_ERR_UNSUPPORTED;
+  return HILL_OK;
+}
+
+// 3-D map of packed rows (head dimension, head, row), box = 64 dims x heads x rows, 128-byte swizzle.
+hill_status make_rows_map(int dtype, const void* p, int heads, int64_t rows, int64_t sh, int64_t st, int box_heads,
+                          int box_rows, CUtensorMap* map) {
+  auto fn = encode_tiled();
+  if (!fn) return HILL_ERR_CUDA;
+  // a dimension of extent 1 may carry any stride
+  if (heads <= 1) sh = kHeadDim;
+  if (rows <= 1) st = std::max<int64_t>(sh * heads, kHeadDim);
+  cuuint64_t gdim[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)heads, (cuuint64_t)std::max<int64_t>(rows, 1)};
+  cuuint64_t gstr[2] = {(cuuint64_t)sh * 2, (cuuint64_t)st * 2};
+  cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows};
+  cuuint32_t estr[3] = {1, 1, 1};
+  if (gstr[0] == 0 || gstr[1] == 0) return HILL_ERR_UNSUPPORTED;
+  const CUtensorMapDataType dt = dtype == HILL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  CUresult r = fn(map, dt, 3, const_cast<void*>(p), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HILL_OK : HILL_ERR_UNSUPPORTED;
+}
+
+// What both calls over prompts take; the maps (v may be NULL).
+hill_status prompt_args(const hill_packed* d, const void* q, const void* k, const void* v, const int32_t* q_start,
+                        const int32_t* k_start, int32_t sinks, int32_t window, PromptArgs* a) {
+  a->q = q;
+  a->k = k;
+  a->v = v;
+  a->q_st = d->q_st;
+  a->q_sh = d->q_sh;
+  a->k_st = d->k_st;
+  a->k_sh = d->k_sh;
+  a->v_st = d->v_st;
+  a->v_sh = d->v_sh;
+  a->q_start = q_start;
+  a->k_start = k_start;
+  a->B = d->batch;
+  a->H = d->num_q_heads;
+  a->Hkv = d->num_kv_heads;
+  a->G = a->H / a->Hkv;
+  a->q_rows = d->q_rows;
+  a->k_rows = d->k_rows;
+  a->q_heads = std::min(a->G, kTileRows);
+  a->q_tokens = kTileRows / a->q_heads;
+  a->passes = cdiv(a->G, a->q_heads);
+  a->sinks = std::min(sinks, kRowsMax);
+  a->window = std::min(window, kRowsMax);
+  hill_status s = make_rows_map(d->dtype, q, a->H, a->q_rows, a->q_sh, a->q_st, a->q_heads, a->q_tokens, &a->qmap);
+  // (without keys nothing is read through these)
+  if (s == HILL_OK) s = make_rows_map(d->dtype, d->k_rows ? k : q, a->Hkv, a->k_rows, a->k_sh, a->k_st, 1, kTileRows, &a->kmap);
+  if (s == HILL_OK && v)
+    s = make_rows_map(d->dtype, d->k_rows ? v : q, a->Hkv, a->k_rows, a->v_sh, a->v_st, 1, kTileRows, &a->vmap);
+  return s;
+}
+
+size_t prompt_workspace(const hill_packed* d, int sms) {
+  const int splits = importance_splits(d->batch, d->num_kv_heads, d->k_rows, sms);
+  return align_up((size_t)splits * d->num_kv_heads * d->k_rows * sizeof(float)) + kAlign;
+}
+
+// 3-D map of a pool (head dimension, slot, page * Hkv + KV head), box = 128 bytes x group slots.
+hill_status make_pool_map(const hill_desc* d, const hill_pages* p, const void* pool, int group, CUtensorMap* map) {
+  auto fn = encode_tiled();
+  if (!fn) return HILL_ERR_CUDA;
+  const cuuint64_t row = p->scales ? kHeadDim : kRowBytes;
+  cuuint64_t gdim[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)p->page, (cuuint64_t)std::max<int64_t>((int64_t)p->pages * d->num_kv_heads, 1)};
+  cuuint64_t gstr[2] = {row, (cuuint64_t)p->page * row};
+  cuuint32_t box[3] = {p->scales ? 128u : 64u, (cuuint32_t)group, 1};
+  cuuint32_t estr[3] = {1, 1, 1};
+  const CUtensorMapDataType dt = p->scales ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                 : d->dtype == HILL_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                         : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+  CUresult r = fn(map, dt, 3, const_cast<void*>(pool), gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HILL_OK : HILL_ERR_UNSUPPORTED;
+}
+
+// Scales of an E4M3 pool as (2 * page, pages * Hkv), box = 2 * group.
+hill_status make_scales_map(const hill_desc* d, const hill_pages* p, int group, CUtensorMap* map) {
+  auto fn = encode_tiled();
+  if (!fn) return HILL_ERR_CUDA;
+  cuuint64_t gdim[2] = {(cuuint64_t)p->page * 2, (cuuint64_t)std::max<int64_t>((int64_t)p->pages * d->num_kv_heads, 1)};
+  cuuint64_t gstr[1] = {(cuuint64_t)p->page * 8};
+  cuuint32_t box[2] = {(cuuint32_t)group * 2, 1};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, p->scales, gdim, gstr, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? HILL_OK : HILL_ERR_UNSUPPORTED;
+}
+
+hill_status check_pages(const hill_desc* d, const hill_pages* p) {
+  if (!p || p->pages < 0 || p->page <= 0 || p->cols < 0) return HILL_ERR_INVALID_ARG;
+  if ((p->pages > 0 && (!p->k || !p->v)) || (p->cols > 0 && d->batch > 0 && !p->table)) return HILL_ERR_INVALID_ARG;
+  if (!aligned16(p->k) || !aligned16(p->v) || !aligned16(p->scales)) return HILL_ERR_INVALID_ARG;
+  if (p->page % 16) return HILL_ERR_UNSUPPORTED;
+  if (p->page > kRowsMax / 2 || (int64_t)(p->pages + 1) * d->num_kv_heads > kRowsMax || (int64_t)p->cols * p->page > kRowsMax)
+    return HILL_ERR_UNSUPPORTED;
+  return HILL_OK;
+}
+
+PagesArgs pages_args(const hill_desc* d, const hill_pages* p, unsigned* err) {
+  PagesArgs a{};
+  a.pk = p->k;
+  a.pv = p->v;
+  a.scales = reinterpret_cast<float2*>(p->scales);
+  a.table = p->table;
+  a.cols = p->cols;
+  a.page = p->page;
+  a.pages = p->pages;
+  a.B = d->batch;
+  a.Hkv = d->num_kv_heads;
+  a.cap = p->cols * p->page;
+  a.err = err;
+  return a;
+}
+
+}  // namespace
+}  // namespace hill
+
+extern "C" {
+
+hill_status hill_prompt_attn(const hill_packed* desc, const void* q, const void* k, const void* v,
+                             const int32_t* q_start, const int32_t* k_start, int32_t sinks, int32_t window,
+                             void* out, float* lse, void* stream) {
+  hill_status s = check_packed(desc);
+  if (s != HILL_OK) return s;
+  if (sinks < 0 || window < 0) return HILL_ERR_INVALID_ARG;
+  if (desc->batch == 0 || desc->q_rows == 0) return HILL_OK;
+  if (!q || !q_start || !k_start || !out || (desc->k_rows > 0 && (!k || !v))) return HILL_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return HILL_ERR_INVALID_ARG;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
+  PromptArgs a{};
+  s = prompt_args(desc, q, k, v ? v : q, q_start, k_start, sinks, window, &a);
+  if (s != HILL_OK) return s;
+  a.out = out;
+  a.lse = lse;
+  a.err = di.err;
+  int kernels = 0;
+  const cudaError_t e = launch_prompt_attn(a, desc->dtype, di.sms, static_cast<cudaStream_t>(stream), &kernels);
+  return from_cuda(counted(e, kernels));
+}
+
+size_t hill_prompt_workspace_bytes(const hill_packed* desc) {
+  if (check_packed(desc) != HILL_OK) return 0;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return 0;
+  return prompt_workspace(desc, di.sms);
+}
+
+hill_status hill_prompt_importance(const hill_packed* desc, const void* q, const void* k, const float* lse,
+                                   const int32_t* q_start, const int32_t* k_start, int32_t sinks, int32_t window,
+                                   int32_t newest, int32_t kvh, float* accum, int32_t cap, void* ws,
+                                   size_t ws_bytes, void* stream) {
+  hill_status s = check_packed(desc);
+  if (s != HILL_OK) return s;
+  if (sinks < 0 || window < 0 || newest < 0 || cap < 0 || cap > kRowsMax) return HILL_ERR_INVALID_ARG;
+  if (desc->batch == 0 || desc->q_rows == 0 || desc->k_rows == 0) return HILL_OK;
+  if (!q || !k || !lse || !q_start || !k_start || (cap > 0 && !accum)) return HILL_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k)) return HILL_ERR_INVALID_ARG;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
+  if (!ws || ws_bytes < prompt_workspace(desc, di.sms)) return HILL_ERR_WORKSPACE;
+  PromptArgs a{};
+  s = prompt_args(desc, q, k, nullptr, q_start, k_start, sinks, window, &a);
+  if (s != HILL_OK) return s;
+  a.newest = std::min(newest, kRowsMax);
+  a.lse = const_cast<float*>(lse);
+  a.accum = accum;
+  a.cap = cap;
+  a.kvh = kvh ? 1 : 0;
+  a.part = reinterpret_cast<float*>(ws_base(ws));
+  a.splits = importance_splits(desc->batch, desc->num_kv_heads, desc->k_rows, di.sms);
+  a.err = di.err;
+  int kernels = 0;
+  const cudaError_t e = launch_prompt_importance(a, desc->dtype, di.sms, static_cast<cudaStream_t>(stream), &kernels);
+  return from_cuda(counted(e, kernels));
+}
+
+hill_status hill_paged_attn(const hill_desc* desc, const void* q, const hill_pages* pages, const int32_t* lens,
+                            int32_t sinks, int32_t window, int32_t kvh, float* accum, float* out, void* ws,
+                            size_t ws_bytes, void* stream) {
+  hill_status s = check_desc(desc);
+  if (s != HILL_OK) return s;
+  s = check_pages(desc, pages);
+  if (s != HILL_OK) return s;
+  if (!q || !lens || !out || sinks < 0 || window < 0 || (int64_t)pages->cols * pages->page != desc->capacity)
+    return HILL_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out)) return HILL_ERR_INVALID_ARG;
+  PagedArgs a{};
+  DeviceInfo di;
+  s = plan_window(desc, lens, sinks, window, kvh, accum, out, q, ws, ws_bytes, &di, &a.w);
+  if (s != HILL_OK || desc->batch == 0) return s;
+  a.group = pages->page % 32 ? 16 : 32;
+  // without pages there is nothing to read: every table entry is outside the pool
+  const void* any = q;
+  s = make_pool_map(desc, pages, pages->pages ? pages->k : any, a.group, &a.w.kmap);
+  if (s == HILL_OK) s = make_pool_map(desc, pages, pages->pages ? pages->v : any, a.group, &a.w.vmap);
+  if (s == HILL_OK && pages->scales) s = make_scales_map(desc, pages, a.group, &a.smap);
+  if (s != HILL_OK) return s;
+  a.table = pages->table;
+  a.cols = pages->cols;
+  a.page = pages->page;
+  a.pages = pages->pages;
+  int kernels = 0;
+  const cudaError_t e = launch_paged_attn(a, desc->dtype, pages->scales != nullptr, di.sms,
+                                          static_cast<cudaStream_t>(stream), &kernels);
+  return from_cuda(counted(e, kernels));
+}
+
+hill_status hill_paged_write(const hill_desc* desc, const hill_pages* pages, const hill_rows* rows,
+                             const int32_t* starts, const int32_t* begin, void* stream) {
+  hill_status s = check_desc(desc);
+  if (s != HILL_OK) return s;
+  s = check_pages(desc, pages);
+  if (s != HILL_OK) return s;
+  if (!rows || rows->rows < 0) return HILL_ERR_INVALID_ARG;
+  if (!stride_ok(rows->k_st) || !stride_ok(rows->k_sh) || !stride_ok(rows->v_st) || !stride_ok(rows->v_sh))
+    return HILL_ERR_INVALID_ARG;
+  if (rows->rows > kRowsMax || (int64_t)rows->rows * desc->num_kv_heads > ((int64_t)kRowsMax << 5)) return HILL_ERR_UNSUPPORTED;
+  if (desc->batch == 0 || rows->rows == 0) return HILL_OK;
+  if (!rows->k || !rows->v || !starts || !begin || !aligned16(rows->k) || !aligned16(rows->v)) return HILL_ERR_INVALID_ARG;
+  DeviceInfo di;
+  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
+  PagesArgs a = pages_args(desc, pages, di.err);
+  a.k = rows->k;
+  a.v = rows->v;
+  a.k_sn = rows->k_st;
+  a.k_sh = rows->k_sh;
+  a.v_sn = rows->v_st;
+  a.v_sh = rows->v_sh;
+  a.rows = rows->rows;
+  a.starts = starts;
+  a.begin = begin;
+  return from_cuda(counted(launch_paged_write(a, desc->dtype, static_cast<cudaStream_t>(stream)), 1));
+}
+
+hill_status hill_paged_read(const hill_desc* desc, const hill_pages* pages, const int32_t* row_begin,
+                            const int32_t* row_end, int32_t max_rows, void* k_cache, void* v_cache, void* stream) {
+  hill_status s = check_desc(desc);
+  if (s != HILL_OK) return s;
+  s = check_pages(desc, pages);
+  if (s != HILL_OK) return s;
+  if (!row_begin || !row_end || max_rows < 0 || !k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache))
+    return HILL_ERR_INVALID_ARG;
+  DeviceInfo di;
+  PagesArgs a = pages_args(desc, pages, nullptr);
+  a.cap = std::min(a.cap, desc->capacity);
+  if (desc->batch == 0 || a.cap == 0 || max_rows == 0) return HILL_OK;
+  if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
+  a.err = di.err;
+  a.ko = k_cache;
+  a.vo = v_cache;
+  a.k_sb = desc->k_sb;
+  a.k_sh = desc->k_sh;
+  a.k_sn = desc->k_sn;
+  a.v_sb = desc->v_sb;
+  a.v_sh = desc->v_sh;
+  a.v_sn = desc->v_sn;
+  a.begin = row_begin;
+  a.end = row_end;
+  return from_cuda(counted(launch_paged_read(a, desc->dtype, std::min(max_rows, a.cap),
+                                             static_cast<cudaStream_t>(stream)), 1));
 }
 
 }  // extern "C"

@@ -171,6 +171,58 @@ struct WindowArgs {
   unsigned* err;
 };
 
+// The same over a cache in pages (paged.cu).  w's maps: 3-D (head dimension, slot of a page, page * Hkv +
+// KV head), 128-byte swizzle, box = 64 dims of 16 bits or 128 codes x `group` slots.
+struct PagedArgs {
+  WindowArgs w;
+  CUtensorMap smap;      // E4M3: scales as (2 * page, pages * Hkv), box = 2 * group
+  const int32_t* table;  // [B][cols]
+  int cols, page, pages;
+  int group;             // consecutive slots per box: 16, or 32 where a page is a multiple of 32
+};
+
+// Rows into and out of pages (pages.cu).
+struct PagesArgs {
+  void* pk;              // pools [pages][Hkv][page][d]: 16 bits, or E4M3 codes
+  void* pv;
+  float2* scales;        // E4M3: [pages][Hkv][page] (K scale, V scale), else NULL
+  const int32_t* table;  // [B][cols]
+  int cols, page, pages;
+  int B, Hkv, cap;       // cap: positions that the table covers, of a read those of the 16-bit cache at most
+  const void* k;         // write: new rows [rows][Hkv][d], strides sn (row) and sh
+  const void* v;
+  void* ko;              // read: 16-bit caches, strides sb, sn, sh
+  void* vo;
+  int64_t k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;
+  int rows;
+  const int32_t* begin;  // [B] first positions
+  const int32_t* end;    // [B], read
+  const int32_t* starts; // [B + 1] first new row of each sequence, write
+  unsigned* err;
+};
+
+// Prompts: packed rows of several sequences (prompt.cu, importance.cu).
+struct PromptArgs {
+  CUtensorMap qmap, kmap, vmap;   // 3-D (head dimension, head, row), 128-byte swizzle; boxes of 64 dims x q_heads x
+                                  // q_tokens query rows, 64 dims x 1 x 128 keys
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh;
+  const int32_t* q_start;         // [B + 1] first row of each sequence
+  const int32_t* k_start;
+  int B, H, Hkv, G, q_rows, k_rows;
+  int q_heads, q_tokens, passes;  // query heads and tokens of a tile of at most 128 rows; tiles for all heads of a group
+  int sinks, window, newest;
+  void* out;                      // [q_rows][H][d]
+  float* lse;                     // [q_rows][H], or NULL; importance: read
+  float* accum;                   // [B][cap], kvh: [B][Hkv][cap]
+  int cap, kvh;
+  float* part;                    // importance: [splits][Hkv][k_rows] sums
+  int splits;
+  unsigned* err;
+};
+
 // Inserts into a cache of fixed size (insert.cu).
 struct InsertArgs {
   const void* k_new;     // [B][Hkv][max_new][d], strides kn_*
@@ -312,6 +364,23 @@ int window_warps(bool q4, int heads_per_pass);   // per CTA, one CTA per SM
 int window_q4_tile(int heads_per_pass);           // tokens
 int window_max_rows();
 cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms, cudaStream_t st, int* kernels);
+
+// The merge of the partials of warps_in_all warps (0: there are none), and the importance.
+cudaError_t launch_window_finish(const WindowArgs& a, int warps_in_all, int sms, cudaStream_t st, int* kernels);
+
+// paged.cu
+cudaError_t launch_paged_attn(const PagedArgs& a, int dtype, bool f8, int sms, cudaStream_t st, int* kernels);
+
+// pages.cu
+cudaError_t launch_paged_write(const PagesArgs& a, int dtype, cudaStream_t st);
+cudaError_t launch_paged_read(const PagesArgs& a, int dtype, int max_rows, cudaStream_t st);
+
+// prompt.cu
+cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels);
+
+// importance.cu
+int importance_splits(int B, int Hkv, int64_t k_rows, int sms);
+cudaError_t launch_prompt_importance(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels);
 
 // insert.cu
 cudaError_t launch_insert(const InsertArgs& a, int dtype, int sms, cudaStream_t st, int* kernels);

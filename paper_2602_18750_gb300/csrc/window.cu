@@ -58,16 +58,13 @@
 
 #include <algorithm>
 #include <atomic>
-#include <type_traits>
 
-#include "hill_internal.h"
+#include "window_common.cuh"
 
 namespace cg = cooperative_groups;
 
 namespace hill {
 namespace {
-
-constexpr int kMaxRows = 2048;            // rows of lens
 
 // Tiles and rings.  4 bits: a slot holds the K codes, V codes and parameters of
 // a tile, and after them 16 bytes per two tokens that no copy writes (notes);
@@ -84,56 +81,6 @@ struct Cfg {
   static constexpr int kSlot = Q4 ? kNotes + kT * 8 : 2 * kBox;
   static constexpr int kSmem = kNW * kSlots * kSlot + 1024;   // + alignment slack
 };
-
-// The visible tiles of a row of n tokens: [0, sink) and from tile `first` on.
-template <int T>
-struct Tiles {
-  int n, start;        // tokens; first token of the window
-  int sink, first, count;
-  __device__ __forceinline__ Tiles(int len, int cap, int sinks, int window) {
-    n = len < 0 ? 0 : min(len, cap);
-    start = max(0, n - window);
-    first = start / T;
-    const int shown = min(sinks, start);   // sinks outside the window
-    const int win = start < n ? (n + T - 1) / T - first : 0;
-    sink = (shown + T - 1) / T;
-    if (win > 0) sink = min(sink, first);
-    count = sink + win;
-  }
-  __device__ __forceinline__ int token(int i) const { return (i < sink ? i : first + i - sink) * T; }
-};
-
-// A list of items dealt out to n warps (at most as many as items, n < 2^15) in
-// parts of equal length: where part w begins, floor(w items / n), and the warp that owns item x.
-struct Parts {
-  int n, each, rest;
-  float per;
-  __device__ __forceinline__ Parts(int items, int n_) : n(n_), each(items / n_), rest(items - items / n_ * n_) {
-    per = __fdividef((float)n_, (float)items);
-  }
-  __device__ __forceinline__ int begin(int w) const { return w * each + w * rest / n; }
-  __device__ __forceinline__ int of(int x) const {
-    int w = min((int)((float)x * per), n - 1);   // within 1
-    while (begin(w) > x) --w;
-    while (w + 1 < n && begin(w + 1) <= x) ++w;
-    return w;
-  }
-};
-
-__device__ __forceinline__ uint32_t transpose8(uint32_t v) {
-  uint32_t d;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
-  return d;
-}
-
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void* tmap, int c0, int c1, int c2, uint32_t bar,
-                                            uint64_t policy) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
-      " [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(dst),
-      "l"(tmap), "r"(c0), "r"(c1), "r"(c2), "r"(bar), "l"(policy)
-      : "memory");
-}
 
 // (a & M) | 0x64006400 in one instruction (the compiler's own choice for the
 // C expression was two: 8 x 64K tokens of 32 heads 480 us, with this 412).
@@ -183,57 +130,6 @@ __device__ __forceinline__ __half2 high_twice(uint32_t v) {   // the high half i
 __device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
-
-__device__ __forceinline__ uint2 lds64(uint32_t addr) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
-  return v;
-}
-
-// Powers of two as floats, from 2^-121 to kMaxFactor = 2^126.  fit_below: the factor that puts
-// the largest of some products, t, at 2^7 if f takes it past 2^12, else f.
-constexpr float kMaxFactor = 8.507059173e37f;
-__device__ __forceinline__ float fit_below(float f, float t) {
-  return t * f > 4096.f ? __uint_as_float((261u - (__float_as_uint(t) >> 23)) << 23) : f;
-}
-// f times 2^k, k >= 0, or as much of it as there is room for: `taken`.
-__device__ __forceinline__ float times_pow2(float f, int k, int& taken) {
-  const uint32_t e = __float_as_uint(f) >> 23;
-  taken = min(k, 253 - (int)e);
-  return __uint_as_float((e + taken) << 23);
-}
-__device__ __forceinline__ float inverse_pow2(float f) { return __uint_as_float((254u << 23) - __float_as_uint(f)); }
-
-template <int I> using Int = std::integral_constant<int, I>;
-template <bool I> using Bool = std::integral_constant<bool, I>;
-
-// Where the warp stands in the list: a run of tiles of consecutive tokens.
-struct Walk {
-  int row, pair, tile;   // pair: KV head and pass within the row; tile: the run's first
-  int j, left;           // first token and length of the run
-};
-
-// Weighted sums of one query head, four channels per lane, from partials.
-struct Merged {
-  float m = kNegHuge, l = 0.f;
-  float4 o{0.f, 0.f, 0.f, 0.f};
-  template <int N>
-  __device__ __forceinline__ void add(const float2 (&ml)[N], const float4 (&v)[N]) {
-    float mn = m;
-#pragma unroll
-    for (int u = 0; u < N; ++u) mn = fmaxf(mn, ml[u].x);
-    const float f = ex2(m - mn);
-    m = mn;
-    l *= f;
-    o = float4{o.x * f, o.y * f, o.z * f, o.w * f};
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-      const float s = ex2(ml[u].x - mn);
-      l = fmaf(ml[u].y, s, l);
-      o = float4{fmaf(v[u].x, s, o.x), fmaf(v[u].y, s, o.y), fmaf(v[u].z, s, o.z), fmaf(v[u].w, s, o.w)};
-    }
-  }
-};
 
 // CL: a cluster of CTAs takes one (row, KV head, pass).
 template <int DT, bool Q4, int HC, bool CL>
@@ -1260,10 +1156,14 @@ cudaError_t launch_window_attn(const WindowArgs& a, int dtype, bool q4, int sms,
   else e = dtype ? go(Int<1>{}, Bool<false>{}) : go(Int<0>{}, Bool<false>{});
   if (e != cudaSuccess) return e;
   *kernels = 1;
-  if (!whole) {
-    const int nw = sms * window_warps(q4, HC);
-    const int warps = merge_warps(a, nw, sms);
-    e = launch_pdl(hill_window_combine_kernel, dim3(a.H, a.B), dim3(warps * 32), 0, st, 0, a, HC, nw);
+  return launch_window_finish(a, whole ? 0 : sms * window_warps(q4, HC), sms, st, kernels);
+}
+
+cudaError_t launch_window_finish(const WindowArgs& a, int warps_in_all, int sms, cudaStream_t st, int* kernels) {
+  cudaError_t e = cudaSuccess;
+  if (warps_in_all > 0) {
+    const int warps = merge_warps(a, warps_in_all, sms);
+    e = launch_pdl(hill_window_combine_kernel, dim3(a.H, a.B), dim3(warps * 32), 0, st, 0, a, a.heads, warps_in_all);
     ++*kernels;
   }
   if (e != cudaSuccess || !a.accum) return e;

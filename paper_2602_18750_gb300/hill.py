@@ -12,7 +12,9 @@ Names follow the C ABI: :func:`hill_score`, :func:`hill_topk_select`,
 :func:`hill_evict_step_kvh`, :func:`hill_evict_step_begin`, :func:`hill_evict_step_begin_f8`,
 :func:`hill_evict_step_end`, :func:`hill_workspace_bytes`, :func:`hill_sync_status`; for a cache of bounded
 size :func:`hill_window_attn`, :func:`hill_window_attn_q4`, :func:`hill_cache_insert`, :func:`hill_cache_insert_q4`,
-:func:`hill_cache_read_q4`, :func:`hill_window_workspace_bytes`.
+:func:`hill_cache_read_q4`, :func:`hill_window_workspace_bytes`; for prompts :func:`hill_prompt_attn`,
+:func:`hill_prompt_importance`; for a cache in pages :func:`hill_paged_attn`, :func:`hill_paged_write`,
+:func:`hill_paged_read`.
 """
 from __future__ import annotations
 
@@ -68,6 +70,29 @@ class hill_new_rows(ctypes.Structure):
 _pack_rows = struct.Struct("@PPqqqqqqiPP").pack
 assert struct.calcsize("@PPqqqqqqiPP") == ctypes.sizeof(hill_new_rows)
 
+class hill_packed(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "num_q_heads", "num_kv_heads", "head_dim", "dtype", "q_rows", "k_rows")] + [
+        (n, ctypes.c_int64) for n in ("q_st", "q_sh", "k_st", "k_sh", "v_st", "v_sh")]
+
+
+class hill_pages(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("table", ctypes.c_void_p),
+        ("pages", ctypes.c_int32), ("page", ctypes.c_int32), ("cols", ctypes.c_int32),
+    ]
+
+
+class hill_rows(ctypes.Structure):
+    _fields_ = [
+        ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("k_st", ctypes.c_int64), ("k_sh", ctypes.c_int64), ("v_st", ctypes.c_int64), ("v_sh", ctypes.c_int64),
+        ("rows", ctypes.c_int32),
+    ]
+
+
+_pack_packed_rows = struct.Struct("@PPqqqqi4x").pack
+assert struct.calcsize("@PPqqqqi4x") == ctypes.sizeof(hill_rows)
+
 _lib = None
 
 
@@ -108,6 +133,14 @@ def load(path: str | None = None) -> ctypes.CDLL:
     lib.hill_cache_insert.argtypes = [D, P, P, P, P, P, P, I32, I32, I32, P, P]
     lib.hill_cache_insert_q4.argtypes = [D, P, P, P, P, P, P, P, I32, I32, I32, P, P]
     lib.hill_cache_read_q4.argtypes = [D, P, P, P, P, P, I32, P, P, P]
+    K, G = ctypes.POINTER(hill_packed), ctypes.POINTER(hill_pages)
+    lib.hill_prompt_workspace_bytes.argtypes = [K]
+    lib.hill_prompt_workspace_bytes.restype = SZ
+    lib.hill_prompt_attn.argtypes = [K, P, P, P, P, P, I32, I32, P, P, P]
+    lib.hill_prompt_importance.argtypes = [K, P, P, P, P, P, I32, I32, I32, I32, P, I32, P, SZ, P]
+    lib.hill_paged_attn.argtypes = [D, P, G, P, I32, I32, I32, P, P, P, SZ, P]
+    lib.hill_paged_write.argtypes = [D, G, P, P, P, P]   # (the third: a hill_rows, by reference or packed)
+    lib.hill_paged_read.argtypes = [D, G, P, P, I32, P, P, P]
     lib.hill_sync_status.argtypes = [P]
     lib.hill_status_string.argtypes = [I32]
     lib.hill_status_string.restype = ctypes.c_char_p
@@ -117,7 +150,8 @@ def load(path: str | None = None) -> ctypes.CDLL:
                  "hill_topk_select_bkp", "hill_evict_step_bkp", "hill_quantize_k", "hill_score_f8",
                  "hill_evict_step_f8", "hill_evict_step_kvh", "hill_evict_step_begin", "hill_evict_step_begin_f8",
                  "hill_evict_step_end", "hill_selftest_wait", "hill_sync_status", "hill_window_attn",
-                 "hill_window_attn_q4", "hill_cache_insert", "hill_cache_insert_q4", "hill_cache_read_q4"):
+                 "hill_window_attn_q4", "hill_cache_insert", "hill_cache_insert_q4", "hill_cache_read_q4",
+                 "hill_prompt_attn", "hill_prompt_importance", "hill_paged_attn", "hill_paged_write", "hill_paged_read"):
         getattr(lib, name).restype = I32
     _lib = lib
     return lib
@@ -438,6 +472,169 @@ def hill_cache_read_q4(desc, k4, v4, params, row_begin, row_end, max_rows, k_cac
                                      _typed(row_begin, _I32, "row_begin"),
                                      _typed(row_end, _I32, "row_end"), int(max_rows), _ptr(k_cache),
                                      _ptr(v_cache), _stream(stream)), "hill_cache_read_q4")
+
+
+_DTYPES = {torch.float16: HILL_F16, torch.bfloat16: HILL_BF16}
+
+
+def _dtype_of(desc):
+    return torch.bfloat16 if desc.dtype else torch.float16
+
+
+def make_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, batch: int) -> hill_packed:
+    """Descriptor of packed prompts: q [q_rows][H][d], k and v [k_rows][Hkv][d] (any strides of rows and heads)."""
+    if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape or k.shape[2] != q.shape[2]:
+        raise ValueError(f"packed rows must be [rows][heads][d], K and V alike; got q {tuple(q.shape)}, K {tuple(k.shape)}, "
+                         f"V {tuple(v.shape)}")
+    if q.dtype not in _DTYPES or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise ValueError(f"q, K and V must share fp16 or bf16; got {q.dtype}, {k.dtype}, {v.dtype}")
+    if q.stride(2) != 1 or k.stride(2) != 1 or v.stride(2) != 1:
+        raise ValueError("head dimension must be contiguous")
+    return hill_packed(int(batch), q.shape[1], k.shape[1], q.shape[2], _DTYPES[q.dtype], q.shape[0], k.shape[0],
+                       q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+
+
+def hill_prompt_workspace_bytes(desc: hill_packed) -> int:
+    return int(load().hill_prompt_workspace_bytes(ctypes.byref(desc)))
+
+
+def alloc_prompt_workspace(desc: hill_packed, device="cuda") -> torch.Tensor:
+    n = hill_prompt_workspace_bytes(desc)
+    if n == 0:
+        raise HillError(HILL_ERR_INVALID_ARG, "hill_prompt_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _packed_rows(t, dtype, rows, heads, st, sh, what: str):
+    """The pointer of packed rows that a descriptor was made for."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype != dtype or t.shape != (rows, heads, 128) or (t.numel() and t.stride() != (st, sh, 1)):
+        raise ValueError(f"{what} must be [{rows}][{heads}][128] of {dtype}, strides ({st}, {sh}, 1), as the descriptor has "
+                         f"it; got {tuple(t.shape)}, {t.dtype}, strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _starts(t, batch, what: str):
+    p = _typed(t, _I32, what)
+    if p is not t and t.numel() != batch + 1:
+        raise ValueError(f"{what} must be [{batch + 1}], got {tuple(t.shape)}")
+    return p
+
+
+def hill_prompt_attn(desc, q, k, v, q_start, k_start, sinks, window, out, lse=None, stream=None) -> None:
+    """Causal attention over packed prompts into out (desc's type); lse: the log of every query's sum of exponentials."""
+    T, dt, B = desc.q_rows, _dtype_of(desc), desc.batch
+    op = _typed(out, dt, "out")
+    if op is not out and out.shape != (T, desc.num_q_heads, desc.head_dim):
+        raise ValueError(f"out must be [{T}][{desc.num_q_heads}][{desc.head_dim}], got {tuple(out.shape)}")
+    lp = _typed(lse, _F32, "lse")
+    if lp is not lse and lse.shape != (T, desc.num_q_heads):
+        raise ValueError(f"lse must be [{T}][{desc.num_q_heads}], got {tuple(lse.shape)}")
+    _check(load().hill_prompt_attn(ctypes.byref(desc),
+                                   _packed_rows(q, dt, T, desc.num_q_heads, desc.q_st, desc.q_sh, "q"),
+                                   _packed_rows(k, dt, desc.k_rows, desc.num_kv_heads, desc.k_st, desc.k_sh, "K"),
+                                   _packed_rows(v, dt, desc.k_rows, desc.num_kv_heads, desc.v_st, desc.v_sh, "V"),
+                                   _starts(q_start, B, "q_start"), _starts(k_start, B, "k_start"), int(sinks), int(window),
+                                   op, lp, _stream(stream)), "hill_prompt_attn")
+
+
+def hill_prompt_importance(desc, q, k, lse, q_start, k_start, sinks, window, newest, accum, kvh=False, ws=None,
+                           stream=None) -> None:
+    """accum [B][cap] (kvh: [B][Hkv][cap]) += the weights that the prompts' tokens receive from the newest queries."""
+    wp, wn = _ws(ws)
+    T, dt, B = desc.q_rows, _dtype_of(desc), desc.batch
+    lp = _typed(lse, _F32, "lse")
+    if lse.shape != (T, desc.num_q_heads):
+        raise ValueError(f"lse must be [{T}][{desc.num_q_heads}], got {tuple(lse.shape)}")
+    ap, rows = _typed(accum, _F32, "accum"), (B, desc.num_kv_heads) if kvh else (B,)
+    if accum.shape[:-1] != rows:
+        raise ValueError(f"accum must be {list(rows)}[cap], got {tuple(accum.shape)}")
+    _check(load().hill_prompt_importance(ctypes.byref(desc),
+                                         _packed_rows(q, dt, T, desc.num_q_heads, desc.q_st, desc.q_sh, "q"),
+                                         _packed_rows(k, dt, desc.k_rows, desc.num_kv_heads, desc.k_st, desc.k_sh, "K"),
+                                         lp, _starts(q_start, B, "q_start"), _starts(k_start, B, "k_start"), int(sinks),
+                                         int(window), int(newest), int(bool(kvh)), ap, accum.shape[-1], wp, wn,
+                                         _stream(stream)), "hill_prompt_importance")
+
+
+def make_pages(k_pool: torch.Tensor, v_pool: torch.Tensor, table: torch.Tensor, scales: torch.Tensor | None = None) -> hill_pages:
+    """A cache in pages: pools [pages][Hkv][page][d] in 16 bits, or E4M3 codes with scales [pages][Hkv][page][2], and
+    the page table [B][cols].  The handle keeps the tensors alive; their contents may change under it."""
+    if k_pool.dim() != 4 or v_pool.shape != k_pool.shape or k_pool.shape[3] != 128 or v_pool.dtype != k_pool.dtype:
+        raise ValueError(f"pools must be [pages][Hkv][page][128], K and V alike; got {tuple(k_pool.shape)} of {k_pool.dtype}, "
+                         f"{tuple(v_pool.shape)} of {v_pool.dtype}")
+    if not k_pool.is_contiguous() or not v_pool.is_contiguous():
+        raise ValueError("pools must be contiguous")
+    if scales is None:
+        if k_pool.dtype not in _DTYPES:
+            raise ValueError(f"pools without scales must be fp16 or bf16, got {k_pool.dtype}")
+    else:
+        if k_pool.dtype not in (torch.float8_e4m3fn, torch.uint8):
+            raise ValueError(f"pools with scales must hold E4M3 codes, got {k_pool.dtype}")
+        if scales.shape != (*k_pool.shape[:3], 2):
+            raise ValueError(f"scales must be {[*k_pool.shape[:3], 2]}, got {tuple(scales.shape)}")
+    if table.dim() != 2:
+        raise ValueError(f"the table must be [B][cols], got {tuple(table.shape)}")
+    p = hill_pages(k_pool.data_ptr(), v_pool.data_ptr(), _typed(scales, _F32, "scales"), _typed(table, _I32, "the table"),
+                   k_pool.shape[0], k_pool.shape[2], table.shape[1])
+    p.tensors = (k_pool, v_pool, table, scales)
+    p.kv_heads, p.batch, p.dtype = k_pool.shape[1], table.shape[0], None if scales is not None else k_pool.dtype
+    return p
+
+
+def _fits(desc, pages) -> None:
+    if desc.num_kv_heads != pages.kv_heads or desc.batch != pages.batch or (pages.dtype and pages.dtype != _dtype_of(desc)):
+        raise ValueError(f"pages of {pages.batch} sequences, {pages.kv_heads} KV heads{f', {pages.dtype}' if pages.dtype else ''} "
+                         f"do not fit a descriptor of {desc.batch}, {desc.num_kv_heads}, {_dtype_of(desc)}")
+
+
+def make_desc_paged(q: torch.Tensor, pages: hill_pages) -> hill_desc:
+    """Descriptor from q [B][H][d] and a cache in pages; its capacity is what the table covers."""
+    B, H, d = q.shape
+    if q.stride(-1) != 1 or d != 128:
+        raise ValueError("head dimension must be 128, contiguous")
+    if q.dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {q.dtype}")
+    desc = hill_desc(B, H, pages.kv_heads, d, pages.cols * pages.page, _DTYPES[q.dtype], q.stride(0), q.stride(1))
+    _fits(desc, pages)
+    return desc
+
+
+def hill_paged_attn(desc, q, pages, lens, sinks, window, out, accum=None, kvh=False, ws=None, stream=None) -> None:
+    """hill_window_attn over a cache in pages."""
+    _fits(desc, pages)
+    if not isinstance(q, int) and q.dtype != _dtype_of(desc):
+        raise ValueError(f"q must be {_dtype_of(desc)}, got {q.dtype}")
+    wp, wn = _ws(ws)
+    _check(load().hill_paged_attn(desc, _ptr(q), pages, _typed(lens, _I32, "lens"), int(sinks), int(window), 1 if kvh else 0,
+                                  _typed(accum, _F32, "accum"), _typed(out, _F32, "out"), wp, wn, _stream(stream)),
+           "hill_paged_attn")
+
+
+def hill_paged_write(desc, pages, k_new, v_new, starts, begin, stream=None) -> None:
+    """New rows [rows][Hkv][d] of several sequences into their pages; E4M3 caches quantise them."""
+    _fits(desc, pages)
+    shape, dt = k_new.shape, _dtype_of(desc)
+    if len(shape) != 3 or v_new.shape != shape or shape[1] != pages.kv_heads or shape[2] != 128 or k_new.dtype != dt or v_new.dtype != dt:
+        raise ValueError(f"new rows must be [rows][{pages.kv_heads}][128] of {dt}, K and V alike; got {tuple(shape)} of "
+                         f"{k_new.dtype}, {tuple(v_new.shape)} of {v_new.dtype}")
+    (kt, kh, k1), (vt, vh, v1) = k_new.stride(), v_new.stride()
+    if k1 != 1 or v1 != 1:
+        raise ValueError("head dimension must be contiguous")
+    b = _typed(begin, _I32, "begin")
+    if b is not begin and begin.numel() != desc.batch:
+        raise ValueError(f"begin must be [{desc.batch}], got {tuple(begin.shape)}")
+    rows = _pack_packed_rows(k_new.data_ptr(), v_new.data_ptr(), kt, kh, vt, vh, shape[0])
+    _check(load().hill_paged_write(desc, pages, rows, _starts(starts, desc.batch, "starts"), b, _stream(stream)),
+           "hill_paged_write")
+
+
+def hill_paged_read(desc, pages, row_begin, row_end, max_rows, k_cache, v_cache, stream=None) -> None:
+    """What positions [row_begin, row_end) of a cache in pages stand for, into 16-bit caches."""
+    _fits(desc, pages)
+    _check(load().hill_paged_read(desc, pages, _typed(row_begin, _I32, "row_begin"), _typed(row_end, _I32, "row_end"),
+                                  int(max_rows), _ptr(k_cache), _ptr(v_cache), _stream(stream)), "hill_paged_read")
 
 
 def hill_selftest_wait(limit_us: int, stream=None) -> None:
