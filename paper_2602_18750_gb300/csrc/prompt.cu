@@ -1,63 +1,454 @@
-// prompt.cu -- causal attention over packed prompts (Eq. 1 for every query of a prompt): one warp per
-// (query row, query head), a lane four channels, the running maximum and sum of the softmax in one pass
-// over the keys.
+// prompt.cu -- causal attention over packed prompts (Eq. 1 for every query of a prompt) on the 5th-generation
+// tensor cores.
+//
+// A unit is two tiles of 128 query rows of one KV head -- a row is a (token, query head of the group), token by
+// token, so the heads of a group share each key tile -- and walks the 128-key tiles that its rows see: those of the
+// sinks, then those of the window up to the diagonal.  One CTA per unit, 12 warps:
+//
+//   softmax   (warps 0-3, 4-7: a tile each, a thread per row) reads S = Q K^T from tensor memory, forms p = 2^(z - m)
+//             and puts it back there in the type of V, over S;
+//   loads     (warp 8) the Q tiles once, K and V tiles in a ring, by TMA (128-byte swizzle);
+//   products  (warp 9) one thread issues S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory,
+//             V with the head dimension contiguous).  The tiles take turns: while one's softmax runs, the tensor
+//             cores have the other's P V and next S;
+//   checks    (warps 10, 11) of V tiles that some row sees only a part of: rows of V that are not finite.
+//
+// Tensor memory holds S and O of both tiles, 4 x 128 columns, all there is.
+//
+// The running maximum m of a row is set 7 below its largest logit (base 2) and raised only when the weights of a
+// tile sum to more than 2^15: no maximum is searched for, and O is not rescaled, until then.  Since S of a tile is
+// complete only after the P V before it, a thread that holds S may rescale O.  The sums l and O are float32; the only
+// rounding to fewer bits is that of p, to fp16 or bf16, half a step of the type (weights below 2^-14 in fp16 keep an
+// absolute 2^-25, which is 2^-32 of the largest weight or less).
+//
+// A hidden key has p = 0, and a hidden value must not reach O by 0 * NaN.  In tiles that some row does not see whole, rows
+// of V that are not finite are set to zero in shared memory before the product, and the rows that see them add
+// p v themselves.
 #include "prompt_common.cuh"
+#include "tc_common.cuh"
 
 namespace hill {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kRows = 128, kKeys = 128, kTiles = 2;
+constexpr int kStages = 5;                       // ring of K and V tiles
+constexpr int kHalf = kKeys * 128;               // 64 dims of 128 rows
+constexpr int kTileBytes = 2 * kHalf;
+constexpr int kMasks = 4;                        // ring of the checks' results
+constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarp = kSoftmaxWarps, kMmaWarp = kLoadWarp + 1, kCheckWarp = kMmaWarp + 1;
+constexpr int kThreads = (kCheckWarp + 2) * 32;
 
-template <int DT>
-__device__ __forceinline__ float4 load4(const uint16_t* p) {
-  const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-  const float2 x = unpack2<DT>(v.x), y = unpack2<DT>(v.y);
-  return float4{x.x, x.y, y.x, y.y};
-}
+constexpr int kOffRing = kTiles * kTileBytes;
+constexpr int kOffBars = kOffRing + kStages * kTileBytes;
+// barriers: Q; ring full, empty; S full, P ready, O done of each tile; checks
+constexpr int kBQ = 0, kBFull = 1, kBEmpty = kBFull + kStages, kBS = kBEmpty + kStages, kBP = kBS + kTiles, kBO = kBP + kTiles,
+              kBCheck = kBO + kTiles, kBars = kBCheck + kMasks;
+constexpr int kOffMasks = kOffBars + ((kBars * 8 + 15) & ~15);
+constexpr int kOffMisc = kOffMasks + kMasks * 16;   // tensor memory address, abort flag, unit
+constexpr int kSmem = kOffMisc + 16 + 1024;
+static_assert(kSmem <= 232448, "shared memory");
 
-template <int DT>
-__global__ void __launch_bounds__(kWarps * 32) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a) {
-  const int lane = threadIdx.x & 31, h = blockIdx.y, g = h / a.G;
-  pdl_wait();
-  if (blockIdx.x == 0 && h == 0)   // every sequence's offsets are looked at once
-    for (int b = threadIdx.x; b < a.B; b += kWarps * 32) seq_at(a, b);
-  const int t = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (t >= a.q_rows) return;
-  int b = 0;
-  while (b < a.B && a.q_start[b + 1] <= t) ++b;
-  if (b == a.B || t < a.q_start[b]) return;
-  const Seq s = seq_at(a, b);
-  const int pos = t - s.q0 + s.shift();
-  const auto* K = static_cast<const uint16_t*>(a.k) + g * a.k_sh + 4 * lane;
-  const auto* V = static_cast<const uint16_t*>(a.v) + g * a.v_sh + 4 * lane;
-  const float4 q = load4<DT>(static_cast<const uint16_t*>(a.q) + t * a.q_st + h * a.q_sh + 4 * lane);
-  float m = kNegHuge, l = 0.f;
-  float4 o{0.f, 0.f, 0.f, 0.f};
-  bool any = false;
-  for (int j = 0; j <= min(pos, s.m - 1); ++j) {
-    if (!sees(a, pos, j)) continue;
-    any = true;
-    const float4 k = load4<DT>(K + (s.k0 + j) * a.k_st), v = load4<DT>(V + (s.k0 + j) * a.v_st);
-    const float z = warp_sum(q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w) * kLog2eInvSqrtD;
-    const float mn = fmaxf(m, z), f = ex2(m - mn), p = ex2(z - mn);
-    m = mn;
-    l = l * f + p;
-    o = float4{o.x * f + p * v.x, o.y * f + p * v.y, o.z * f + p * v.z, o.w * f + p * v.w};
+constexpr uint32_t kColS = 0, kColO = kTiles * kKeys, kCols = 512;
+
+// What a unit's rows see, in key tiles.
+struct Plan {
+  int first[kTiles], last[kTiles];   // positions of a tile's first and last token (last < first: no such tile)
+  int sinks, window, nsink, wfirst, count;
+  __device__ __forceinline__ int key(int i) const { return kKeys * (i < nsink ? i : wfirst + i - nsink); }
+  __device__ __forceinline__ bool active(int t, int j0) const {
+    return first[t] <= last[t] && j0 <= last[t] && (j0 < sinks || j0 + kKeys - 1 > first[t] - window);
   }
-  const float inv = any ? 1.f / l : 0.f;
-  const int64_t at = (int64_t)t * a.H + h;
-  reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at * kHeadDim)[lane] =
-      uint2{pack2<DT>(o.x * inv, o.y * inv), pack2<DT>(o.z * inv, o.w * inv)};
-  if (a.lse && lane == 0) a.lse[at] = any ? m * 0.6931471805599453f + logf(l) : -INFINITY;
+  __device__ __forceinline__ bool full(int t, int j0) const {
+    const int j1 = j0 + kKeys - 1;
+    return j1 <= first[t] && (j1 < sinks || j0 > last[t] - window);
+  }
+  __device__ __forceinline__ bool partial(int j0) const {
+    bool p = false;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) p = p || (active(t, j0) && !full(t, j0));
+    return p;
+  }
+  __device__ __forceinline__ int last_active(int t) const {
+    int i = count - 1;
+    while (i >= 0 && !active(t, key(i))) --i;
+    return i;
+  }
+};
+
+__device__ __forceinline__ uint32_t bits_to(int x) { return x < 0 ? 0u : (x >= 31 ? ~0u : (2u << x) - 1u); }   // 0 .. x
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units) {
+  extern __shared__ unsigned char psm_raw[];
+  const uint32_t base = (smem_addr(psm_raw) + 1023u) & ~1023u;
+  unsigned char* const mem = psm_raw + (base - smem_addr(psm_raw));
+  uint32_t* const masks = reinterpret_cast<uint32_t*>(mem + kOffMasks);
+  volatile int* const misc = reinterpret_cast<int*>(mem + kOffMisc);   // 0: tensor memory, 1: abort, 2: sequence, 3: unit in it
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  auto bar = [&](int i) { return base + kOffBars + (uint32_t)(i * 8); };
+  const int gp = blockIdx.x / units, u = blockIdx.x - gp * units, g = gp / a.passes, pass = gp - g * a.passes;
+
+  if (warp == 0) {
+    pdl_wait();
+    // the unit's sequence: 2 * q_tokens tokens to a unit
+    int seq = -1, in_seq = 0, before = 0;
+    for (int b0 = 0; b0 < a.B && seq < 0; b0 += 32) {
+      const int b = b0 + lane;
+      const int mine = b < a.B ? (seq_at(a, b).n + 2 * a.q_tokens - 1) / (2 * a.q_tokens) : 0;
+      int inc = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      const unsigned past = __ballot_sync(0xffffffffu, before + inc > u);
+      if (past) {
+        const int at = __ffs(past) - 1;
+        seq = b0 + at;
+        // the last tokens of a sequence, which see the most keys, go first
+        in_seq = before + __shfl_sync(0xffffffffu, inc, at) - 1 - u;
+      }
+      before += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) {
+      misc[1] = 0;
+      misc[2] = seq;
+      misc[3] = in_seq;
+    }
+  } else if (warp == kLoadWarp && lane == 0) {
+    mbar_init(bar(kBQ), 1);
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(bar(kBFull + i), 1);
+      mbar_init(bar(kBEmpty + i), 1);
+    }
+    for (int t = 0; t < kTiles; ++t) {
+      mbar_init(bar(kBS + t), 1);
+      mbar_init(bar(kBP + t), 4);
+      mbar_init(bar(kBO + t), 1);
+    }
+    for (int i = 0; i < kMasks; ++i) mbar_init(bar(kBCheck + i), 2);
+    fence_barrier_init();
+    prefetch_tmap(&a.qmap);
+    prefetch_tmap(&a.kmap);
+    prefetch_tmap(&a.vmap);
+  } else if (warp == kMmaWarp) {
+    tmem_alloc(base + kOffMisc, kCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_wait();
+  const uint32_t tmem = (uint32_t)misc[0];
+  const int b = misc[2];
+  const Seq s = b >= 0 ? seq_at(a, b) : Seq{0, 0, 0, 0};
+  const int token0 = misc[3] * 2 * a.q_tokens, shift = s.shift();
+  Plan plan;
+  plan.sinks = a.sinks;
+  plan.window = a.window;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) {
+    plan.first[t] = token0 + t * a.q_tokens + shift;
+    plan.last[t] = min(token0 + (t + 1) * a.q_tokens, s.n) - 1 + shift;
+  }
+  const int lowest = plan.first[0], highest = max(plan.last[0], plan.last[1]);
+  plan.wfirst = max(0, lowest - a.window + 1) / kKeys;
+  const int end = highest < 0 ? 0 : highest / kKeys + 1;   // key tiles up to the diagonal
+  plan.nsink = min(min((a.sinks + kKeys - 1) / kKeys, plan.wfirst), end);
+  plan.count = b >= 0 ? plan.nsink + max(0, end - plan.wfirst) : 0;
+
+  auto wait = [&](int i, uint32_t parity) {
+    if (misc[1]) return false;
+    if (mbar_wait(bar(i), parity, a.err)) return true;
+    misc[1] = 1;
+    return false;
+  };
+  auto ring = [&](int n) { return base + kOffRing + (uint32_t)((n % kStages) * kTileBytes); };   // n: 2 i for K, 2 i + 1 for V
+  auto full = [&](int n) { return wait(kBFull + n % kStages, (uint32_t)(n / kStages) & 1u); };
+
+  if (warp < kSoftmaxWarps) {
+    // ------------------------------------------------------------ softmax of a tile
+    const int t = warp >> 2;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = tmem + lanes + kColS + t * kKeys, to = tmem + lanes + kColO + t * kHeadDim;
+    const int row = (warp & 3) * 32 + lane, tok = row / a.q_heads, hg = pass * a.q_heads + row - tok * a.q_heads;
+    const int i_tok = token0 + t * a.q_tokens + tok;
+    const bool valid = b >= 0 && tok < a.q_tokens && hg < a.G && i_tok < s.n;
+    const int pos = i_tok + shift;
+    const float2 c2 = both(valid ? kLog2eInvSqrtD : 0.f);   // (a row that is none has logits of 0)
+    float m = kNegHuge, l = 0.f;
+    {
+      uint32_t zero[32];
+#pragma unroll
+      for (int i = 0; i < 32; ++i) zero[i] = 0u;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tc_st32(to + 32 * c, zero);
+      tc_wait_st();
+    }
+    int n = 0, checked = 0;
+    bool ok = true;
+    for (int i = 0; i < plan.count && ok; ++i) {
+      const int j0 = plan.key(i);
+      const bool part = plan.partial(j0);
+      if (!plan.active(t, j0)) {
+        checked += part;
+        continue;
+      }
+      const bool whole = plan.full(t, j0);
+      // the keys that the row sees, as bits
+      uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};
+      if (!whole) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          vis[w] = valid ? bits_to(pos - j0 - 32 * w) & (bits_to(a.sinks - 1 - j0 - 32 * w) | ~bits_to(pos - j0 - a.window - 32 * w))
+                         : 0u;
+      }
+      ok = __all_sync(0xffffffffu, wait(kBS + t, (uint32_t)n & 1u));
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t p[64];
+      float sum;
+      uint32_t sv[2][32];
+      auto weights = [&](auto masked_tag) {
+        constexpr bool kMasked = decltype(masked_tag)::value;
+        const float2 m2 = both(-m);
+        float2 sums[2] = {both(0.f), both(0.f)};
+        tc_ld32(ts, sv[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tc_landed(sv[c & 1]);
+          if (c < 3) tc_ld32(ts + 32 * (c + 1), sv[(c + 1) & 1]);
+#pragma unroll
+          for (int k = 0; k < 32; k += 2) {
+            float2 z{__uint_as_float(sv[c & 1][k]), __uint_as_float(sv[c & 1][k + 1])};
+            if (kMasked) {
+              z.x = (vis[c] >> k) & 1u ? z.x : -INFINITY;
+              z.y = (vis[c] >> (k + 1)) & 1u ? z.y : -INFINITY;
+            }
+            const float2 x = fma2(z, c2, m2);
+            const float2 e{ex2(x.x), ex2(x.y)};
+            sums[(k >> 1) & 1] = add2(sums[(k >> 1) & 1], e);
+            p[c * 16 + (k >> 1)] = pack2<DT>(e.x, e.y);
+          }
+        }
+        const float2 s2 = add2(sums[0], sums[1]);
+        sum = s2.x + s2.y;
+      };
+      for (int again = 0;; ++again) {
+        if (whole) weights(std::false_type{});
+        else weights(std::true_type{});
+        if (again || !__any_sync(0xffffffffu, sum > 32768.f)) break;
+        // a weight may be past 2^15: the maximum is raised, what the old one has given shrinks
+        float top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tc_ld32(ts + 32 * c, sv[0]);
+          tc_landed(sv[0]);
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if ((vis[c] >> k) & 1u) top = fmaxf(top, __uint_as_float(sv[0][k]) * c2.x);
+        }
+        // (a row whose weights are within keeps its maximum: what one row sees changes no bit of another's)
+        const float mn = sum > 32768.f ? fmaxf(m, top - 7.f) : m, f = ex2(m - mn);
+        m = mn;
+        l *= f;
+        for (int c = 0; c < 4 && n > 0; ++c) {
+          tc_ld32(to + 32 * c, sv[0]);
+          tc_landed(sv[0]);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) sv[0][k] = __float_as_uint(__uint_as_float(sv[0][k]) * f);
+          tc_st32(to + 32 * c, sv[0]);
+        }
+      }
+      l += sum;
+      tc_st32(ts, p);
+      tc_st32(ts + 32, p + 32);
+      tc_wait_st();
+      if (part) {
+        ok = __all_sync(0xffffffffu, wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u));
+        if (!ok) break;
+        for (int w = 0; w < 4; ++w) {
+          // values that are not finite: the rows that see them take p v
+          for (uint32_t bad = masks[(checked % kMasks) * 4 + w]; bad; bad &= bad - 1u) {
+            const int k = __ffs(bad) - 1;
+            const uint32_t two = tc_ld1(ts + 16 * w + (k >> 1));
+            const float2 pk = unpack2<DT>(two);
+            const bool see = (w == 0 ? vis[0] : w == 1 ? vis[1] : w == 2 ? vis[2] : vis[3]) >> k & 1u;
+            const float pw = k & 1 ? pk.y : pk.x;
+            const auto* v = static_cast<const uint16_t*>(a.v) + (int64_t)(s.k0 + j0 + 32 * w + k) * a.v_st + (int64_t)g * a.v_sh;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              tc_ld32(to + 32 * c, sv[0]);
+              tc_landed(sv[0]);
+#pragma unroll
+              for (int e = 0; e < 32; e += 2) {
+                const float2 x = unpack2<DT>(*reinterpret_cast<const uint32_t*>(v + 32 * c + e));
+                if (see && valid) {
+                  sv[0][e] = __float_as_uint(fmaf(pw, x.x, __uint_as_float(sv[0][e])));
+                  sv[0][e + 1] = __float_as_uint(fmaf(pw, x.y, __uint_as_float(sv[0][e + 1])));
+                }
+              }
+              tc_st32(to + 32 * c, sv[0]);
+            }
+            tc_wait_st();
+          }
+        }
+        ++checked;
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(kBP + t));
+      ++n;
+    }
+    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(kBO + t, 0u));
+    if (ok && b >= 0) {
+      tc_fence_after();
+      // does the row see anything?
+      const bool sees_any = pos >= 0 && (a.window > 0 || a.sinks > 0);
+      const float inv = sees_any ? 1.f / l : 0.f;
+      const int64_t at = (int64_t)(s.q0 + i_tok) * a.H + g * a.G + hg;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t sv[32];
+        tc_ld32(to + 32 * c, sv);
+        tc_landed(sv);
+        if (!valid) continue;
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * kHeadDim + 32 * c);
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          uint32_t w[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            w[x] = pack2<DT>(__uint_as_float(sv[e + 2 * x]) * inv, __uint_as_float(sv[e + 2 * x + 1]) * inv);
+          dst[e / 8] = uint4{w[0], w[1], w[2], w[3]};
+        }
+      }
+      if (a.lse && valid) a.lse[at] = sees_any ? fmaf(m, 0.69314718f, logf(l)) : -INFINITY;
+    }
+  } else if (warp == kLoadWarp) {
+    // ------------------------------------------------------------ loads
+    if (lane == 0 && plan.count > 0) {
+      const int tiles = plan.last[1] >= plan.first[1] ? 2 : 1;
+      const uint32_t q_bytes = (uint32_t)(a.q_heads * a.q_tokens * 128);
+      mbar_arrive_expect_tx(bar(kBQ), tiles * 2 * q_bytes);
+      for (int t = 0; t < tiles; ++t)
+        for (int h = 0; h < 2; ++h)
+          tma_tile_3d(base + t * kTileBytes + h * kHalf, &a.qmap, 64 * h, g * a.G + pass * a.q_heads,
+                      s.q0 + token0 + t * a.q_tokens, bar(kBQ));
+      int n = 0;
+      for (; n < 2 * plan.count; ++n) {
+        if (n >= kStages && !wait(kBEmpty + n % kStages, (uint32_t)(n / kStages - 1) & 1u)) break;
+        const uint32_t full_bar = bar(kBFull + n % kStages);
+        const void* map = n & 1 ? &a.vmap : &a.kmap;
+        mbar_arrive_expect_tx(full_bar, kTileBytes);
+        for (int h = 0; h < 2; ++h) tma_tile_3d(ring(n) + h * kHalf, map, 64 * h, g, s.k0 + plan.key(n >> 1), full_bar);
+      }
+      if (misc[1]) {   // what is under way has to land before the CTA goes
+        mbar_wait(bar(kBQ), 0u, a.err);
+        for (int x = max(0, n - kStages); x < n; ++x) mbar_wait(bar(kBFull + x % kStages), (uint32_t)(x / kStages) & 1u, a.err);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ------------------------------------------------------------ products
+    if (lane == 0 && plan.count > 0) {
+      constexpr uint32_t kIdescS = f16_idesc(DT, kRows, kKeys, false), kIdescO = f16_idesc(DT, kRows, kHeadDim, true);
+      const int last[kTiles] = {plan.last_active(0), plan.last_active(1)};
+      int n[kTiles] = {0, 0}, checked = 0;
+      bool ok = wait(kBQ, 0u);
+      for (int i = 0; i <= plan.count && ok; ++i) {
+        const int jv = i > 0 ? plan.key(i - 1) : 0, jk = i < plan.count ? plan.key(i) : 0;
+        if (i > 0) {
+          ok = full(2 * i - 1);
+          if (ok && plan.partial(jv)) {
+            ok = wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
+            ++checked;
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          if (ok && i > 0 && plan.active(t, jv)) {   // O += P V
+            ok = wait(kBP + t, (uint32_t)(n[t] - 1) & 1u);
+            if (ok) {
+              tc_fence_after();
+              const uint32_t vb = ring(2 * i - 1);
+#pragma unroll
+              for (int k = 0; k < kKeys / 16; ++k)
+                tc_mma_f16_ts(tmem + kColO + t * kHeadDim, tmem + kColS + t * kKeys + 8 * k,
+                              smem_desc_sw128_mn(vb + 2048 * k, kHalf), kIdescO, 1u);
+              if (i - 1 == last[t]) tc_commit(bar(kBO + t));
+            }
+          }
+          if (t == 0 && ok && i < plan.count) ok = full(2 * i);
+          if (ok && i < plan.count && plan.active(t, jk)) {   // S = Q K^T
+            tc_fence_after();
+            const uint32_t qb = base + t * kTileBytes, kb = ring(2 * i);
+#pragma unroll
+            for (int k = 0; k < kHeadDim / 16; ++k)
+              tc_mma_f16(tmem + kColS + t * kKeys, smem_desc_sw128(qb + (k >> 2) * kHalf + (k & 3) * 32),
+                         smem_desc_sw128(kb + (k >> 2) * kHalf + (k & 3) * 32), kIdescS, k > 0 ? 1u : 0u);
+            tc_commit(bar(kBS + t));
+            ++n[t];
+          }
+        }
+        if (ok && i > 0) tc_commit(bar(kBEmpty + (2 * i - 1) % kStages));
+        if (ok && i < plan.count) tc_commit(bar(kBEmpty + (2 * i) % kStages));
+      }
+      if (!ok) {   // products under way end before the tensor memory is released
+        tc_commit(bar(kBQ));
+        mbar_wait(bar(kBQ), 1u, a.err);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------ checks
+    int checked = 0;
+    bool ok = true;
+    for (int i = 0; i < plan.count && ok; ++i) {
+      // (every tile is waited for: the parity of a later use of a slot says nothing before the earlier one has landed)
+      ok = __all_sync(0xffffffffu, full(2 * i) && full(2 * i + 1));
+      if (!ok) break;
+      if (!plan.partial(plan.key(i))) continue;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int w = (warp - kCheckWarp) * 2 + e, r = 32 * w + lane;
+        bool bad = false;
+#pragma unroll 4
+        for (int c = 0; c < 16; ++c) {
+          const uint4 v = lds128(ring(2 * i + 1) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+          constexpr uint32_t kExp = DT == 0 ? 0x7c00u : 0x7f80u;
+#pragma unroll
+          for (int y = 0; y < 4; ++y) bad = bad || (x[y] & kExp) == kExp || ((x[y] >> 16) & kExp) == kExp;
+        }
+        const uint32_t mask = __ballot_sync(0xffffffffu, bad);
+        if (bad)
+          for (int c = 0; c < 16; ++c) sts128_zero(ring(2 * i + 1) + (c >> 3) * kHalf + r * 128 + (c & 7) * 16);
+        if (mask) fence_proxy_async();
+        if (lane == 0) masks[(checked % kMasks) * 4 + w] = mask;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(kBCheck + checked % kMasks));
+      ++checked;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, kCols);
+  }
 }
 
 }  // namespace
 
 cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels) {
   *kernels = 1;
-  const dim3 grid((a.q_rows + kWarps - 1) / kWarps, a.H);
-  return dtype ? launch_pdl(hill_prompt_attn_kernel<1>, grid, dim3(kWarps * 32), 0, st, 0, a)
-               : launch_pdl(hill_prompt_attn_kernel<0>, grid, dim3(kWarps * 32), 0, st, 0, a);
+  // units of all sequences, at most
+  const int units = a.q_rows / (2 * a.q_tokens) + a.B;
+  auto kern = dtype ? hill_prompt_attn_kernel<1> : hill_prompt_attn_kernel<0>;
+  static int cache[2][64] = {{0}};
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), kSmem, cache[dtype ? 1 : 0]);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kern, dim3((unsigned)units * a.Hkv * a.passes), dim3(kThreads), kSmem, st, 0, a, units);
 }
 
 }  // namespace hill
