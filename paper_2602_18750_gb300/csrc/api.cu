@@ -1283,9 +1283,17 @@ hill_status prompt_args(const hill_packed* d, const void* q, const void* k, cons
   return s;
 }
 
-size_t prompt_workspace(const hill_packed* d, int sms) {
-  const int splits = importance_splits(d->batch, d->num_kv_heads, d->k_rows, sms);
-  return align_up((size_t)splits * d->num_kv_heads * d->k_rows * sizeof(float)) + kAlign;
+// Workspace of hill_prompt_importance: totals, the blocks, the sums of their parts.
+struct PromptLayout {
+  size_t info, part, total;
+};
+PromptLayout prompt_layout(const hill_packed* d, int sms) {
+  const ImportanceSpace space = importance_space(d->batch, d->num_kv_heads, d->k_rows, sms);
+  PromptLayout L;
+  L.info = kAlign;
+  L.part = L.info + align_up(space.info);
+  L.total = L.part + align_up(space.part) + kAlign;
+  return L;
 }
 
 // 3-D map of a pool (head dimension, slot, page * Hkv + KV head), box = 128 bytes x group slots.
@@ -1375,7 +1383,7 @@ size_t hill_prompt_workspace_bytes(const hill_packed* desc) {
   if (check_packed(desc) != HILL_OK) return 0;
   DeviceInfo di;
   if (device_info(&di) != cudaSuccess) return 0;
-  return prompt_workspace(desc, di.sms);
+  return prompt_layout(desc, di.sms).total;
 }
 
 hill_status hill_prompt_importance(const hill_packed* desc, const void* q, const void* k, const float* lse,
@@ -1390,7 +1398,8 @@ hill_status hill_prompt_importance(const hill_packed* desc, const void* q, const
   if (!aligned16(q) || !aligned16(k)) return HILL_ERR_INVALID_ARG;
   DeviceInfo di;
   if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
-  if (!ws || ws_bytes < prompt_workspace(desc, di.sms)) return HILL_ERR_WORKSPACE;
+  const PromptLayout L = prompt_layout(desc, di.sms);
+  if (!ws || ws_bytes < L.total) return HILL_ERR_WORKSPACE;
   PromptArgs a{};
   s = prompt_args(desc, q, k, nullptr, q_start, k_start, sinks, window, &a);
   if (s != HILL_OK) return s;
@@ -1399,8 +1408,11 @@ hill_status hill_prompt_importance(const hill_packed* desc, const void* q, const
   a.accum = accum;
   a.cap = cap;
   a.kvh = kvh ? 1 : 0;
-  a.part = reinterpret_cast<float*>(ws_base(ws));
-  a.splits = importance_splits(desc->batch, desc->num_kv_heads, desc->k_rows, di.sms);
+  unsigned char* base = ws_base(ws);
+  a.totals = reinterpret_cast<int2*>(base);
+  a.tiles = reinterpret_cast<int64_t*>(base + sizeof(int2));
+  a.info = reinterpret_cast<BlockInfo*>(base + L.info);
+  a.part = reinterpret_cast<float*>(base + L.part);
   a.err = di.err;
   int kernels = 0;
   const cudaError_t e = launch_prompt_importance(a, desc->dtype, di.sms, static_cast<cudaStream_t>(stream), &kernels);

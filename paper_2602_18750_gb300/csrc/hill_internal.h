@@ -201,6 +201,8 @@ struct PagesArgs {
   unsigned* err;
 };
 
+struct BlockInfo;   // importance.cu
+
 // Prompts: packed rows of several sequences (prompt.cu, importance.cu).
 struct PromptArgs {
   CUtensorMap qmap, kmap, vmap;   // 3-D (head dimension, head, row), 128-byte swizzle; boxes of 64 dims x q_heads x
@@ -218,8 +220,11 @@ struct PromptArgs {
   float* lse;                     // [q_rows][H], or NULL; importance: read
   float* accum;                   // [B][cap], kvh: [B][Hkv][cap]
   int cap, kvh;
-  float* part;                    // importance: [splits][Hkv][k_rows] sums
-  int splits;
+  // importance: sums of parts of blocks; what each block is; their number and that of the parts; tiles in all
+  float* part;
+  BlockInfo* info;
+  int2* totals;
+  int64_t* tiles;
   unsigned* err;
 };
 
@@ -379,7 +384,10 @@ cudaError_t launch_paged_read(const PagesArgs& a, int dtype, int max_rows, cudaS
 cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels);
 
 // importance.cu
-int importance_splits(int B, int Hkv, int64_t k_rows, int sms);
+struct ImportanceSpace {   // bytes of workspace
+  size_t part, info;
+};
+ImportanceSpace importance_space(int B, int Hkv, int64_t k_rows, int sms);
 cudaError_t launch_prompt_importance(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels);
 
 // insert.cu

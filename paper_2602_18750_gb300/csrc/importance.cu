@@ -1,51 +1,432 @@
-// importance.cu -- the attention weights that a prompt's tokens receive, summed over its queries (Sec. 4.1 for
-// prompt tokens): one warp per (sequence, KV head or all, key), a lane four channels.
+// importance.cu -- the attention weights that a prompt's tokens receive, summed over its queries and query heads
+// (Sec. 4.1 for prompt tokens), on the 5th-generation tensor cores.
+//
+//   accum_j += sum over rows r = (query, head) of 2^(z_rj - lse_r log2 e)
+//
+// A block is 256 keys of one KV head, two tiles of 128.  S^T = K Q^T has the keys as lanes of tensor memory and 128 query
+// rows as columns, so the sum over queries stays inside a thread: it reads its key's 128 logits, subtracts the rows'
+// statistics (the same for all threads, from shared memory) and adds the exponentials.  A query row is a
+// (token, query head of the group), token by token.
+//
+// All (KV head, block, tile of 128 query rows) that a query of the block's sees form one list, dealt out to the CTAs
+// in equal runs (one CTA per SM), whatever the prompts' lengths.  A run covers a few blocks; the sums of the part of
+// block x that CTA c has go to segment x + c of the workspace: runs are in order, so no two parts share one.  A second
+// kernel adds a block's segments, and the KV heads, in a fixed order.
+//
+// 12 warps: sums (0-3, 4-7: a key tile each), loads (8: K of two blocks, Q tiles in a ring, by TMA), products (9: one
+// thread), statistics (10).  Tensor memory holds two S^T for each key tile, all 512 columns.
+#include <algorithm>
+#include <type_traits>
+
 #include "prompt_common.cuh"
+#include "tc_common.cuh"
 
 namespace hill {
+
+// What the second kernel needs of a block (of every KV head).
+struct BlockInfo {
+  int64_t before;   // tiles of the blocks before it
+  int tiles, b, j0, keys;
+};
+
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kRows = 128, kKeys = 128, kTiles = 2, kBlock = kTiles * kKeys;
+constexpr int kStages = 3, kStats = 3;           // rings of Q tiles and of their statistics
+constexpr int kHalf = 128 * 128, kTileBytes = 2 * kHalf;
+constexpr int kSumWarps = 4 * kTiles, kLoadWarp = kSumWarps, kMmaWarp = kLoadWarp + 1, kStatWarp = kMmaWarp + 1;
+constexpr int kWarps = 12, kThreads = kWarps * 32;
 
-template <int DT>
-__device__ __forceinline__ float4 load4(const uint16_t* p) {
-  const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-  const float2 x = unpack2<DT>(v.x), y = unpack2<DT>(v.y);
-  return float4{x.x, x.y, y.x, y.y};
+constexpr int kOffK = 0, kOffQ = 2 * kTiles * kTileBytes, kOffStats = kOffQ + kStages * kTileBytes;
+constexpr int kOffToken = kOffStats + kStats * kRows * 4;   // token of a row within its tile, one byte each
+constexpr int kOffBars = kOffToken + kRows;
+constexpr int kBKFull = 0, kBKEmpty = 2, kBQFull = 4, kBQEmpty = kBQFull + kStages, kBLFull = kBQEmpty + kStages,
+              kBLEmpty = kBLFull + kStats, kBSFull = kBLEmpty + kStats, kBSEmpty = kBSFull + 4, kBDone = kBSEmpty + 4,
+              kBars = kBDone + 1;
+constexpr int kOffMisc = kOffBars + kBars * 8;   // tensor memory address, abort flag
+constexpr int kSmem = kOffMisc + 16 + 1024;
+static_assert(kSmem <= 232448, "shared memory");
+
+// The queries that count for keys [j0, j0 + kBlock): the first of them, and how many tiles they make.
+__device__ __forceinline__ int block_tiles(const PromptArgs& a, const Seq& s, int j0, int& first) {
+  const int64_t shift = s.shift();
+  const int64_t lo = max((int64_t)max(0, s.n - a.newest), j0 - shift);
+  int64_t hi = s.n;
+  if (j0 >= a.sinks) hi = min(hi, (int64_t)j0 + kBlock - 1 + a.window - shift);
+  first = (int)min(lo, (int64_t)s.n);
+  return hi > lo ? (int)((hi - lo + a.q_tokens - 1) / a.q_tokens) * a.passes : 0;
 }
+__device__ __forceinline__ int seq_blocks(const PromptArgs& a, const Seq& s) { return (min(s.m, a.cap) + kBlock - 1) / kBlock; }
+
+// Where a CTA stands: tile x of `tiles` of block (g, blk), whose keys begin at j0 of sequence b.
+struct Cursor {
+  int g, blk, b, j0, x;
+};
 
 template <int DT>
-__global__ void __launch_bounds__(kWarps * 32) hill_prompt_importance_kernel(const __grid_constant__ PromptArgs a) {
-  const int lane = threadIdx.x & 31, b = blockIdx.z, row = blockIdx.y;
+__global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(const __grid_constant__ PromptArgs a) {
+  extern __shared__ unsigned char ism_raw[];
+  const uint32_t base = (smem_addr(ism_raw) + 1023u) & ~1023u;
+  unsigned char* const mem = ism_raw + (base - smem_addr(ism_raw));
+  volatile int* const misc = reinterpret_cast<int*>(mem + kOffMisc);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
+  auto bar = [&](int i) { return base + kOffBars + (uint32_t)(i * 8); };
+
+  if (warp == kLoadWarp && lane == 0) {
+    auto init = [&](int first, int n, int count) {
+      for (int i = 0; i < n; ++i) mbar_init(bar(first + i), count);
+    };
+    init(kBKFull, 2, 1);
+    init(kBKEmpty, 2, 1);
+    init(kBQFull, kStages, 1);
+    init(kBQEmpty, kStages, 1);
+    init(kBLFull, kStats, 1);
+    init(kBLEmpty, kStats, kSumWarps);
+    init(kBSFull, 4, 1);
+    init(kBSEmpty, 4, 4);
+    init(kBDone, 1, 1);
+    misc[1] = 0;
+    fence_barrier_init();
+    prefetch_tmap(&a.qmap);
+    prefetch_tmap(&a.kmap);
+  } else if (warp == kMmaWarp) {
+    tmem_alloc(base + kOffMisc, 512);
+    tmem_relinquish();
+  }
   pdl_wait();
-  const Seq s = seq_at(a, b);
-  const int j = blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (s.m > a.cap && j == 0 && lane == 0) raise_error(a.err, kErrDevArg);
-  if (j >= min(s.m, a.cap)) return;
-  float sum = 0.f;
-  for (int g = a.kvh ? row : 0; g < (a.kvh ? row + 1 : a.Hkv); ++g) {
-    const float4 k = load4<DT>(static_cast<const uint16_t*>(a.k) + (s.k0 + j) * a.k_st + g * a.k_sh + 4 * lane);
-    for (int i = max(0, s.n - a.newest); i < s.n; ++i) {
-      if (!sees(a, i + s.shift(), j)) continue;
-      for (int h = g * a.G; h < (g + 1) * a.G; ++h) {
-        const float4 q = load4<DT>(static_cast<const uint16_t*>(a.q) + (s.q0 + i) * a.q_st + h * a.q_sh + 4 * lane);
-        const float z = warp_sum(q.x * k.x + q.y * k.y + q.z * k.z + q.w * k.w) * kLog2eInvSqrtD;
-        sum += ex2(z - a.lse[(int64_t)(s.q0 + i) * a.H + h] * 1.4426950408889634f);
+
+  // ------------------------------------------------------------ the list
+  // (the tables of the set-up lie in the rings)
+  int* const first_blk = reinterpret_cast<int*>(mem);                       // [B + 1] first block of each sequence
+  int64_t* const sums = reinterpret_cast<int64_t*>(mem + 4096);             // [warps]
+  Cursor* const start = reinterpret_cast<Cursor*>(mem + 4096 + 256);
+  if (warp == 0) {
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+      const int b = b0 + lane;
+      int mine = 0;
+      if (b < a.B) {
+        const Seq s = seq_at(a, b);
+        if (s.m > a.cap && blockIdx.x == 0) raise_error(a.err, kErrDevArg);
+        mine = seq_blocks(a, s);
       }
+      int inc = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += y;
+      }
+      if (b < a.B) first_blk[b] = before + inc - mine;
+      before += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    if (lane == 0) first_blk[a.B] = before;
+  }
+  __syncthreads();
+  // every thread counts the tiles of a run of blocks
+  const int nblk = first_blk[a.B], each = (nblk + kThreads - 1) / kThreads;
+  const int blk0 = min(nblk, tid * each), blk1 = min(nblk, blk0 + each);
+  int b0 = 0;
+  if (blk0 < blk1) {   // the last sequence that begins at or before blk0
+    int hi = a.B - 1;
+    while (b0 < hi) {
+      const int mid = (b0 + hi + 1) >> 1;
+      if (first_blk[mid] <= blk0) b0 = mid;
+      else hi = mid - 1;
     }
   }
-  if (lane == 0) a.accum[((int64_t)b * (a.kvh ? a.Hkv : 1) + row) * a.cap + j] += sum;
+  int64_t mine = 0;
+  for (int blk = blk0, b = b0; blk < blk1; ++blk) {
+    while (first_blk[b + 1] <= blk) ++b;
+    int first;
+    mine += block_tiles(a, seq_at(a, b), (blk - first_blk[b]) * kBlock, first);
+  }
+  int64_t inc = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t y = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += y;
+  }
+  if (lane == 31) sums[warp] = inc;
+  __syncthreads();
+  int64_t before = inc - mine, all = 0;
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += sums[w];
+    all += sums[w];
+  }
+  const int64_t total = all * a.Hkv, per = (total + gridDim.x - 1) / gridDim.x;
+  const int64_t w0 = min(total, blockIdx.x * per), w1 = min(total, w0 + per);
+  const int g0 = all ? (int)(w0 / all) : 0;
+  const int64_t at0 = w0 - g0 * all;
+  if (blk0 < blk1 && (blockIdx.x == 0 || (at0 >= before && at0 < before + mine))) {
+    int64_t at = before;
+    for (int blk = blk0, b = b0; blk < blk1; ++blk) {
+      while (first_blk[b + 1] <= blk) ++b;
+      const Seq s = seq_at(a, b);
+      const int j0 = (blk - first_blk[b]) * kBlock;
+      int first;
+      const int tiles = block_tiles(a, s, j0, first);
+      if (blockIdx.x == 0) a.info[blk] = BlockInfo{at, tiles, b, j0, min(min(s.m, a.cap) - j0, kBlock)};
+      if (at0 >= at && at0 < at + tiles) *start = Cursor{g0, blk, b, j0, (int)(at0 - at)};
+      at += tiles;
+    }
+  }
+  if (blockIdx.x == 0 && tid == 0) {
+    *a.totals = int2{nblk, (int)gridDim.x};
+    *a.tiles = all;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = (uint32_t)misc[0];
+  const Cursor begin = w0 < w1 ? *start : Cursor{};
+  __syncthreads();
+  // rows that no Q box covers hold zeros (weight 2^-inf); the rings change hands from here to the loads
+  const int box_rows = a.q_heads * a.q_tokens;
+  for (int i = tid; i < kStages * 2 * (kRows - box_rows) * 8; i += kThreads) {
+    const int per_tile = (kRows - box_rows) * 8, tile = i / per_tile, r = i - tile * per_tile;
+    sts128_zero(base + kOffQ + tile * kHalf + box_rows * 128 + r * 16);
+  }
+  if (tid < kRows) mem[kOffToken + tid] = (unsigned char)(tid / a.q_heads);
+  fence_proxy_async();
+  __syncthreads();
+
+  auto wait = [&](int i, uint32_t parity) {
+    if (misc[1]) return false;
+    if (mbar_wait(bar(i), parity, a.err)) return true;
+    misc[1] = 1;
+    return false;
+  };
+  // A walk over the CTA's parts of blocks: f(part, cursor, sequence, first query, tiles) -> go on?
+  auto walk = [&](auto&& f) {
+    Cursor c = begin;
+    int64_t left = w1 - w0;
+    for (int part = 0; left > 0; ++part) {
+      const Seq s = seq_at(a, c.b);
+      int first;
+      const int tiles = block_tiles(a, s, c.j0, first), n = (int)min((int64_t)(tiles - c.x), left);
+      if (!f(part, c, s, first, n)) return;
+      left -= n;
+      if (left == 0) return;
+      // the next block with tiles
+      c.x = 0;
+      int next = 0;
+      do {
+        ++c.blk;
+        c.j0 += kBlock;
+        while (c.j0 >= min(seq_at(a, c.b).m, a.cap)) {
+          c.j0 = 0;
+          if (++c.b == a.B) {
+            c.b = 0;
+            c.blk = 0;
+            ++c.g;
+          }
+        }
+        next = block_tiles(a, seq_at(a, c.b), c.j0, first);
+      } while (next == 0);
+    }
+  };
+  // tile x of a part: its tokens begin at
+  auto tile_token = [&](const Cursor& c, int first, int x) { return first + (c.x + x) / a.passes * a.q_tokens; };
+  auto tile_pass = [&](const Cursor& c, int x) { return (c.x + x) % a.passes; };
+
+  if (warp < kSumWarps) {
+    // ------------------------------------------------------------ sums of a key tile
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * 2 * kRows;
+    const float2 c2 = both(kLog2eInvSqrtD);
+    int n = 0;
+    walk([&](int part, const Cursor& c, const Seq& s, int first, int tiles) {
+      const int k0 = c.j0 + t * kKeys, j = k0 + row;
+      float total = 0.f;
+      bool ok = true;
+      for (int x = 0; x < tiles; ++x, ++n) {
+        const int token = tile_token(c, first, x), heads = min(a.G - tile_pass(c, x) * a.q_heads, a.q_heads);
+        const int p0 = token + s.shift(), p1 = min(token + a.q_tokens, s.n) - 1 + s.shift();   // positions
+        const bool whole = token + a.q_tokens <= s.n && heads == a.q_heads && k0 + kKeys - 1 <= p0 &&
+                           (k0 + kKeys - 1 < a.sinks || k0 > p1 - a.window);
+        ok = wait(kBSFull + t * 2 + (n & 1), (uint32_t)(n >> 1) & 1u) && wait(kBLFull + n % kStats, (uint32_t)(n / kStats) & 1u);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        tc_fence_after();
+        const uint32_t st = base + kOffStats + (n % kStats) * kRows * 4, ts = lanes + (n & 1) * kRows;
+        float2 sum[2] = {both(0.f), both(0.f)};
+        auto add = [&](auto masked_tag) {
+          constexpr bool kMasked = decltype(masked_tag)::value;
+          uint32_t sv[2][32];
+          tc_ld32(ts, sv[0]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            tc_landed(sv[q & 1]);
+            if (q < 3) tc_ld32(ts + 32 * (q + 1), sv[(q + 1) & 1]);
+            else {   // S^T has been read
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(bar(kBSEmpty + t * 2 + (n & 1)));
+            }
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) {
+              const uint4 l4 = lds128(st + (32 * q + k) * 4);
+              const float2 l2[2] = {{__uint_as_float(l4.x), __uint_as_float(l4.y)}, {__uint_as_float(l4.z), __uint_as_float(l4.w)}};
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const float2 z{__uint_as_float(sv[q & 1][k + 2 * e]), __uint_as_float(sv[q & 1][k + 2 * e + 1])};
+                const float2 y = fma2(z, c2, l2[e]);
+                float2 w{ex2(y.x), ex2(y.y)};
+                if (kMasked) {
+                  auto seen = [&](int r) {
+                    const int tk = mem[kOffToken + r], pos = p0 + tk;
+                    return r < box_rows && pos <= p1 && r - tk * a.q_heads < heads && sees(a, pos, j);
+                  };
+                  w.x = seen(32 * q + k + 2 * e) ? w.x : 0.f;
+                  w.y = seen(32 * q + k + 2 * e + 1) ? w.y : 0.f;
+                }
+                sum[e] = add2(sum[e], w);
+              }
+            }
+          }
+        };
+        if (whole) add(std::false_type{});
+        else add(std::true_type{});
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kBLEmpty + n % kStats));
+        const float2 both_sums = add2(sum[0], sum[1]);
+        total += both_sums.x + both_sums.y;
+      }
+      a.part[((int64_t)c.g * nblk + c.blk + blockIdx.x) * kBlock + t * kKeys + row] = total;
+      return true;
+    });
+  } else if (warp == kLoadWarp) {
+    // ------------------------------------------------------------ loads
+    if (lane == 0) {
+      int n = 0, parts = 0;
+      walk([&](int part, const Cursor& c, const Seq& s, int first, int tiles) {
+        if (part >= 2 && !wait(kBKEmpty + (part & 1), (uint32_t)(part / 2 - 1) & 1u)) return false;
+        mbar_arrive_expect_tx(bar(kBKFull + (part & 1)), kTiles * kTileBytes);
+        for (int t = 0; t < kTiles; ++t)
+          for (int h = 0; h < 2; ++h)
+            tma_tile_3d(base + kOffK + ((part & 1) * kTiles + t) * kTileBytes + h * kHalf, &a.kmap, 64 * h, c.g,
+                        s.k0 + c.j0 + t * kKeys, bar(kBKFull + (part & 1)));
+        parts = part + 1;
+        for (int x = 0; x < tiles; ++x, ++n) {
+          const int slot = n % kStages;
+          if (n >= kStages && !wait(kBQEmpty + slot, (uint32_t)(n / kStages - 1) & 1u)) return false;
+          mbar_arrive_expect_tx(bar(kBQFull + slot), (uint32_t)box_rows * 256);
+          for (int h = 0; h < 2; ++h)
+            tma_tile_3d(base + kOffQ + slot * kTileBytes + h * kHalf, &a.qmap, 64 * h, c.g * a.G + tile_pass(c, x) * a.q_heads,
+                        s.q0 + tile_token(c, first, x), bar(kBQFull + slot));
+        }
+        return true;
+      });
+      if (misc[1]) {   // what is under way has to land before the CTA goes
+        for (int x = max(0, n - kStages); x < n; ++x) mbar_wait(bar(kBQFull + x % kStages), (uint32_t)(x / kStages) & 1u, a.err);
+        for (int x = max(0, parts - 2); x < parts; ++x) mbar_wait(bar(kBKFull + (x & 1)), (uint32_t)(x / 2) & 1u, a.err);
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ------------------------------------------------------------ products
+    if (lane == 0) {
+      constexpr uint32_t kIdesc = f16_idesc(DT, kKeys, kRows, false);
+      int n = 0;
+      walk([&](int part, const Cursor& c, const Seq& s, int first, int tiles) {
+        if (!wait(kBKFull + (part & 1), (uint32_t)(part / 2) & 1u)) return false;
+        for (int x = 0; x < tiles; ++x, ++n) {
+          const int slot = n % kStages, buf = n & 1;
+          if (!wait(kBQFull + slot, (uint32_t)(n / kStages) & 1u)) return false;
+          const uint32_t qb = base + kOffQ + slot * kTileBytes;
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            if (n >= 2 && !wait(kBSEmpty + t * 2 + buf, (uint32_t)(n / 2 - 1) & 1u)) return false;
+            tc_fence_after();
+            const uint32_t kb = base + kOffK + ((part & 1) * kTiles + t) * kTileBytes;
+#pragma unroll
+            for (int k = 0; k < kHeadDim / 16; ++k)
+              tc_mma_f16(tmem + (t * 2 + buf) * kRows, smem_desc_sw128(kb + (k >> 2) * kHalf + (k & 3) * 32),
+                         smem_desc_sw128(qb + (k >> 2) * kHalf + (k & 3) * 32), kIdesc, k > 0 ? 1u : 0u);
+            tc_commit(bar(kBSFull + t * 2 + buf));
+          }
+          tc_commit(bar(kBQEmpty + slot));
+        }
+        tc_commit(bar(kBKEmpty + (part & 1)));
+        return true;
+      });
+      // products under way end before the tensor memory is released
+      tc_commit(bar(kBDone));
+      mbar_wait(bar(kBDone), 0u, a.err);
+    }
+  } else if (warp == kStatWarp) {
+    // ------------------------------------------------------------ the rows' statistics, -lse log2 e
+    int n = 0;
+    walk([&](int part, const Cursor& c, const Seq& s, int first, int tiles) {
+      float v[4];
+      auto load = [&](int x) {
+        const int token = tile_token(c, first, x), h0 = tile_pass(c, x) * a.q_heads;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = lane + 32 * e, tk = r / a.q_heads, hg = h0 + r - tk * a.q_heads;
+          const bool there = tk < a.q_tokens && token + tk < s.n && hg < a.G;
+          v[e] = there ? a.lse[(int64_t)(s.q0 + token + tk) * a.H + c.g * a.G + hg] * -1.44269504f : -INFINITY;
+        }
+      };
+      load(0);
+      for (int x = 0; x < tiles; ++x, ++n) {
+        bool ok = n < kStats || wait(kBLEmpty + n % kStats, (uint32_t)(n / kStats - 1) & 1u);
+        if (!__all_sync(0xffffffffu, ok)) return false;
+        float* to = reinterpret_cast<float*>(mem + kOffStats) + (n % kStats) * kRows;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) to[lane + 32 * e] = v[e];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar(kBLFull + n % kStats));
+        if (x + 1 < tiles) load(x + 1);
+      }
+      return true;
+    });
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
 }
+
+// The parts of a block, in the order of the CTAs, over its KV head or all of them.
+__global__ void __launch_bounds__(kBlock) hill_prompt_importance_sum_kernel(const __grid_constant__ PromptArgs a) {
+  pdl_wait();
+  const int blk = blockIdx.x;
+  const int2 totals = *a.totals;
+  if (blk >= totals.x) return;
+  const BlockInfo f = a.info[blk];
+  if (f.tiles == 0 || (int)threadIdx.x >= f.keys) return;
+  const int64_t all = *a.tiles, total = all * a.Hkv, per = (total + totals.y - 1) / totals.y;
+  float sum = 0.f;
+  for (int g = a.kvh ? blockIdx.y : 0; g < (a.kvh ? (int)blockIdx.y + 1 : a.Hkv); ++g) {
+    const int64_t w = g * all + f.before;
+    const int c0 = (int)(w / per), c1 = (int)((w + f.tiles - 1) / per);
+    for (int c = c0; c <= c1; ++c) sum += a.part[((int64_t)g * totals.x + blk + c) * kBlock + threadIdx.x];
+  }
+  a.accum[((int64_t)f.b * (a.kvh ? a.Hkv : 1) + blockIdx.y) * a.cap + f.j0 + threadIdx.x] += sum;
+}
+
+int64_t most_blocks(int B, int64_t k_rows) { return k_rows / kBlock + B; }
 
 }  // namespace
 
-int importance_splits(int B, int Hkv, int64_t k_rows, int sms) { return 1; }
+ImportanceSpace importance_space(int B, int Hkv, int64_t k_rows, int sms) {
+  ImportanceSpace s;
+  s.part = (size_t)(Hkv * most_blocks(B, k_rows) + sms) * kBlock * sizeof(float);
+  s.info = (size_t)most_blocks(B, k_rows) * sizeof(BlockInfo);
+  return s;
+}
 
 cudaError_t launch_prompt_importance(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels) {
-  *kernels = 1;
-  const dim3 grid((a.cap + kWarps - 1) / kWarps, a.kvh ? a.Hkv : 1, a.B);
-  return dtype ? launch_pdl(hill_prompt_importance_kernel<1>, grid, dim3(kWarps * 32), 0, st, 0, a)
-               : launch_pdl(hill_prompt_importance_kernel<0>, grid, dim3(kWarps * 32), 0, st, 0, a);
+  auto kern = dtype ? hill_prompt_importance_kernel<1> : hill_prompt_importance_kernel<0>;
+  static int cache[2][64] = {{0}};
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), kSmem, cache[dtype ? 1 : 0]);
+  if (e != cudaSuccess) return e;
+  *kernels = 2;
+  e = launch_pdl(kern, dim3(sms), dim3(kThreads), kSmem, st, 0, a);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(hill_prompt_importance_sum_kernel, dim3((unsigned)most_blocks(a.B, a.k_rows), a.kvh ? a.Hkv : 1),
+                    dim3(kBlock), 0, st, 0, a);
 }
 
 }  // namespace hill
