@@ -38,8 +38,7 @@ constexpr int kSumWarps = 4 * kTiles, kLoadWarp = kSumWarps, kMmaWarp = kLoadWar
 constexpr int kWarps = 12, kThreads = kWarps * 32;
 
 constexpr int kOffK = 0, kOffQ = 2 * kTiles * kTileBytes, kOffStats = kOffQ + kStages * kTileBytes;
-constexpr int kOffToken = kOffStats + kStats * kRows * 4;   // token of a row within its tile, one byte each
-constexpr int kOffBars = kOffToken + kRows;
+constexpr int kOffBars = kOffStats + kStats * kRows * 4;
 constexpr int kBKFull = 0, kBKEmpty = 2, kBQFull = 4, kBQEmpty = kBQFull + kStages, kBLFull = kBQEmpty + kStages,
               kBLEmpty = kBLFull + kStats, kBSFull = kBLEmpty + kStats, kBSEmpty = kBSFull + 4, kBDone = kBSEmpty + 4,
               kBars = kBDone + 1;
@@ -186,7 +185,6 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
     const int per_tile = (kRows - box_rows) * 8, tile = i / per_tile, r = i - tile * per_tile;
     sts128_zero(base + kOffQ + tile * kHalf + box_rows * 128 + r * 16);
   }
-  if (tid < kRows) mem[kOffToken + tid] = (unsigned char)(tid / a.q_heads);
   fence_proxy_async();
   __syncthreads();
 
@@ -249,6 +247,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
         tc_fence_after();
         const uint32_t st = base + kOffStats + (n % kStats) * kRows * 4, ts = lanes + (n & 1) * kRows;
         float2 sum[2] = {both(0.f), both(0.f)};
+        uint32_t vis[4];   // the tile's rows that see the key
         auto add = [&](auto masked_tag) {
           constexpr bool kMasked = decltype(masked_tag)::value;
           uint32_t sv[2][32];
@@ -272,20 +271,32 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
                 const float2 y = fma2(z, c2, l2[e]);
                 float2 w{ex2(y.x), ex2(y.y)};
                 if (kMasked) {
-                  auto seen = [&](int r) {
-                    const int tk = mem[kOffToken + r], pos = p0 + tk;
-                    return r < box_rows && pos <= p1 && r - tk * a.q_heads < heads && sees(a, pos, j);
-                  };
-                  w.x = seen(32 * q + k + 2 * e) ? w.x : 0.f;
-                  w.y = seen(32 * q + k + 2 * e + 1) ? w.y : 0.f;
+                  w.x = (vis[q] >> (k + 2 * e)) & 1u ? w.x : 0.f;
+                  w.y = (vis[q] >> (k + 2 * e + 1)) & 1u ? w.y : 0.f;
                 }
                 sum[e] = add2(sum[e], w);
               }
             }
           }
         };
-        if (whole) add(std::false_type{});
-        else add(std::true_type{});
+        if (whole) {
+          add(std::false_type{});
+        } else {
+          // the rows that see the key are consecutive: of tokens from the key's own to the window's last (a tile of
+          // fewer heads than q_heads has one token)
+          const int from = max(0, j - p0) * a.q_heads;
+          const int last = j < a.sinks ? p1 : min(p1, j + a.window - 1);
+          const int to = min(last - p0 + 1, a.q_tokens) * a.q_heads - (a.q_heads - heads);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) vis[q] = bits_to(to - 1 - 32 * q) & ~bits_to(from - 1 - 32 * q);
+          if (__any_sync(0xffffffffu, from < to)) {
+            add(std::true_type{});
+          } else {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kBSEmpty + t * 2 + (n & 1)));
+          }
+        }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar(kBLEmpty + n % kStats));
         const float2 both_sums = add2(sum[0], sum[1]);

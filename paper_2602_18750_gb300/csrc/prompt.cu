@@ -75,8 +75,6 @@ struct Plan {
   }
 };
 
-__device__ __forceinline__ uint32_t bits_to(int x) { return x < 0 ? 0u : (x >= 31 ? ~0u : (2u << x) - 1u); }   // 0 .. x
-
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units) {
   extern __shared__ unsigned char psm_raw[];

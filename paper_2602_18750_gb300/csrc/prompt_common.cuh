@@ -24,9 +24,8 @@ __device__ __forceinline__ Seq seq_at(const PromptArgs& a, int b) {
   return s;
 }
 
-__device__ __forceinline__ bool sees(const PromptArgs& a, int pos, int j) {
-  return j <= pos && (j < a.sinks || j > pos - a.window);
-}
+// Bits 0 to x.
+__device__ __forceinline__ uint32_t bits_to(int x) { return x < 0 ? 0u : (x >= 31 ? ~0u : (2u << x) - 1u); }
 
 }  // namespace
 }  // namespace hill
