@@ -350,46 +350,82 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     // ------------------------------------------------------------ products
     if (lane == 0 && plan.count > 0) {
       constexpr uint32_t kIdescS = f16_idesc(DT, kRows, kKeys, false), kIdescO = f16_idesc(DT, kRows, kHeadDim, true);
+      // what to do in a round, known before its waits: the tensor cores are not to wait for this thread's arithmetic
+      struct Round {
+        bool pv[kTiles], qk[kTiles], end[kTiles], check;
+      };
       const int last[kTiles] = {plan.last_active(0), plan.last_active(1)};
-      int n[kTiles] = {0, 0}, checked = 0;
+      auto look = [&](int i) {
+        Round r{};
+        const int jv = i > 0 ? plan.key(i - 1) : 0, jk = i < plan.count ? plan.key(i) : 0;
+        r.check = i > 0 && plan.partial(jv);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          r.pv[t] = i > 0 && plan.active(t, jv);
+          r.qk[t] = i < plan.count && plan.active(t, jk);
+          r.end[t] = i - 1 == last[t];
+        }
+        return r;
+      };
+      const uint64_t q_desc = smem_desc_sw128(base), k_desc = smem_desc_sw128(base + kOffRing),
+                     v_desc = smem_desc_sw128_mn(base + kOffRing, kHalf);
+      int slot_v = 1, slot_k = 0;           // ring slots of V of the round before, and of K
+      uint32_t phase_v = 0, phase_k = 0;
+      auto step = [&](int& slot, uint32_t& phase) {
+        slot += 2;
+        if (slot >= kStages) {
+          slot -= kStages;
+          phase ^= 1u;
+        }
+      };
+      uint32_t phase_p[kTiles] = {0u, 0u};
+      int checked = 0;
       bool ok = wait(kBQ, 0u);
       for (int i = 0; i <= plan.count && ok; ++i) {
-        const int jv = i > 0 ? plan.key(i - 1) : 0, jk = i < plan.count ? plan.key(i) : 0;
+        const Round r = look(i);
+        const uint64_t v0 = v_desc + (uint32_t)(slot_v * (kTileBytes >> 4)), k0 = k_desc + (uint32_t)(slot_k * (kTileBytes >> 4));
         if (i > 0) {
-          ok = full(2 * i - 1);
-          if (ok && plan.partial(jv)) {
+          ok = wait(kBFull + slot_v, phase_v);
+          if (ok && r.check) {
             ok = wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
             ++checked;
           }
         }
+        if (ok && i < plan.count) ok = wait(kBFull + slot_k, phase_k);
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-          if (ok && i > 0 && plan.active(t, jv)) {   // O += P V
-            ok = wait(kBP + t, (uint32_t)(n[t] - 1) & 1u);
+          if (ok && r.pv[t]) {   // O += P V
+            ok = wait(kBP + t, phase_p[t]);
+            phase_p[t] ^= 1u;
             if (ok) {
               tc_fence_after();
-              const uint32_t vb = ring(2 * i - 1);
 #pragma unroll
               for (int k = 0; k < kKeys / 16; ++k)
-                tc_mma_f16_ts(tmem + kColO + t * kHeadDim, tmem + kColS + t * kKeys + 8 * k,
-                              smem_desc_sw128_mn(vb + 2048 * k, kHalf), kIdescO, 1u);
-              if (i - 1 == last[t]) tc_commit(bar(kBO + t));
+                tc_mma_f16_ts(tmem + kColO + t * kHeadDim, tmem + kColS + t * kKeys + 8 * k, v0 + (uint32_t)(k * (2048 >> 4)),
+                              kIdescO, 1u);
+              if (r.end[t]) tc_commit(bar(kBO + t));
             }
           }
-          if (t == 0 && ok && i < plan.count) ok = full(2 * i);
-          if (ok && i < plan.count && plan.active(t, jk)) {   // S = Q K^T
+          if (ok && r.qk[t]) {   // S = Q K^T
             tc_fence_after();
-            const uint32_t qb = base + t * kTileBytes, kb = ring(2 * i);
 #pragma unroll
-            for (int k = 0; k < kHeadDim / 16; ++k)
-              tc_mma_f16(tmem + kColS + t * kKeys, smem_desc_sw128(qb + (k >> 2) * kHalf + (k & 3) * 32),
-                         smem_desc_sw128(kb + (k >> 2) * kHalf + (k & 3) * 32), kIdescS, k > 0 ? 1u : 0u);
+            for (int k = 0; k < kHeadDim / 16; ++k) {
+              const uint32_t at = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
+              tc_mma_f16(tmem + kColS + t * kKeys, q_desc + (uint32_t)(t * (kTileBytes >> 4)) + at, k0 + at, kIdescS,
+                         k > 0 ? 1u : 0u);
+            }
             tc_commit(bar(kBS + t));
-            ++n[t];
           }
         }
-        if (ok && i > 0) tc_commit(bar(kBEmpty + (2 * i - 1) % kStages));
-        if (ok && i < plan.count) tc_commit(bar(kBEmpty + (2 * i) % kStages));
+        if (!ok) break;
+        if (i > 0) {
+          tc_commit(bar(kBEmpty + slot_v));
+          step(slot_v, phase_v);
+        }
+        if (i < plan.count) {
+          tc_commit(bar(kBEmpty + slot_k));
+          step(slot_k, phase_k);
+        }
       }
       if (!ok) {   // products under way end before the tensor memory is released
         tc_commit(bar(kBQ));
