@@ -156,8 +156,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   plan.count = b >= 0 ? plan.nsink + max(0, end - plan.wfirst) : 0;
 
   auto wait = [&](int i, uint32_t parity) {
-    if (misc[1]) return false;
-    if (mbar_wait(bar(i), parity, a.err)) return true;
+    if (mbar_try_wait(bar(i), parity)) return true;
+    if (!misc[1] && mbar_wait(bar(i), parity, a.err)) return true;
     misc[1] = 1;
     return false;
   };
@@ -348,25 +348,13 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     }
   } else if (warp == kMmaWarp) {
     // ------------------------------------------------------------ products
-    if (lane == 0 && plan.count > 0) {
+    if (plan.count > 0) {
       constexpr uint32_t kIdescS = f16_idesc(DT, kRows, kKeys, false), kIdescO = f16_idesc(DT, kRows, kHeadDim, true);
-      // what to do in a round, known before its waits: the tensor cores are not to wait for this thread's arithmetic
-      struct Round {
-        bool pv[kTiles], qk[kTiles], end[kTiles], check;
-      };
+      // What to do in a round is worked out for 32 rounds at a time, a lane each: issuing products takes as long as the
+      // tensor cores take them, so arithmetic here is time in which they stand still (1085 of 3470 cycles a round).
+      // act[t], cut: key tiles i0 .. that tile t's rows see, and those that some row does not see whole
+      uint32_t act[kTiles] = {0u, 0u}, cut = 0u, act_before[kTiles] = {0u, 0u}, cut_before = 0u;
       const int last[kTiles] = {plan.last_active(0), plan.last_active(1)};
-      auto look = [&](int i) {
-        Round r{};
-        const int jv = i > 0 ? plan.key(i - 1) : 0, jk = i < plan.count ? plan.key(i) : 0;
-        r.check = i > 0 && plan.partial(jv);
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          r.pv[t] = i > 0 && plan.active(t, jv);
-          r.qk[t] = i < plan.count && plan.active(t, jk);
-          r.end[t] = i - 1 == last[t];
-        }
-        return r;
-      };
       const uint64_t q_desc = smem_desc_sw128(base), k_desc = smem_desc_sw128(base + kOffRing),
                      v_desc = smem_desc_sw128_mn(base + kOffRing, kHalf);
       int slot_v = 1, slot_k = 0;           // ring slots of V of the round before, and of K
@@ -381,12 +369,31 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       uint32_t phase_p[kTiles] = {0u, 0u};
       int checked = 0;
       bool ok = wait(kBQ, 0u);
-      for (int i = 0; i <= plan.count && ok; ++i) {
-        const Round r = look(i);
+      for (int i = 0; i <= plan.count; ++i) {
+        if ((i & 31) == 0) {
+          __syncwarp();
+          const int mine = i + lane, j0 = plan.key(mine);
+          const bool there = mine < plan.count;
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            act_before[t] = act[t] >> 31;
+            act[t] = __ballot_sync(0xffffffffu, there && plan.active(t, j0));
+          }
+          cut_before = cut >> 31;
+          cut = __ballot_sync(0xffffffffu, there && plan.partial(j0));
+        }
+        const uint32_t check = i & 31 ? cut >> ((i - 1) & 31) & 1u : cut_before;
+        uint32_t pv[kTiles], qk[kTiles];
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) {
+          qk[t] = act[t] >> (i & 31) & 1u;
+          pv[t] = i & 31 ? act[t] >> ((i - 1) & 31) & 1u : act_before[t];
+        }
+        if (lane != 0 || !ok) continue;
         const uint64_t v0 = v_desc + (uint32_t)(slot_v * (kTileBytes >> 4)), k0 = k_desc + (uint32_t)(slot_k * (kTileBytes >> 4));
         if (i > 0) {
           ok = wait(kBFull + slot_v, phase_v);
-          if (ok && r.check) {
+          if (ok && check) {
             ok = wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
             ++checked;
           }
@@ -394,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
         if (ok && i < plan.count) ok = wait(kBFull + slot_k, phase_k);
 #pragma unroll
         for (int t = 0; t < kTiles; ++t) {
-          if (ok && r.pv[t]) {   // O += P V
+          if (ok && pv[t]) {   // O += P V
             ok = wait(kBP + t, phase_p[t]);
             phase_p[t] ^= 1u;
             if (ok) {
@@ -403,10 +410,10 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
               for (int k = 0; k < kKeys / 16; ++k)
                 tc_mma_f16_ts(tmem + kColO + t * kHeadDim, tmem + kColS + t * kKeys + 8 * k, v0 + (uint32_t)(k * (2048 >> 4)),
                               kIdescO, 1u);
-              if (r.end[t]) tc_commit(bar(kBO + t));
+              if (i - 1 == last[t]) tc_commit(bar(kBO + t));
             }
           }
-          if (ok && r.qk[t]) {   // S = Q K^T
+          if (ok && qk[t]) {   // S = Q K^T
             tc_fence_after();
 #pragma unroll
             for (int k = 0; k < kHeadDim / 16; ++k) {
@@ -417,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
             tc_commit(bar(kBS + t));
           }
         }
-        if (!ok) break;
+        if (!ok) continue;
         if (i > 0) {
           tc_commit(bar(kBEmpty + slot_v));
           step(slot_v, phase_v);
@@ -427,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
           step(slot_k, phase_k);
         }
       }
-      if (!ok) {   // products under way end before the tensor memory is released
+      if (!ok && lane == 0) {   // products under way end before the tensor memory is released
         tc_commit(bar(kBQ));
         mbar_wait(bar(kBQ), 1u, a.err);
       }
