@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
   __syncthreads();
 
   auto wait = [&](int i, uint32_t parity) {
-    if (mbar_try_wait(bar(i), parity)) return true;
-    if (!misc[1] && mbar_wait(bar(i), parity, a.err)) return true;
+    if (mbar_try_wait_long(bar(i), parity)) return true;
+    if (!misc[1] && mbar_wait_long(bar(i), parity, a.err)) return true;
     misc[1] = 1;
     return false;
   };

@@ -3,15 +3,23 @@
 //
 // A unit is two tiles of 128 query rows of one KV head -- a row is a (token, query head of the group), token by
 // token, so the heads of a group share each key tile -- and walks the 128-key tiles that its rows see: those of the
-// sinks, then those of the window up to the diagonal.  One CTA per unit, 12 warps:
+// sinks, then those of the window up to the diagonal.  One CTA per unit, 20 warps:
 //
-//   softmax   (warps 0-3, 4-7: a tile each, a thread per row) reads S = Q K^T from tensor memory, forms p = 2^(z - m)
-//             and puts it back there in the type of V, over S;
-//   loads     (warp 8) the Q tiles once, K and V tiles in a ring, by TMA (128-byte swizzle);
-//   products  (warp 9) one thread issues S = Q K^T (both operands in shared memory) and O += P V (P in tensor memory,
-//             V with the head dimension contiguous).  The tiles take turns: while one's softmax runs, the tensor
-//             cores have the other's P V and next S;
-//   checks    (warps 10, 11) of V tiles that some row sees only a part of: rows of V that are not finite.
+//   softmax   (warps 0-7, 8-15: a tile each, a thread per half row) reads S = Q K^T from tensor memory, forms
+//             p = 2^(z - m) and puts it back there in the type of V, over S;
+//   loads     (warp 16) the Q tiles once, K and V tiles in a ring, by TMA (128-byte swizzle);
+//   products  (warps 17, 18) a thread for each tile issues S = Q K^T (both operands in shared memory) and O += P V (P in
+//             tensor memory, V with the head dimension contiguous), in turns: while one tile's softmax runs, the tensor cores
+//             have the other's P V and next S;
+//   checks    (warp 19) of V tiles that some row sees only a part of: rows of V that are not finite.
+//
+// What keeps the tensor cores waiting is looked at in cycles of a round (both tiles, 2048 of products), on 8K tokens of
+// 32 heads.  Issuing takes as long as the tensor cores take the products, so whatever else an issuing thread does -- waits,
+// commits, 1400 cycles a round -- is time in which they stand still: one thread for both tiles 4100.  Two threads
+// without turns 4600: the tiles fall into step, and both softmaxes run while nothing is there to multiply.
+//
+// Round i of a tile is O += P V of key tile i - 1 and S of key tile i; V of the one and K of the other come, and are
+// given back, together.
 //
 // Tensor memory holds S and O of both tiles, 4 x 128 columns, all there is.
 //
@@ -24,6 +32,9 @@
 // A hidden key has p = 0, and a hidden value must not reach O by 0 * NaN.  In tiles that some row does not see whole, rows
 // of V that are not finite are set to zero in shared memory before the product, and the rows that see them add
 // p v themselves.
+#include <atomic>
+#include <type_traits>
+
 #include "prompt_common.cuh"
 #include "tc_common.cuh"
 
@@ -35,17 +46,22 @@ constexpr int kStages = 5;                       // ring of K and V tiles
 constexpr int kHalf = kKeys * 128;               // 64 dims of 128 rows
 constexpr int kTileBytes = 2 * kHalf;
 constexpr int kMasks = 4;                        // ring of the checks' results
-constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarp = kSoftmaxWarps, kMmaWarp = kLoadWarp + 1, kCheckWarp = kMmaWarp + 1;
-constexpr int kThreads = (kCheckWarp + 2) * 32;
+constexpr int kSoftmaxWarps = 8 * kTiles, kLoadWarp = kSoftmaxWarps, kMmaWarp = kLoadWarp + 1, kCheckWarp = kMmaWarp + kTiles;
+constexpr int kThreads = (kCheckWarp + 1) * 32;
+constexpr int kRounds = 4;                       // rounds whose barriers are told apart
 
 constexpr int kOffRing = kTiles * kTileBytes;
 constexpr int kOffBars = kOffRing + kStages * kTileBytes;
-// barriers: Q; ring full, empty; S full, P ready, O done of each tile; checks
-constexpr int kBQ = 0, kBFull = 1, kBEmpty = kBFull + kStages, kBS = kBEmpty + kStages, kBP = kBS + kTiles, kBO = kBP + kTiles,
-              kBCheck = kBO + kTiles, kBars = kBCheck + kMasks;
+// barriers: Q; a round's K and V there, given back; S full, P ready, O done of each tile; checks
+constexpr int kBQ = 0, kBFull = 1, kBDone = kBFull + kRounds, kBS = kBDone + kRounds, kBP = kBS + kTiles, kBO = kBP + kTiles,
+              kBCheck = kBO + kTiles, kBEnd = kBCheck + kMasks, kBTurn = kBEnd + kTiles, kBars = kBTurn + kTiles;
 constexpr int kOffMasks = kOffBars + ((kBars * 8 + 15) & ~15);
 constexpr int kOffMisc = kOffMasks + kMasks * 16;   // tensor memory address, abort flag, unit
-constexpr int kSmem = kOffMisc + 16 + 1024;
+constexpr int kOffPeer = kOffMisc + 16;             // [tile][half][row] what the halves of a row tell each other
+constexpr int kSmem = kOffPeer + kTiles * 2 * kRows * 4;
+// registers of a thread: at launch, and then of the softmax warps and of the others
+constexpr int kRegs = 96, kRegsSoftmax = 104, kRegsOther = 64;
+static_assert(kSoftmaxWarps * kRegsSoftmax + (kThreads / 32 - kSoftmaxWarps) * kRegsOther <= kThreads / 32 * kRegs, "registers");
 static_assert(kSmem <= 232448, "shared memory");
 
 constexpr uint32_t kColS = 0, kColO = kTiles * kKeys, kCols = 512;
@@ -75,11 +91,21 @@ struct Plan {
   }
 };
 
+// Does x hold for any of the 256 threads that meet at barrier `id`?
+__device__ __forceinline__ bool tile_any(int id, bool x) {
+  int any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.or.pred q, %2, 256, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
+      : "=r"(any)
+      : "r"((int)x), "r"(id)
+      : "memory");
+  return any != 0;
+}
+
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units) {
-  extern __shared__ unsigned char psm_raw[];
-  const uint32_t base = (smem_addr(psm_raw) + 1023u) & ~1023u;
-  unsigned char* const mem = psm_raw + (base - smem_addr(psm_raw));
+  extern __shared__ __align__(1024) unsigned char mem[];
+  const uint32_t base = smem_addr(mem);
   uint32_t* const masks = reinterpret_cast<uint32_t*>(mem + kOffMasks);
   volatile int* const misc = reinterpret_cast<int*>(mem + kOffMisc);   // 0: tensor memory, 1: abort, 2: sequence, 3: unit in it
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -115,16 +141,18 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     }
   } else if (warp == kLoadWarp && lane == 0) {
     mbar_init(bar(kBQ), 1);
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < kRounds; ++i) {
       mbar_init(bar(kBFull + i), 1);
-      mbar_init(bar(kBEmpty + i), 1);
+      mbar_init(bar(kBDone + i), kTiles + 1);   // both tiles' products, and the checks
     }
     for (int t = 0; t < kTiles; ++t) {
       mbar_init(bar(kBS + t), 1);
-      mbar_init(bar(kBP + t), 4);
+      mbar_init(bar(kBP + t), 8);
+      mbar_init(bar(kBTurn + t), 1);
       mbar_init(bar(kBO + t), 1);
+      mbar_init(bar(kBEnd + t), 1);
     }
-    for (int i = 0; i < kMasks; ++i) mbar_init(bar(kBCheck + i), 2);
+    for (int i = 0; i < kMasks; ++i) mbar_init(bar(kBCheck + i), 1);
     fence_barrier_init();
     prefetch_tmap(&a.qmap);
     prefetch_tmap(&a.kmap);
@@ -156,36 +184,38 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   plan.count = b >= 0 ? plan.nsink + max(0, end - plan.wfirst) : 0;
 
   auto wait = [&](int i, uint32_t parity) {
-    if (mbar_try_wait(bar(i), parity)) return true;
-    if (!misc[1] && mbar_wait(bar(i), parity, a.err)) return true;
+    if (mbar_try_wait_long(bar(i), parity)) return true;
+    if (!misc[1] && mbar_wait_long(bar(i), parity, a.err)) return true;
     misc[1] = 1;
     return false;
   };
   auto ring = [&](int n) { return base + kOffRing + (uint32_t)((n % kStages) * kTileBytes); };   // n: 2 i for K, 2 i + 1 for V
-  auto full = [&](int n) { return wait(kBFull + n % kStages, (uint32_t)(n / kStages) & 1u); };
+  auto of_round = [&](int first, int i) { return wait(first + i % kRounds, (uint32_t)(i / kRounds) & 1u); };
 
   if (warp < kSoftmaxWarps) {
-    // ------------------------------------------------------------ softmax of a tile
-    const int t = warp >> 2;
+    // ------------------------------------------------------------ softmax of half the columns of a tile
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
+    const int t = warp >> 3, half = (warp >> 2) & 1;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + kColS + t * kKeys, to = tmem + lanes + kColO + t * kHeadDim;
+    const uint32_t ts = tmem + lanes + kColS + t * kKeys, to = tmem + lanes + kColO + t * kHeadDim + 64 * half;
     const int row = (warp & 3) * 32 + lane, tok = row / a.q_heads, hg = pass * a.q_heads + row - tok * a.q_heads;
     const int i_tok = token0 + t * a.q_tokens + tok;
     const bool valid = b >= 0 && tok < a.q_tokens && hg < a.G && i_tok < s.n;
     const int pos = i_tok + shift;
     const float2 c2 = both(valid ? kLog2eInvSqrtD : 0.f);   // (a row that is none has logits of 0)
-    float m = kNegHuge, l = 0.f;
+    float* const peer = reinterpret_cast<float*>(mem + kOffPeer) + t * 2 * kRows + row;   // [half]
+    float m = kNegHuge, l = 0.f;   // of the row; of this half
     {
       uint32_t zero[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) zero[i] = 0u;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) tc_st32(to + 32 * c, zero);
+      tc_st32(to, zero);
+      tc_st32(to + 32, zero);
       tc_wait_st();
     }
     int n = 0, checked = 0;
     bool ok = true;
-    for (int i = 0; i < plan.count && ok; ++i) {
+    for (int i = 0; i < plan.count; ++i) {
       const int j0 = plan.key(i);
       const bool part = plan.partial(j0);
       if (!plan.active(t, j0)) {
@@ -194,104 +224,120 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       }
       const bool whole = plan.full(t, j0);
       // the keys that the row sees, as bits
-      uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};
+      uint32_t vis[2] = {~0u, ~0u};
       if (!whole) {
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          vis[w] = valid ? bits_to(pos - j0 - 32 * w) & (bits_to(a.sinks - 1 - j0 - 32 * w) | ~bits_to(pos - j0 - a.window - 32 * w))
-                         : 0u;
-      }
-      ok = __all_sync(0xffffffffu, wait(kBS + t, (uint32_t)n & 1u));
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t p[64];
-      float sum;
-      uint32_t sv[2][32];
-      auto weights = [&](auto masked_tag) {
-        constexpr bool kMasked = decltype(masked_tag)::value;
-        const float2 m2 = both(-m);
-        float2 sums[2] = {both(0.f), both(0.f)};
-        tc_ld32(ts, sv[0]);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          tc_landed(sv[c & 1]);
-          if (c < 3) tc_ld32(ts + 32 * (c + 1), sv[(c + 1) & 1]);
-#pragma unroll
-          for (int k = 0; k < 32; k += 2) {
-            float2 z{__uint_as_float(sv[c & 1][k]), __uint_as_float(sv[c & 1][k + 1])};
-            if (kMasked) {
-              z.x = (vis[c] >> k) & 1u ? z.x : -INFINITY;
-              z.y = (vis[c] >> (k + 1)) & 1u ? z.y : -INFINITY;
-            }
-            const float2 x = fma2(z, c2, m2);
-            const float2 e{ex2(x.x), ex2(x.y)};
-            sums[(k >> 1) & 1] = add2(sums[(k >> 1) & 1], e);
-            p[c * 16 + (k >> 1)] = pack2<DT>(e.x, e.y);
-          }
+        for (int w = 0; w < 2; ++w) {
+          const int k0 = j0 + 64 * half + 32 * w;
+          vis[w] = valid ? bits_to(pos - k0) & (bits_to(a.sinks - 1 - k0) | ~bits_to(pos - k0 - a.window)) : 0u;
         }
-        const float2 s2 = add2(sums[0], sums[1]);
-        sum = s2.x + s2.y;
-      };
+      }
+      ok = wait(kBS + t, (uint32_t)n & 1u);
+      const uint32_t* const mask = masks + (checked % kMasks) * 4;
+      if (part) {
+        ok = ok && wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
+        ++checked;
+      }
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      uint32_t p[32];
+      float sum;
       for (int again = 0;; ++again) {
+        auto weights = [&](auto masked_tag) {
+          constexpr bool kMasked = decltype(masked_tag)::value;
+          const float2 m2 = both(-m);
+          float2 sums[2] = {both(0.f), both(0.f)};
+          uint32_t sv[2][16];
+          tc_ld16(ts + 64 * half, sv[0]);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            tc_wait_ld();
+            if (c < 3) tc_ld16(ts + 64 * half + 16 * (c + 1), sv[(c + 1) & 1]);
+#pragma unroll
+            for (int k = 0; k < 16; k += 2) {
+              float2 z{__uint_as_float(sv[c & 1][k]), __uint_as_float(sv[c & 1][k + 1])};
+              if (kMasked) {
+                z.x = (vis[c >> 1] >> (16 * (c & 1) + k)) & 1u ? z.x : -INFINITY;
+                z.y = (vis[c >> 1] >> (16 * (c & 1) + k + 1)) & 1u ? z.y : -INFINITY;
+              }
+              const float2 x = fma2(z, c2, m2);
+              const float2 e{ex2(x.x), ex2(x.y)};
+              sums[(k >> 1) & 1] = add2(sums[(k >> 1) & 1], e);
+              p[c * 8 + (k >> 1)] = pack2<DT>(e.x, e.y);
+            }
+          }
+          const float2 s2 = add2(sums[0], sums[1]);
+          sum = s2.x + s2.y;
+        };
         if (whole) weights(std::false_type{});
         else weights(std::true_type{});
-        if (again || !__any_sync(0xffffffffu, sum > 32768.f)) break;
-        // a weight may be past 2^15: the maximum is raised, what the old one has given shrinks
+        // From here on S may be written over, where no weight of the tile is past 2^15.  (All threads of the tile
+        // come here whatever happens; a wait that ran out for one ends the work of all.)
+        const bool over = sum > 32768.f;
+        const bool vote = tile_any(1 + t, over || !ok);
+        if (again || !vote) break;
+        ok = !tile_any(1 + t, !ok);
+        if (!ok) break;
+        // the maximum is raised, what the old one has given shrinks (a row whose weights are within keeps its maximum:
+        // what one row sees changes no bit of another's)
         float top = -INFINITY;
+        uint32_t sv[32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          tc_ld32(ts + 32 * c, sv[0]);
-          tc_landed(sv[0]);
+        for (int c = 0; c < 2; ++c) {
+          tc_ld32(ts + 64 * half + 32 * c, sv);
+          tc_landed(sv);
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if ((vis[c] >> k) & 1u) top = fmaxf(top, __uint_as_float(sv[0][k]) * c2.x);
+            if ((vis[c] >> k) & 1u) top = fmaxf(top, __uint_as_float(sv[k]) * c2.x);
         }
-        // (a row whose weights are within keeps its maximum: what one row sees changes no bit of another's)
-        const float mn = sum > 32768.f ? fmaxf(m, top - 7.f) : m, f = ex2(m - mn);
+        peer[half * kRows] = over ? top : -INFINITY;
+        named_sync(1 + t, 256);
+        const float mn = fmaxf(m, fmaxf(peer[0], peer[kRows]) - 7.f), f = ex2(m - mn);
         m = mn;
         l *= f;
-        for (int c = 0; c < 4 && n > 0; ++c) {
-          tc_ld32(to + 32 * c, sv[0]);
-          tc_landed(sv[0]);
+        for (int c = 0; c < 2 && n > 0; ++c) {
+          tc_ld32(to + 32 * c, sv);
+          tc_landed(sv);
 #pragma unroll
-          for (int k = 0; k < 32; ++k) sv[0][k] = __float_as_uint(__uint_as_float(sv[0][k]) * f);
-          tc_st32(to + 32 * c, sv[0]);
+          for (int k = 0; k < 32; ++k) sv[k] = __float_as_uint(__uint_as_float(sv[k]) * f);
+          tc_st32(to + 32 * c, sv);
         }
       }
+      if (!ok) break;
       l += sum;
-      tc_st32(ts, p);
-      tc_st32(ts + 32, p + 32);
+      tc_st32(ts + 32 * half, p);
       tc_wait_st();
       if (part) {
-        ok = __all_sync(0xffffffffu, wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u));
-        if (!ok) break;
-        for (int w = 0; w < 4; ++w) {
+        if (mask[0] | mask[1] | mask[2] | mask[3]) {
           // values that are not finite: the rows that see them take p v
-          for (uint32_t bad = masks[(checked % kMasks) * 4 + w]; bad; bad &= bad - 1u) {
-            const int k = __ffs(bad) - 1;
-            const uint32_t two = tc_ld1(ts + 16 * w + (k >> 1));
-            const float2 pk = unpack2<DT>(two);
-            const bool see = (w == 0 ? vis[0] : w == 1 ? vis[1] : w == 2 ? vis[2] : vis[3]) >> k & 1u;
-            const float pw = k & 1 ? pk.y : pk.x;
-            const auto* v = static_cast<const uint16_t*>(a.v) + (int64_t)(s.k0 + j0 + 32 * w + k) * a.v_st + (int64_t)g * a.v_sh;
+          tc_fence_before();
+          named_sync(1 + t, 256);   // both halves of p are there
+          tc_fence_after();
+          for (int w = 0; w < 4; ++w) {
+            for (uint32_t bad = mask[w]; bad; bad &= bad - 1u) {
+              const int k = __ffs(bad) - 1, j = j0 + 32 * w + k;
+              const float2 pk = unpack2<DT>(tc_ld1(ts + 16 * w + (k >> 1)));
+              const bool see = valid && j <= pos && (j < a.sinks || j > pos - a.window);
+              const float pw = k & 1 ? pk.y : pk.x;
+              const auto* v = static_cast<const uint16_t*>(a.v) + (int64_t)(s.k0 + j) * a.v_st + (int64_t)g * a.v_sh + 64 * half;
+              for (int c = 0; c < 2; ++c) {
+                uint32_t sv[32];
+                tc_ld32(to + 32 * c, sv);
+                tc_landed(sv);
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              tc_ld32(to + 32 * c, sv[0]);
-              tc_landed(sv[0]);
-#pragma unroll
-              for (int e = 0; e < 32; e += 2) {
-                const float2 x = unpack2<DT>(*reinterpret_cast<const uint32_t*>(v + 32 * c + e));
-                if (see && valid) {
-                  sv[0][e] = __float_as_uint(fmaf(pw, x.x, __uint_as_float(sv[0][e])));
-                  sv[0][e + 1] = __float_as_uint(fmaf(pw, x.y, __uint_as_float(sv[0][e + 1])));
+                for (int e = 0; e < 32; e += 2) {
+                  const float2 x = unpack2<DT>(*reinterpret_cast<const uint32_t*>(v + 32 * c + e));
+                  if (see) {
+                    sv[e] = __float_as_uint(fmaf(pw, x.x, __uint_as_float(sv[e])));
+                    sv[e + 1] = __float_as_uint(fmaf(pw, x.y, __uint_as_float(sv[e + 1])));
+                  }
                 }
+                tc_st32(to + 32 * c, sv);
               }
-              tc_st32(to + 32 * c, sv[0]);
+              tc_wait_st();
             }
-            tc_wait_st();
           }
         }
-        ++checked;
       }
       tc_fence_before();
       __syncwarp();
@@ -299,19 +345,22 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       ++n;
     }
     if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(kBO + t, 0u));
-    if (ok && b >= 0) {
+    if (!tile_any(1 + t, !ok) && b >= 0) {
       tc_fence_after();
+      peer[half * kRows] = l;
+      named_sync(1 + t, 256);
+      l = peer[0] + peer[kRows];
       // does the row see anything?
       const bool sees_any = pos >= 0 && (a.window > 0 || a.sinks > 0);
       const float inv = sees_any ? 1.f / l : 0.f;
       const int64_t at = (int64_t)(s.q0 + i_tok) * a.H + g * a.G + hg;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < 2; ++c) {
         uint32_t sv[32];
         tc_ld32(to + 32 * c, sv);
         tc_landed(sv);
         if (!valid) continue;
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * kHeadDim + 32 * c);
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * kHeadDim + 64 * half + 32 * c);
 #pragma unroll
         for (int e = 0; e < 32; e += 8) {
           uint32_t w[4];
@@ -321,9 +370,11 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
           dst[e / 8] = uint4{w[0], w[1], w[2], w[3]};
         }
       }
-      if (a.lse && valid) a.lse[at] = sees_any ? fmaf(m, 0.69314718f, logf(l)) : -INFINITY;
+      if (a.lse && valid && half == 0) a.lse[at] = sees_any ? fmaf(m, 0.69314718f, logf(l)) : -INFINITY;
     }
-  } else if (warp == kLoadWarp) {
+  } else {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
+  if (warp == kLoadWarp) {
     // ------------------------------------------------------------ loads
     if (lane == 0 && plan.count > 0) {
       const int tiles = plan.last[1] >= plan.first[1] ? 2 : 1;
@@ -333,143 +384,126 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
         for (int h = 0; h < 2; ++h)
           tma_tile_3d(base + t * kTileBytes + h * kHalf, &a.qmap, 64 * h, g * a.G + pass * a.q_heads,
                       s.q0 + token0 + t * a.q_tokens, bar(kBQ));
-      int n = 0;
-      for (; n < 2 * plan.count; ++n) {
-        if (n >= kStages && !wait(kBEmpty + n % kStages, (uint32_t)(n / kStages - 1) & 1u)) break;
-        const uint32_t full_bar = bar(kBFull + n % kStages);
-        const void* map = n & 1 ? &a.vmap : &a.kmap;
-        mbar_arrive_expect_tx(full_bar, kTileBytes);
-        for (int h = 0; h < 2; ++h) tma_tile_3d(ring(n) + h * kHalf, map, 64 * h, g, s.k0 + plan.key(n >> 1), full_bar);
+      // round i brings V of key tile i - 1 (tile 2 i - 1 of the ring) and K of key tile i (2 i); a tile of the ring is
+      // free when the round that used it last is done
+      int done = 0, i = 0;
+      bool ok = true;
+      for (; i <= plan.count && ok; ++i) {
+        const uint32_t full_bar = bar(kBFull + i % kRounds);
+        mbar_arrive_expect_tx(full_bar, ((i > 0) + (i < plan.count)) * kTileBytes);
+        for (int n = max(0, 2 * i - 1); n <= min(2 * i, 2 * plan.count - 1); ++n) {
+          for (const int used = (n - kStages + 1) >> 1; ok && n >= kStages && done <= used; ++done) ok = of_round(kBDone, done);
+          const void* map = n & 1 ? &a.vmap : &a.kmap;
+          // (on a wait that ran out the tile comes all the same: its barrier has been told of it)
+          for (int h = 0; h < 2; ++h) tma_tile_3d(ring(n) + h * kHalf, map, 64 * h, g, s.k0 + plan.key(n >> 1), full_bar);
+        }
       }
       if (misc[1]) {   // what is under way has to land before the CTA goes
         mbar_wait(bar(kBQ), 0u, a.err);
-        for (int x = max(0, n - kStages); x < n; ++x) mbar_wait(bar(kBFull + x % kStages), (uint32_t)(x / kStages) & 1u, a.err);
+        for (int x = max(0, i - kRounds); x < i; ++x) mbar_wait(bar(kBFull + x % kRounds), (uint32_t)(x / kRounds) & 1u, a.err);
       }
     }
-  } else if (warp == kMmaWarp) {
+  } else if (warp < kCheckWarp) {
     // ------------------------------------------------------------ products
     if (plan.count > 0) {
       constexpr uint32_t kIdescS = f16_idesc(DT, kRows, kKeys, false), kIdescO = f16_idesc(DT, kRows, kHeadDim, true);
-      // What to do in a round is worked out for 32 rounds at a time, a lane each: issuing products takes as long as the
-      // tensor cores take them, so arithmetic here is time in which they stand still (1085 of 3470 cycles a round).
-      // act[t], cut: key tiles i0 .. that tile t's rows see, and those that some row does not see whole
-      uint32_t act[kTiles] = {0u, 0u}, cut = 0u, act_before[kTiles] = {0u, 0u}, cut_before = 0u;
-      const int last[kTiles] = {plan.last_active(0), plan.last_active(1)};
-      const uint64_t q_desc = smem_desc_sw128(base), k_desc = smem_desc_sw128(base + kOffRing),
+      const int t = warp - kMmaWarp;
+      const int last = plan.last_active(t);
+      const uint64_t q_desc = smem_desc_sw128(base + t * kTileBytes), k_desc = smem_desc_sw128(base + kOffRing),
                      v_desc = smem_desc_sw128_mn(base + kOffRing, kHalf);
-      int slot_v = 1, slot_k = 0;           // ring slots of V of the round before, and of K
-      uint32_t phase_v = 0, phase_k = 0;
-      auto step = [&](int& slot, uint32_t& phase) {
-        slot += 2;
-        if (slot >= kStages) {
-          slot -= kStages;
-          phase ^= 1u;
-        }
-      };
-      uint32_t phase_p[kTiles] = {0u, 0u};
+      const uint32_t ts = tmem + kColS + t * kKeys, to = tmem + kColO + t * kHeadDim;
+      int slot_v = 1, slot_k = 0;           // of the ring, for V of the key tile before and for K
+      auto step = [&](int& slot) { slot = slot + 2 >= kStages ? slot + 2 - kStages : slot + 2; };
+      uint32_t phase_p = 0u;
       int checked = 0;
+      // what to do in a round is worked out for 32 rounds at a time, a lane each: key tiles that the rows of tile t see,
+      // and those that some row of the unit does not see whole
+      uint32_t act = 0u, cut = 0u, act_before = 0u, cut_before = 0u;
       bool ok = wait(kBQ, 0u);
       for (int i = 0; i <= plan.count; ++i) {
         if ((i & 31) == 0) {
           __syncwarp();
-          const int mine = i + lane, j0 = plan.key(mine);
-          const bool there = mine < plan.count;
-#pragma unroll
-          for (int t = 0; t < kTiles; ++t) {
-            act_before[t] = act[t] >> 31;
-            act[t] = __ballot_sync(0xffffffffu, there && plan.active(t, j0));
-          }
+          const int j0 = plan.key(i + lane);
+          const bool there = i + lane < plan.count;
+          act_before = act >> 31;
           cut_before = cut >> 31;
+          act = __ballot_sync(0xffffffffu, there && plan.active(t, j0));
           cut = __ballot_sync(0xffffffffu, there && plan.partial(j0));
         }
         const uint32_t check = i & 31 ? cut >> ((i - 1) & 31) & 1u : cut_before;
-        uint32_t pv[kTiles], qk[kTiles];
-#pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          qk[t] = act[t] >> (i & 31) & 1u;
-          pv[t] = i & 31 ? act[t] >> ((i - 1) & 31) & 1u : act_before[t];
-        }
+        const uint32_t pv = i & 31 ? act >> ((i - 1) & 31) & 1u : act_before, qk = act >> (i & 31) & 1u;
         if (lane != 0 || !ok) continue;
         const uint64_t v0 = v_desc + (uint32_t)(slot_v * (kTileBytes >> 4)), k0 = k_desc + (uint32_t)(slot_k * (kTileBytes >> 4));
-        if (i > 0) {
-          ok = wait(kBFull + slot_v, phase_v);
-          if (ok && check) {
-            ok = wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
-            ++checked;
-          }
+        ok = of_round(kBFull, i);
+        if (ok && check) {
+          ok = wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
+          ++checked;
         }
-        if (ok && i < plan.count) ok = wait(kBFull + slot_k, phase_k);
+        if (ok && pv) {   // O += P V
+          ok = wait(kBP + t, phase_p);
+          phase_p ^= 1u;
+        }
+        if (ok) ok = wait(kBTurn + t, t == 0 ? (uint32_t)(i & 1) ^ 1u : (uint32_t)i & 1u);
+        if (ok && pv) {
+          tc_fence_after();
 #pragma unroll
-        for (int t = 0; t < kTiles; ++t) {
-          if (ok && pv[t]) {   // O += P V
-            ok = wait(kBP + t, phase_p[t]);
-            phase_p[t] ^= 1u;
-            if (ok) {
-              tc_fence_after();
+          for (int k = 0; k < kKeys / 16; ++k) tc_mma_f16_ts(to, ts + 8 * k, v0 + (uint32_t)(k * (2048 >> 4)), kIdescO, 1u);
+          if (i - 1 == last) tc_commit(bar(kBO + t));
+        }
+        if (ok && qk) {   // S = Q K^T
+          tc_fence_after();
 #pragma unroll
-              for (int k = 0; k < kKeys / 16; ++k)
-                tc_mma_f16_ts(tmem + kColO + t * kHeadDim, tmem + kColS + t * kKeys + 8 * k, v0 + (uint32_t)(k * (2048 >> 4)),
-                              kIdescO, 1u);
-              if (i - 1 == last[t]) tc_commit(bar(kBO + t));
-            }
+          for (int k = 0; k < kHeadDim / 16; ++k) {
+            const uint32_t at = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
+            tc_mma_f16(ts, q_desc + at, k0 + at, kIdescS, k > 0 ? 1u : 0u);
           }
-          if (ok && qk[t]) {   // S = Q K^T
-            tc_fence_after();
-#pragma unroll
-            for (int k = 0; k < kHeadDim / 16; ++k) {
-              const uint32_t at = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
-              tc_mma_f16(tmem + kColS + t * kKeys, q_desc + (uint32_t)(t * (kTileBytes >> 4)) + at, k0 + at, kIdescS,
-                         k > 0 ? 1u : 0u);
-            }
-            tc_commit(bar(kBS + t));
-          }
+          tc_commit(bar(kBS + t));
         }
-        if (!ok) continue;
-        if (i > 0) {
-          tc_commit(bar(kBEmpty + slot_v));
-          step(slot_v, phase_v);
-        }
-        if (i < plan.count) {
-          tc_commit(bar(kBEmpty + slot_k));
-          step(slot_k, phase_k);
-        }
+        mbar_arrive(bar(kBTurn + 1 - t));   // the other tile's turn
+        if (ok) tc_commit(bar(kBDone + i % kRounds));
+        if (i > 0) step(slot_v);
+        step(slot_k);
       }
       if (!ok && lane == 0) {   // products under way end before the tensor memory is released
-        tc_commit(bar(kBQ));
-        mbar_wait(bar(kBQ), 1u, a.err);
+        tc_commit(bar(kBEnd + t));
+        mbar_wait(bar(kBEnd + t), 0u, a.err);
       }
     }
   } else {
     // ------------------------------------------------------------ checks
     int checked = 0;
-    bool ok = true;
-    for (int i = 0; i < plan.count && ok; ++i) {
-      // (every tile is waited for: the parity of a later use of a slot says nothing before the earlier one has landed)
-      ok = __all_sync(0xffffffffu, full(2 * i) && full(2 * i + 1));
+    bool ok = plan.count > 0;
+    for (int i = 0; i <= plan.count && ok; ++i) {
+      // (every round is waited for: the parity of a later use of a barrier says nothing before the earlier one is over)
+      ok = __all_sync(0xffffffffu, of_round(kBFull, i));
       if (!ok) break;
-      if (!plan.partial(plan.key(i))) continue;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int w = (warp - kCheckWarp) * 2 + e, r = 32 * w + lane;
+      const bool look = i > 0 && plan.partial(plan.key(i - 1));
+      const uint32_t v = ring(max(1, 2 * i - 1));
+      for (int w = 0; w < 4 && look; ++w) {
+        const int r = 32 * w + lane;
         bool bad = false;
 #pragma unroll 4
         for (int c = 0; c < 16; ++c) {
-          const uint4 v = lds128(ring(2 * i + 1) + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-          const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+          const uint4 x4 = lds128(v + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+          const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
           constexpr uint32_t kExp = DT == 0 ? 0x7c00u : 0x7f80u;
 #pragma unroll
           for (int y = 0; y < 4; ++y) bad = bad || (x[y] & kExp) == kExp || ((x[y] >> 16) & kExp) == kExp;
         }
         const uint32_t mask = __ballot_sync(0xffffffffu, bad);
         if (bad)
-          for (int c = 0; c < 16; ++c) sts128_zero(ring(2 * i + 1) + (c >> 3) * kHalf + r * 128 + (c & 7) * 16);
+          for (int c = 0; c < 16; ++c) sts128_zero(v + (c >> 3) * kHalf + r * 128 + (c & 7) * 16);
         if (mask) fence_proxy_async();
         if (lane == 0) masks[(checked % kMasks) * 4 + w] = mask;
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar(kBCheck + checked % kMasks));
-      ++checked;
+      if (lane == 0) {
+        if (look) mbar_arrive(bar(kBCheck + checked % kMasks));
+        mbar_arrive(bar(kBDone + i % kRounds));
+      }
+      checked += look;
     }
+  }
   }
   tc_fence_before();
   __syncthreads();
@@ -487,7 +521,17 @@ cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStre
   const int units = a.q_rows / (2 * a.q_tokens) + a.B;
   auto kern = dtype ? hill_prompt_attn_kernel<1> : hill_prompt_attn_kernel<0>;
   static int cache[2][64] = {{0}};
-  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), kSmem, cache[dtype ? 1 : 0]);
+  // the split of registers between the warps holds for what the kernel is launched with
+  static std::atomic<int> regs[2];
+  cudaError_t e;
+  if (regs[dtype ? 1 : 0].load(std::memory_order_relaxed) == 0) {
+    cudaFuncAttributes attr;
+    e = cudaFuncGetAttributes(&attr, kern);
+    if (e != cudaSuccess) return e;
+    if (attr.numRegs < kRegs) return cudaErrorInvalidConfiguration;
+    regs[dtype ? 1 : 0].store(attr.numRegs, std::memory_order_relaxed);
+  }
+  e = ensure_smem_attr(reinterpret_cast<const void*>(kern), kSmem, cache[dtype ? 1 : 0]);
   if (e != cudaSuccess) return e;
   return launch_pdl(kern, dim3((unsigned)units * a.Hkv * a.passes), dim3(kThreads), kSmem, st, 0, a, units);
 }

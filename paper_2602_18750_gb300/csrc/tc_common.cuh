@@ -117,6 +117,29 @@ __device__ __forceinline__ void tma_tile_3d(uint32_t dst, const void* tmap, int 
       : "memory");
 }
 
+// As mbar_wait, for waits of whole phases of work: the warp sleeps up to 100 us at a time instead of asking again and
+// again, which takes the queue that the exponentials and the loads of tensor memory go through.
+__device__ __forceinline__ bool mbar_try_wait_long(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(100000u)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ bool mbar_wait_long(uint32_t bar, uint32_t parity, unsigned* err) {
+  const unsigned long long t0 = global_ns();
+  while (!mbar_try_wait_long(bar, parity))
+    if (global_ns() - t0 > kWaitLimitNs) {
+      raise_error(err, kErrTimeout);
+      return false;
+    }
+  return true;
+}
+
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 }  // namespace
