@@ -102,6 +102,19 @@ __device__ __forceinline__ bool tile_any(int id, bool x) {
   return any != 0;
 }
 
+// What the key tiles from i on are to tile t, worked out for 32 at a time, a lane each: whether its rows see them, see them
+// whole, and whether some row of the unit does not see them whole.
+struct Ahead {
+  uint32_t act = 0u, full = 0u, cut = 0u;
+  __device__ __forceinline__ void look(const Plan& plan, int t, int i, int lane) {
+    const int j0 = plan.key(i + lane);
+    const bool there = i + lane < plan.count;
+    act = __ballot_sync(0xffffffffu, there && plan.active(t, j0));
+    full = __ballot_sync(0xffffffffu, there && plan.full(t, j0));
+    cut = __ballot_sync(0xffffffffu, there && plan.partial(j0));
+  }
+};
+
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units) {
   extern __shared__ __align__(1024) unsigned char mem[];
@@ -215,14 +228,15 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     }
     int n = 0, checked = 0;
     bool ok = true;
+    Ahead ahead;
     for (int i = 0; i < plan.count; ++i) {
-      const int j0 = plan.key(i);
-      const bool part = plan.partial(j0);
-      if (!plan.active(t, j0)) {
+      if ((i & 31) == 0) ahead.look(plan, t, i, lane);
+      const bool part = ahead.cut >> (i & 31) & 1u, whole = ahead.full >> (i & 31) & 1u;
+      if (!(ahead.act >> (i & 31) & 1u)) {
         checked += part;
         continue;
       }
-      const bool whole = plan.full(t, j0);
+      const int j0 = plan.key(i);
       // the keys that the row sees, as bits
       uint32_t vis[2] = {~0u, ~0u};
       if (!whole) {
@@ -416,22 +430,17 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       auto step = [&](int& slot) { slot = slot + 2 >= kStages ? slot + 2 - kStages : slot + 2; };
       uint32_t phase_p = 0u;
       int checked = 0;
-      // what to do in a round is worked out for 32 rounds at a time, a lane each: key tiles that the rows of tile t see,
-      // and those that some row of the unit does not see whole
-      uint32_t act = 0u, cut = 0u, act_before = 0u, cut_before = 0u;
+      Ahead ahead;
+      uint32_t act_before = 0u, cut_before = 0u;
       bool ok = wait(kBQ, 0u);
       for (int i = 0; i <= plan.count; ++i) {
         if ((i & 31) == 0) {
           __syncwarp();
-          const int j0 = plan.key(i + lane);
-          const bool there = i + lane < plan.count;
-          act_before = act >> 31;
-          cut_before = cut >> 31;
-          act = __ballot_sync(0xffffffffu, there && plan.active(t, j0));
-          cut = __ballot_sync(0xffffffffu, there && plan.partial(j0));
+          ahead.look(plan, t, i, lane);
         }
-        const uint32_t check = i & 31 ? cut >> ((i - 1) & 31) & 1u : cut_before;
-        const uint32_t pv = i & 31 ? act >> ((i - 1) & 31) & 1u : act_before, qk = act >> (i & 31) & 1u;
+        const uint32_t check = cut_before, pv = act_before, qk = ahead.act >> (i & 31) & 1u;
+        act_before = qk;
+        cut_before = ahead.cut >> (i & 31) & 1u;
         if (lane != 0 || !ok) continue;
         const uint64_t v0 = v_desc + (uint32_t)(slot_v * (kTileBytes >> 4)), k0 = k_desc + (uint32_t)(slot_k * (kTileBytes >> 4));
         ok = of_round(kBFull, i);
@@ -473,11 +482,15 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     // ------------------------------------------------------------ checks
     int checked = 0;
     bool ok = plan.count > 0;
+    Ahead ahead;
+    uint32_t cut_before = 0u;
     for (int i = 0; i <= plan.count && ok; ++i) {
+      if ((i & 31) == 0) ahead.look(plan, 0, i, lane);
+      const bool look = cut_before;
+      cut_before = ahead.cut >> (i & 31) & 1u;
       // (every round is waited for: the parity of a later use of a barrier says nothing before the earlier one is over)
       ok = __all_sync(0xffffffffu, of_round(kBFull, i));
       if (!ok) break;
-      const bool look = i > 0 && plan.partial(plan.key(i - 1));
       const uint32_t v = ring(max(1, 2 * i - 1));
       for (int w = 0; w < 4 && look; ++w) {
         const int r = 32 * w + lane;
