@@ -432,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       int checked = 0;
       Ahead ahead;
       uint32_t act_before = 0u, cut_before = 0u;
-      bool ok = wait(kBQ, 0u);
+      bool ok = lane != 0 || wait(kBQ, 0u);
       for (int i = 0; i <= plan.count; ++i) {
         if ((i & 31) == 0) {
           __syncwarp();
@@ -492,17 +492,24 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       ok = __all_sync(0xffffffffu, of_round(kBFull, i));
       if (!ok) break;
       const uint32_t v = ring(max(1, 2 * i - 1));
+#pragma unroll 1
       for (int w = 0; w < 4 && look; ++w) {
         const int r = 32 * w + lane;
-        bool bad = false;
-#pragma unroll 4
+        // 0 * x summed: not a number where an x is not finite
+        using T2 = typename std::conditional<DT == 0, __half2, __nv_bfloat162>::type;
+        const uint32_t none = 0u;
+        const T2 zero = *reinterpret_cast<const T2*>(&none);
+        T2 sum[4] = {zero, zero, zero, zero};
+#pragma unroll
         for (int c = 0; c < 16; ++c) {
           const uint4 x4 = lds128(v + (c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
           const uint32_t x[4] = {x4.x, x4.y, x4.z, x4.w};
-          constexpr uint32_t kExp = DT == 0 ? 0x7c00u : 0x7f80u;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) bad = bad || (x[y] & kExp) == kExp || ((x[y] >> 16) & kExp) == kExp;
+          for (int y = 0; y < 4; ++y) sum[y] = __hfma2(*reinterpret_cast<const T2*>(&x[y]), zero, sum[y]);
         }
+        const T2 all = __hadd2(__hadd2(sum[0], sum[1]), __hadd2(sum[2], sum[3]));
+        const float2 f = unpack2<DT>(*reinterpret_cast<const uint32_t*>(&all));
+        const bool bad = !(f.x == 0.f && f.y == 0.f);
         const uint32_t mask = __ballot_sync(0xffffffffu, bad);
         if (bad)
           for (int c = 0; c < 16; ++c) sts128_zero(v + (c >> 3) * kHalf + r * 128 + (c & 7) * 16);
