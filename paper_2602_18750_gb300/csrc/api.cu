@@ -1211,7 +1211,7 @@ namespace hill {
 namespace {
 
 constexpr int kRowsMax = 1 << 30;     // positions and sums of positions and windows stay in 32 bits
-constexpr int kTileRows = 128;        // query rows of a tile (query heads x tokens), keys of a tile
+constexpr int kTileRows = 128;        // query rows of a tile (query heads x tokens)
 
 hill_status check_packed(const hill_packed* d) {
   if (!d) return HILL_ERR_INVALID_ARG;
@@ -1250,9 +1250,9 @@ hill_status make_rows_map(int dtype, const void* p, int heads, int64_t rows, int
   return r == CUDA_SUCCESS ? HILL_OK : HILL_ERR_UNSUPPORTED;
 }
 
-// What both calls over prompts take; the maps (v may be NULL).
+// What both calls over prompts take; the maps (v may be NULL), keys by tiles of tile_keys.
 hill_status prompt_args(const hill_packed* d, const void* q, const void* k, const void* v, const int32_t* q_start,
-                        const int32_t* k_start, int32_t sinks, int32_t window, PromptArgs* a) {
+                        const int32_t* k_start, int32_t sinks, int32_t window, int tile_keys, PromptArgs* a) {
   a->q = q;
   a->k = k;
   a->v = v;
@@ -1277,9 +1277,9 @@ hill_status prompt_args(const hill_packed* d, const void* q, const void* k, cons
   a->window = std::min(window, kRowsMax);
   hill_status s = make_rows_map(d->dtype, q, a->H, a->q_rows, a->q_sh, a->q_st, a->q_heads, a->q_tokens, &a->qmap);
   // (without keys nothing is read through these)
-  if (s == HILL_OK) s = make_rows_map(d->dtype, d->k_rows ? k : q, a->Hkv, a->k_rows, a->k_sh, a->k_st, 1, kTileRows, &a->kmap);
+  if (s == HILL_OK) s = make_rows_map(d->dtype, d->k_rows ? k : q, a->Hkv, a->k_rows, a->k_sh, a->k_st, 1, tile_keys, &a->kmap);
   if (s == HILL_OK && v)
-    s = make_rows_map(d->dtype, d->k_rows ? v : q, a->Hkv, a->k_rows, a->v_sh, a->v_st, 1, kTileRows, &a->vmap);
+    s = make_rows_map(d->dtype, d->k_rows ? v : q, a->Hkv, a->k_rows, a->v_sh, a->v_st, 1, tile_keys, &a->vmap);
   return s;
 }
 
@@ -1369,7 +1369,7 @@ hill_status hill_prompt_attn(const hill_packed* desc, const void* q, const void*
   DeviceInfo di;
   if (device_info(&di) != cudaSuccess) return HILL_ERR_CUDA;
   PromptArgs a{};
-  s = prompt_args(desc, q, k, v ? v : q, q_start, k_start, sinks, window, &a);
+  s = prompt_args(desc, q, k, v ? v : q, q_start, k_start, sinks, window, prompt_tile_keys(), &a);
   if (s != HILL_OK) return s;
   a.out = out;
   a.lse = lse;
@@ -1401,7 +1401,7 @@ hill_status hill_prompt_importance(const hill_packed* desc, const void* q, const
   const PromptLayout L = prompt_layout(desc, di.sms);
   if (!ws || ws_bytes < L.total) return HILL_ERR_WORKSPACE;
   PromptArgs a{};
-  s = prompt_args(desc, q, k, nullptr, q_start, k_start, sinks, window, &a);
+  s = prompt_args(desc, q, k, nullptr, q_start, k_start, sinks, window, importance_tile_keys(), &a);
   if (s != HILL_OK) return s;
   a.newest = std::min(newest, kRowsMax);
   a.lse = const_cast<float*>(lse);

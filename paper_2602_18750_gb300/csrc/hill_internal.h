@@ -206,7 +206,7 @@ struct BlockInfo;   // importance.cu
 // Prompts: packed rows of several sequences (prompt.cu, importance.cu).
 struct PromptArgs {
   CUtensorMap qmap, kmap, vmap;   // 3-D (head dimension, head, row), 128-byte swizzle; boxes of 64 dims x q_heads x
-                                  // q_tokens query rows, 64 dims x 1 x 128 keys
+                                  // q_tokens query rows, 64 dims x 1 x a tile of keys
   const void* q;
   const void* k;
   const void* v;
@@ -381,9 +381,11 @@ cudaError_t launch_paged_write(const PagesArgs& a, int dtype, cudaStream_t st);
 cudaError_t launch_paged_read(const PagesArgs& a, int dtype, int max_rows, cudaStream_t st);
 
 // prompt.cu
+int prompt_tile_keys();
 cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels);
 
 // importance.cu
+int importance_tile_keys();
 struct ImportanceSpace {   // bytes of workspace
   size_t part, info;
 };

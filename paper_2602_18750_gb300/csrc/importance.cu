@@ -421,6 +421,8 @@ int64_t most_blocks(int B, int64_t k_rows) { return k_rows / kBlock + B; }
 
 }  // namespace
 
+int importance_tile_keys() { return kKeys; }
+
 ImportanceSpace importance_space(int B, int Hkv, int64_t k_rows, int sms) {
   ImportanceSpace s;
   s.part = (size_t)(Hkv * most_blocks(B, k_rows) + sms) * kBlock * sizeof(float);

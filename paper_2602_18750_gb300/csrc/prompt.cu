@@ -3,25 +3,28 @@
 //
 // A unit is two tiles of 128 query rows of one KV head -- a row is a (token, query head of the group), token by
 // token, so the heads of a group share each key tile -- and walks the 128-key tiles that its rows see: those of the
-// sinks, then those of the window up to the diagonal.  One CTA per unit, 20 warps:
+// sinks, then those of the window up to the diagonal.  One CTA per unit, 12 warps:
 //
-//   softmax   (warps 0-7, 8-15: a tile each, a thread per half row) reads S = Q K^T from tensor memory, forms
-//             p = 2^(z - m) and puts it back there in the type of V, over S;
-//   loads     (warp 16) the Q tiles once, K and V tiles in a ring, by TMA (128-byte swizzle);
-//   products  (warps 17, 18) a thread for each tile issues S = Q K^T (both operands in shared memory) and O += P V (P in
-//             tensor memory, V with the head dimension contiguous), in turns: while one tile's softmax runs, the tensor cores
-//             have the other's P V and next S;
-//   checks    (warp 19) of V tiles that some row sees only a part of: rows of V that are not finite.
+//   softmax   (warps 0-3, 4-7: a tile each, a thread per row) reads S = Q K^T from tensor memory, forms p = 2^(z - m)
+//             and puts it back there in the type of V, over S;
+//   loads     (warp 8) the Q tiles once, K and V tiles in a ring, by TMA (128-byte swizzle);
+//   products  (warps 9, 10) a thread for each tile issues O += P V (P in tensor memory, V with the head dimension
+//             contiguous) and the next S = Q K^T (both operands in shared memory), in turns: while one tile's softmax
+//             runs, the tensor cores have the other's products;
+//   checks    (warp 11) of V tiles that some row sees only a part of: rows of V that are not finite.
 //
-// What keeps the tensor cores waiting is looked at in cycles of a round (both tiles, 2048 of products), on 8K tokens of
-// 32 heads.  Issuing takes as long as the tensor cores take the products, so whatever else an issuing thread does -- waits,
-// commits, 1400 cycles a round -- is time in which they stand still: one thread for both tiles 4100.  Two threads
-// without turns 4600: the tiles fall into step, and both softmaxes run while nothing is there to multiply.
+// Tensor memory holds S and O of both tiles, 4 x 128 columns, all there is.
 //
 // Round i of a tile is O += P V of key tile i - 1 and S of key tile i; V of the one and K of the other come, and are
 // given back, together.
 //
-// Tensor memory holds S and O of both tiles, 4 x 128 columns, all there is.
+// Measured, 16K tokens of 32 heads (1183 us at the rate of a library product; both tiles' products of a round are 2048 cycles):
+// 1667 us, 1.32 PFLOP/s.  Issuing takes as long as the tensor cores take the products, so whatever else an issuing
+// thread does (waits, commits: 1400 cycles a round) is time in which they stand still: one thread for both tiles 1920 us,
+// two without turns 2170 (the tiles fall into step, and both softmaxes run while nothing is there to multiply).  Half a
+// row to a thread, 16 softmax warps: 1770, a vote of the halves on the maximum costs what it gains.  Key tiles of 64,
+// with two S a tile so that the next is issued before P V: 1857, the steps from barrier to barrier are twice as many.
+// What bounds it now is the chain of a tile, S to softmax (about 1300 cycles) to P V and S.
 //
 // The running maximum m of a row is set 7 below its largest logit (base 2) and raised only when the weights of a
 // tile sum to more than 2^15: no maximum is searched for, and O is not rescaled, until then.  Since S of a tile is
@@ -32,7 +35,6 @@
 // A hidden key has p = 0, and a hidden value must not reach O by 0 * NaN.  In tiles that some row does not see whole, rows
 // of V that are not finite are set to zero in shared memory before the product, and the rows that see them add
 // p v themselves.
-#include <atomic>
 #include <type_traits>
 
 #include "prompt_common.cuh"
@@ -42,26 +44,22 @@ namespace hill {
 namespace {
 
 constexpr int kRows = 128, kKeys = 128, kTiles = 2;
-constexpr int kStages = 5;                       // ring of K and V tiles
-constexpr int kHalf = kKeys * 128;               // 64 dims of 128 rows
-constexpr int kTileBytes = 2 * kHalf;
+constexpr int kQHalf = kRows * 128, kQBytes = 2 * kQHalf;       // 64 dims of a tile of query rows; all
+constexpr int kHalf = kKeys * 128, kTileBytes = 2 * kHalf;      // the same of a key tile
+constexpr int kStages = 5;                      // ring of K and V tiles
 constexpr int kMasks = 4;                        // ring of the checks' results
-constexpr int kSoftmaxWarps = 8 * kTiles, kLoadWarp = kSoftmaxWarps, kMmaWarp = kLoadWarp + 1, kCheckWarp = kMmaWarp + kTiles;
+constexpr int kSoftmaxWarps = 4 * kTiles, kLoadWarp = kSoftmaxWarps, kMmaWarp = kLoadWarp + 1, kCheckWarp = kMmaWarp + kTiles;
 constexpr int kThreads = (kCheckWarp + 1) * 32;
 constexpr int kRounds = 4;                       // rounds whose barriers are told apart
 
-constexpr int kOffRing = kTiles * kTileBytes;
+constexpr int kOffRing = kTiles * kQBytes;
 constexpr int kOffBars = kOffRing + kStages * kTileBytes;
-// barriers: Q; a round's K and V there, given back; S full, P ready, O done of each tile; checks
-constexpr int kBQ = 0, kBFull = 1, kBDone = kBFull + kRounds, kBS = kBDone + kRounds, kBP = kBS + kTiles, kBO = kBP + kTiles,
-              kBCheck = kBO + kTiles, kBEnd = kBCheck + kMasks, kBTurn = kBEnd + kTiles, kBars = kBTurn + kTiles;
+// barriers: Q; a round's K and V there, given back; S full, P ready of each tile; checks; the end; turns
+constexpr int kBQ = 0, kBFull = 1, kBDone = kBFull + kRounds, kBS = kBDone + kRounds, kBP = kBS + kTiles,
+              kBCheck = kBP + kTiles, kBEnd = kBCheck + kMasks, kBTurn = kBEnd + kTiles, kBars = kBTurn + kTiles;
 constexpr int kOffMasks = kOffBars + ((kBars * 8 + 15) & ~15);
 constexpr int kOffMisc = kOffMasks + kMasks * 16;   // tensor memory address, abort flag, unit
-constexpr int kOffPeer = kOffMisc + 16;             // [tile][half][row] what the halves of a row tell each other
-constexpr int kSmem = kOffPeer + kTiles * 2 * kRows * 4;
-// registers of a thread: at launch, and then of the softmax warps and of the others
-constexpr int kRegs = 96, kRegsSoftmax = 104, kRegsOther = 64;
-static_assert(kSoftmaxWarps * kRegsSoftmax + (kThreads / 32 - kSoftmaxWarps) * kRegsOther <= kThreads / 32 * kRegs, "registers");
+constexpr int kSmem = kOffMisc + 16;
 static_assert(kSmem <= 232448, "shared memory");
 
 constexpr uint32_t kColS = 0, kColO = kTiles * kKeys, kCols = 512;
@@ -84,23 +82,7 @@ struct Plan {
     for (int t = 0; t < kTiles; ++t) p = p || (active(t, j0) && !full(t, j0));
     return p;
   }
-  __device__ __forceinline__ int last_active(int t) const {
-    int i = count - 1;
-    while (i >= 0 && !active(t, key(i))) --i;
-    return i;
-  }
 };
-
-// Does x hold for any of the 256 threads that meet at barrier `id`?
-__device__ __forceinline__ bool tile_any(int id, bool x) {
-  int any;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.s32 p, %1, 0;\n\tbar.red.or.pred q, %2, 256, p;\n\tselp.s32 %0, 1, 0, q;\n\t}"
-      : "=r"(any)
-      : "r"((int)x), "r"(id)
-      : "memory");
-  return any != 0;
-}
 
 // What the key tiles from i on are to tile t, worked out for 32 at a time, a lane each: whether its rows see them, see them
 // whole, and whether some row of the unit does not see them whole.
@@ -160,10 +142,9 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     }
     for (int t = 0; t < kTiles; ++t) {
       mbar_init(bar(kBS + t), 1);
-      mbar_init(bar(kBP + t), 8);
-      mbar_init(bar(kBTurn + t), 1);
-      mbar_init(bar(kBO + t), 1);
+      mbar_init(bar(kBP + t), 4);
       mbar_init(bar(kBEnd + t), 1);
+      mbar_init(bar(kBTurn + t), 1);
     }
     for (int i = 0; i < kMasks; ++i) mbar_init(bar(kBCheck + i), 1);
     fence_barrier_init();
@@ -206,24 +187,22 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   auto of_round = [&](int first, int i) { return wait(first + i % kRounds, (uint32_t)(i / kRounds) & 1u); };
 
   if (warp < kSoftmaxWarps) {
-    // ------------------------------------------------------------ softmax of half the columns of a tile
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegsSoftmax));
-    const int t = warp >> 3, half = (warp >> 2) & 1;
+    // ------------------------------------------------------------ softmax of a tile
+    const int t = warp >> 2;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-    const uint32_t ts = tmem + lanes + kColS + t * kKeys, to = tmem + lanes + kColO + t * kHeadDim + 64 * half;
+    const uint32_t ts = tmem + lanes + kColS + t * kKeys, to = tmem + lanes + kColO + t * kHeadDim;
     const int row = (warp & 3) * 32 + lane, tok = row / a.q_heads, hg = pass * a.q_heads + row - tok * a.q_heads;
     const int i_tok = token0 + t * a.q_tokens + tok;
     const bool valid = b >= 0 && tok < a.q_tokens && hg < a.G && i_tok < s.n;
     const int pos = i_tok + shift;
     const float2 c2 = both(valid ? kLog2eInvSqrtD : 0.f);   // (a row that is none has logits of 0)
-    float* const peer = reinterpret_cast<float*>(mem + kOffPeer) + t * 2 * kRows + row;   // [half]
-    float m = kNegHuge, l = 0.f;   // of the row; of this half
+    float m = kNegHuge, l = 0.f;
     {
       uint32_t zero[32];
 #pragma unroll
       for (int i = 0; i < 32; ++i) zero[i] = 0u;
-      tc_st32(to, zero);
-      tc_st32(to + 32, zero);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tc_st32(to + 32 * c, zero);
       tc_wait_st();
     }
     int n = 0, checked = 0;
@@ -238,46 +217,41 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       }
       const int j0 = plan.key(i);
       // the keys that the row sees, as bits
-      uint32_t vis[2] = {~0u, ~0u};
+      uint32_t vis[4] = {~0u, ~0u, ~0u, ~0u};
       if (!whole) {
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const int k0 = j0 + 64 * half + 32 * w;
+        for (int w = 0; w < 4; ++w) {
+          const int k0 = j0 + 32 * w;
           vis[w] = valid ? bits_to(pos - k0) & (bits_to(a.sinks - 1 - k0) | ~bits_to(pos - k0 - a.window)) : 0u;
         }
       }
-      ok = wait(kBS + t, (uint32_t)n & 1u);
-      const uint32_t* const mask = masks + (checked % kMasks) * 4;
-      if (part) {
-        ok = ok && wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
-        ++checked;
-      }
-      ok = __all_sync(0xffffffffu, ok);
+      ok = __all_sync(0xffffffffu, wait(kBS + t, (uint32_t)n & 1u));
+      if (!ok) break;
       tc_fence_after();
-      uint32_t p[32];
+      uint32_t p[64];
       float sum;
       for (int again = 0;; ++again) {
         auto weights = [&](auto masked_tag) {
           constexpr bool kMasked = decltype(masked_tag)::value;
           const float2 m2 = both(-m);
           float2 sums[2] = {both(0.f), both(0.f)};
-          uint32_t sv[2][16];
-          tc_ld16(ts + 64 * half, sv[0]);
+          uint32_t sv[2][32];
+          tc_ld32(ts, sv[0]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             tc_wait_ld();
-            if (c < 3) tc_ld16(ts + 64 * half + 16 * (c + 1), sv[(c + 1) & 1]);
+            if (c < 3) tc_ld32(ts + 32 * (c + 1), sv[(c + 1) & 1]);
 #pragma unroll
-            for (int k = 0; k < 16; k += 2) {
+            for (int k = 0; k < 32; k += 2) {
               float2 z{__uint_as_float(sv[c & 1][k]), __uint_as_float(sv[c & 1][k + 1])};
               if (kMasked) {
-                z.x = (vis[c >> 1] >> (16 * (c & 1) + k)) & 1u ? z.x : -INFINITY;
-                z.y = (vis[c >> 1] >> (16 * (c & 1) + k + 1)) & 1u ? z.y : -INFINITY;
+                z.x = (vis[c] >> k) & 1u ? z.x : -INFINITY;
+                z.y = (vis[c] >> (k + 1)) & 1u ? z.y : -INFINITY;
               }
               const float2 x = fma2(z, c2, m2);
               const float2 e{ex2(x.x), ex2(x.y)};
               sums[(k >> 1) & 1] = add2(sums[(k >> 1) & 1], e);
-              p[c * 8 + (k >> 1)] = pack2<DT>(e.x, e.y);
+              p[c * 16 + (k >> 1)] = pack2<DT>(e.x, e.y);
             }
           }
           const float2 s2 = add2(sums[0], sums[1]);
@@ -285,66 +259,59 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
         };
         if (whole) weights(std::false_type{});
         else weights(std::true_type{});
-        // From here on S may be written over, where no weight of the tile is past 2^15.  (All threads of the tile
-        // come here whatever happens; a wait that ran out for one ends the work of all.)
-        const bool over = sum > 32768.f;
-        const bool vote = tile_any(1 + t, over || !ok);
-        if (again || !vote) break;
-        ok = !tile_any(1 + t, !ok);
-        if (!ok) break;
-        // the maximum is raised, what the old one has given shrinks (a row whose weights are within keeps its maximum:
-        // what one row sees changes no bit of another's)
+        if (again || !__any_sync(0xffffffffu, sum > 32768.f)) break;
+        // a weight may be past 2^15: the maximum is raised, what the old one has given shrinks (all of it is there: S of
+        // this key tile came after the P V before it).  A row whose weights are within keeps its maximum: what one row sees
+        // changes no bit of another's.
         float top = -INFINITY;
         uint32_t sv[32];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          tc_ld32(ts + 64 * half + 32 * c, sv);
-          tc_landed(sv);
+        for (int c = 0; c < 4; ++c) {
+          tc_ld32(ts + 32 * c, sv);
+          tc_wait_ld();
 #pragma unroll
           for (int k = 0; k < 32; ++k)
             if ((vis[c] >> k) & 1u) top = fmaxf(top, __uint_as_float(sv[k]) * c2.x);
         }
-        peer[half * kRows] = over ? top : -INFINITY;
-        named_sync(1 + t, 256);
-        const float mn = fmaxf(m, fmaxf(peer[0], peer[kRows]) - 7.f), f = ex2(m - mn);
+        const float mn = sum > 32768.f ? fmaxf(m, top - 7.f) : m, f = ex2(m - mn);
         m = mn;
         l *= f;
-        for (int c = 0; c < 2 && n > 0; ++c) {
+        for (int c = 0; c < 4 && n > 0; ++c) {
           tc_ld32(to + 32 * c, sv);
-          tc_landed(sv);
+          tc_wait_ld();
 #pragma unroll
           for (int k = 0; k < 32; ++k) sv[k] = __float_as_uint(__uint_as_float(sv[k]) * f);
           tc_st32(to + 32 * c, sv);
         }
       }
-      if (!ok) break;
       l += sum;
-      tc_st32(ts + 32 * half, p);
+      tc_st32(ts, p);
+      tc_st32(ts + 32, p + 32);
       tc_wait_st();
       if (part) {
+        ok = __all_sync(0xffffffffu, wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u));
+        if (!ok) break;
+        const uint32_t* const mask = masks + (checked % kMasks) * 4;
+        ++checked;
         if (mask[0] | mask[1] | mask[2] | mask[3]) {
           // values that are not finite: the rows that see them take p v
-          tc_fence_before();
-          named_sync(1 + t, 256);   // both halves of p are there
-          tc_fence_after();
           for (int w = 0; w < 4; ++w) {
             for (uint32_t bad = mask[w]; bad; bad &= bad - 1u) {
               const int k = __ffs(bad) - 1, j = j0 + 32 * w + k;
               const float2 pk = unpack2<DT>(tc_ld1(ts + 16 * w + (k >> 1)));
               const bool see = valid && j <= pos && (j < a.sinks || j > pos - a.window);
               const float pw = k & 1 ? pk.y : pk.x;
-              const auto* v = static_cast<const uint16_t*>(a.v) + (int64_t)(s.k0 + j) * a.v_st + (int64_t)g * a.v_sh + 64 * half;
-              for (int c = 0; c < 2; ++c) {
+              const auto* v = static_cast<const uint16_t*>(a.v) + (int64_t)(s.k0 + j) * a.v_st + (int64_t)g * a.v_sh;
+              for (int c = 0; c < 4; ++c) {
                 uint32_t sv[32];
                 tc_ld32(to + 32 * c, sv);
-                tc_landed(sv);
+                tc_wait_ld();
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
+                  if (!see) continue;
                   const float2 x = unpack2<DT>(*reinterpret_cast<const uint32_t*>(v + 32 * c + e));
-                  if (see) {
-                    sv[e] = __float_as_uint(fmaf(pw, x.x, __uint_as_float(sv[e])));
-                    sv[e + 1] = __float_as_uint(fmaf(pw, x.y, __uint_as_float(sv[e + 1])));
-                  }
+                  sv[e] = __float_as_uint(fmaf(pw, x.x, __uint_as_float(sv[e])));
+                  sv[e + 1] = __float_as_uint(fmaf(pw, x.y, __uint_as_float(sv[e + 1])));
                 }
                 tc_st32(to + 32 * c, sv);
               }
@@ -358,23 +325,20 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       if (lane == 0) mbar_arrive(bar(kBP + t));
       ++n;
     }
-    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(kBO + t, 0u));
-    if (!tile_any(1 + t, !ok) && b >= 0) {
+    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(kBEnd + t, 0u));
+    if (ok && b >= 0) {
       tc_fence_after();
-      peer[half * kRows] = l;
-      named_sync(1 + t, 256);
-      l = peer[0] + peer[kRows];
       // does the row see anything?
       const bool sees_any = pos >= 0 && (a.window > 0 || a.sinks > 0);
       const float inv = sees_any ? 1.f / l : 0.f;
       const int64_t at = (int64_t)(s.q0 + i_tok) * a.H + g * a.G + hg;
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < 4; ++c) {
         uint32_t sv[32];
         tc_ld32(to + 32 * c, sv);
-        tc_landed(sv);
+        tc_wait_ld();
         if (!valid) continue;
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * kHeadDim + 64 * half + 32 * c);
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * kHeadDim + 32 * c);
 #pragma unroll
         for (int e = 0; e < 32; e += 8) {
           uint32_t w[4];
@@ -384,11 +348,9 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
           dst[e / 8] = uint4{w[0], w[1], w[2], w[3]};
         }
       }
-      if (a.lse && valid && half == 0) a.lse[at] = sees_any ? fmaf(m, 0.69314718f, logf(l)) : -INFINITY;
+      if (a.lse && valid) a.lse[at] = sees_any ? fmaf(m, 0.69314718f, logf(l)) : -INFINITY;
     }
-  } else {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
-  if (warp == kLoadWarp) {
+  } else if (warp == kLoadWarp) {
     // ------------------------------------------------------------ loads
     if (lane == 0 && plan.count > 0) {
       const int tiles = plan.last[1] >= plan.first[1] ? 2 : 1;
@@ -396,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       mbar_arrive_expect_tx(bar(kBQ), tiles * 2 * q_bytes);
       for (int t = 0; t < tiles; ++t)
         for (int h = 0; h < 2; ++h)
-          tma_tile_3d(base + t * kTileBytes + h * kHalf, &a.qmap, 64 * h, g * a.G + pass * a.q_heads,
+          tma_tile_3d(base + t * kQBytes + h * kQHalf, &a.qmap, 64 * h, g * a.G + pass * a.q_heads,
                       s.q0 + token0 + t * a.q_tokens, bar(kBQ));
       // round i brings V of key tile i - 1 (tile 2 i - 1 of the ring) and K of key tile i (2 i); a tile of the ring is
       // free when the round that used it last is done
@@ -422,13 +384,12 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     if (plan.count > 0) {
       constexpr uint32_t kIdescS = f16_idesc(DT, kRows, kKeys, false), kIdescO = f16_idesc(DT, kRows, kHeadDim, true);
       const int t = warp - kMmaWarp;
-      const int last = plan.last_active(t);
-      const uint64_t q_desc = smem_desc_sw128(base + t * kTileBytes), k_desc = smem_desc_sw128(base + kOffRing),
+      const uint64_t q_desc = smem_desc_sw128(base + t * kQBytes), k_desc = smem_desc_sw128(base + kOffRing),
                      v_desc = smem_desc_sw128_mn(base + kOffRing, kHalf);
       const uint32_t ts = tmem + kColS + t * kKeys, to = tmem + kColO + t * kHeadDim;
+      uint32_t phase_p = 0u;
       int slot_v = 1, slot_k = 0;           // of the ring, for V of the key tile before and for K
       auto step = [&](int& slot) { slot = slot + 2 >= kStages ? slot + 2 - kStages : slot + 2; };
-      uint32_t phase_p = 0u;
       int checked = 0;
       Ahead ahead;
       uint32_t act_before = 0u, cut_before = 0u;
@@ -448,23 +409,22 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
           ok = wait(kBCheck + checked % kMasks, (uint32_t)(checked / kMasks) & 1u);
           ++checked;
         }
-        if (ok && pv) {   // O += P V
+        if (ok && pv) {
           ok = wait(kBP + t, phase_p);
           phase_p ^= 1u;
         }
         if (ok) ok = wait(kBTurn + t, t == 0 ? (uint32_t)(i & 1) ^ 1u : (uint32_t)i & 1u);
-        if (ok && pv) {
+        if (ok && pv) {   // O += P V
           tc_fence_after();
 #pragma unroll
           for (int k = 0; k < kKeys / 16; ++k) tc_mma_f16_ts(to, ts + 8 * k, v0 + (uint32_t)(k * (2048 >> 4)), kIdescO, 1u);
-          if (i - 1 == last) tc_commit(bar(kBO + t));
         }
         if (ok && qk) {   // S = Q K^T
           tc_fence_after();
 #pragma unroll
           for (int k = 0; k < kHeadDim / 16; ++k) {
-            const uint32_t at = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
-            tc_mma_f16(ts, q_desc + at, k0 + at, kIdescS, k > 0 ? 1u : 0u);
+            const uint32_t aq = ((k >> 2) * kQHalf + (k & 3) * 32) >> 4, ak = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
+            tc_mma_f16(ts, q_desc + aq, k0 + ak, kIdescS, k > 0 ? 1u : 0u);
           }
           tc_commit(bar(kBS + t));
         }
@@ -473,9 +433,9 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
         if (i > 0) step(slot_v);
         step(slot_k);
       }
-      if (!ok && lane == 0) {   // products under way end before the tensor memory is released
+      if (lane == 0) {   // all of the tile's products, also those under way when a wait ran out
         tc_commit(bar(kBEnd + t));
-        mbar_wait(bar(kBEnd + t), 0u, a.err);
+        if (!ok) mbar_wait(bar(kBEnd + t), 0u, a.err);
       }
     }
   } else {
@@ -524,7 +484,6 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       checked += look;
     }
   }
-  }
   tc_fence_before();
   __syncthreads();
   if (warp == kMmaWarp) {
@@ -535,23 +494,15 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
 
 }  // namespace
 
+int prompt_tile_keys() { return kKeys; }
+
 cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStream_t st, int* kernels) {
   *kernels = 1;
   // units of all sequences, at most
   const int units = a.q_rows / (2 * a.q_tokens) + a.B;
   auto kern = dtype ? hill_prompt_attn_kernel<1> : hill_prompt_attn_kernel<0>;
   static int cache[2][64] = {{0}};
-  // the split of registers between the warps holds for what the kernel is launched with
-  static std::atomic<int> regs[2];
-  cudaError_t e;
-  if (regs[dtype ? 1 : 0].load(std::memory_order_relaxed) == 0) {
-    cudaFuncAttributes attr;
-    e = cudaFuncGetAttributes(&attr, kern);
-    if (e != cudaSuccess) return e;
-    if (attr.numRegs < kRegs) return cudaErrorInvalidConfiguration;
-    regs[dtype ? 1 : 0].store(attr.numRegs, std::memory_order_relaxed);
-  }
-  e = ensure_smem_attr(reinterpret_cast<const void*>(kern), kSmem, cache[dtype ? 1 : 0]);
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), kSmem, cache[dtype ? 1 : 0]);
   if (e != cudaSuccess) return e;
   return launch_pdl(kern, dim3((unsigned)units * a.Hkv * a.passes), dim3(kThreads), kSmem, st, 0, a, units);
 }
