@@ -13,8 +13,9 @@
 // block x that CTA c has go to segment x + c of the workspace: runs are in order, so no two parts share one.  A second
 // kernel adds a block's segments, and the KV heads, in a fixed order.
 //
-// 12 warps: sums (0-3, 4-7: a key tile each), loads (8: K of two blocks, Q tiles in a ring, by TMA), products (9: one
-// thread), statistics (10).  Tensor memory holds two S^T for each key tile, all 512 columns.
+// 12 warps: sums (0-3, 4-7: a key tile each), loads (8: K of two blocks, Q tiles in a ring, by TMA), products (9, 10: one
+// thread for each key tile: issuing takes as long as the tensor cores take the products, so what a thread does besides
+// would be time in which they stand still), statistics (11).  Tensor memory holds two S^T for each key tile, all 512 columns.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,14 +35,14 @@ namespace {
 constexpr int kRows = 128, kKeys = 128, kTiles = 2, kBlock = kTiles * kKeys;
 constexpr int kStages = 3, kStats = 3;           // rings of Q tiles and of their statistics
 constexpr int kHalf = 128 * 128, kTileBytes = 2 * kHalf;
-constexpr int kSumWarps = 4 * kTiles, kLoadWarp = kSumWarps, kMmaWarp = kLoadWarp + 1, kStatWarp = kMmaWarp + 1;
+constexpr int kSumWarps = 4 * kTiles, kLoadWarp = kSumWarps, kMmaWarp = kLoadWarp + 1, kStatWarp = kMmaWarp + kTiles;
 constexpr int kWarps = 12, kThreads = kWarps * 32;
 
 constexpr int kOffK = 0, kOffQ = 2 * kTiles * kTileBytes, kOffStats = kOffQ + kStages * kTileBytes;
 constexpr int kOffBars = kOffStats + kStats * kRows * 4;
 constexpr int kBKFull = 0, kBKEmpty = 2, kBQFull = 4, kBQEmpty = kBQFull + kStages, kBLFull = kBQEmpty + kStages,
               kBLEmpty = kBLFull + kStats, kBSFull = kBLEmpty + kStats, kBSEmpty = kBSFull + 4, kBDone = kBSEmpty + 4,
-              kBars = kBDone + 1;
+              kBars = kBDone + kTiles;
 constexpr int kOffMisc = kOffBars + kBars * 8;   // tensor memory address, abort flag
 constexpr int kSmem = kOffMisc + 16 + 1024;
 static_assert(kSmem <= 232448, "shared memory");
@@ -76,14 +77,14 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
       for (int i = 0; i < n; ++i) mbar_init(bar(first + i), count);
     };
     init(kBKFull, 2, 1);
-    init(kBKEmpty, 2, 1);
+    init(kBKEmpty, 2, kTiles);
     init(kBQFull, kStages, 1);
-    init(kBQEmpty, kStages, 1);
+    init(kBQEmpty, kStages, kTiles);
     init(kBLFull, kStats, 1);
     init(kBLEmpty, kStats, kSumWarps);
     init(kBSFull, 4, 1);
     init(kBSEmpty, 4, 4);
-    init(kBDone, 1, 1);
+    init(kBDone, kTiles, 1);
     misc[1] = 0;
     fence_barrier_init();
     prefetch_tmap(&a.qmap);
@@ -332,36 +333,41 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
         for (int x = max(0, parts - 2); x < parts; ++x) mbar_wait(bar(kBKFull + (x & 1)), (uint32_t)(x / 2) & 1u, a.err);
       }
     }
-  } else if (warp == kMmaWarp) {
-    // ------------------------------------------------------------ products
+  } else if (warp < kStatWarp) {
+    // ------------------------------------------------------------ products of a key tile
     if (lane == 0) {
       constexpr uint32_t kIdesc = f16_idesc(DT, kKeys, kRows, false);
-      int n = 0;
+      const int t = warp - kMmaWarp;
+      const uint64_t k_desc = smem_desc_sw128(base + kOffK + t * kTileBytes), q_desc = smem_desc_sw128(base + kOffQ);
+      int n = 0, slot = 0;
+      uint32_t phase = 0u;
       walk([&](int part, const Cursor& c, const Seq& s, int first, int tiles) {
         if (!wait(kBKFull + (part & 1), (uint32_t)(part / 2) & 1u)) return false;
+        const uint64_t k0 = k_desc + (uint32_t)((part & 1) * (kTiles * kTileBytes >> 4));
         for (int x = 0; x < tiles; ++x, ++n) {
-          const int slot = n % kStages, buf = n & 1;
-          if (!wait(kBQFull + slot, (uint32_t)(n / kStages) & 1u)) return false;
-          const uint32_t qb = base + kOffQ + slot * kTileBytes;
+          const int buf = n & 1;
+          const uint64_t q0 = q_desc + (uint32_t)(slot * (kTileBytes >> 4));
+          if (!wait(kBQFull + slot, phase)) return false;
+          if (n >= 2 && !wait(kBSEmpty + t * 2 + buf, (uint32_t)(n / 2 - 1) & 1u)) return false;
+          tc_fence_after();
 #pragma unroll
-          for (int t = 0; t < kTiles; ++t) {
-            if (n >= 2 && !wait(kBSEmpty + t * 2 + buf, (uint32_t)(n / 2 - 1) & 1u)) return false;
-            tc_fence_after();
-            const uint32_t kb = base + kOffK + ((part & 1) * kTiles + t) * kTileBytes;
-#pragma unroll
-            for (int k = 0; k < kHeadDim / 16; ++k)
-              tc_mma_f16(tmem + (t * 2 + buf) * kRows, smem_desc_sw128(kb + (k >> 2) * kHalf + (k & 3) * 32),
-                         smem_desc_sw128(qb + (k >> 2) * kHalf + (k & 3) * 32), kIdesc, k > 0 ? 1u : 0u);
-            tc_commit(bar(kBSFull + t * 2 + buf));
+          for (int k = 0; k < kHeadDim / 16; ++k) {
+            const uint32_t at = ((k >> 2) * kHalf + (k & 3) * 32) >> 4;
+            tc_mma_f16(tmem + (t * 2 + buf) * kRows, k0 + at, q0 + at, kIdesc, k > 0 ? 1u : 0u);
           }
+          tc_commit(bar(kBSFull + t * 2 + buf));
           tc_commit(bar(kBQEmpty + slot));
+          if (++slot == kStages) {
+            slot = 0;
+            phase ^= 1u;
+          }
         }
         tc_commit(bar(kBKEmpty + (part & 1)));
         return true;
       });
       // products under way end before the tensor memory is released
-      tc_commit(bar(kBDone));
-      mbar_wait(bar(kBDone), 0u, a.err);
+      tc_commit(bar(kBDone + t));
+      mbar_wait(bar(kBDone + t), 0u, a.err);
     }
   } else if (warp == kStatWarp) {
     // ------------------------------------------------------------ the rows' statistics, -lse log2 e

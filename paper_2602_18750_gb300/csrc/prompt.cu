@@ -332,21 +332,30 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       const bool sees_any = pos >= 0 && (a.window > 0 || a.sinks > 0);
       const float inv = sees_any ? 1.f / l : 0.f;
       const int64_t at = (int64_t)(s.q0 + i_tok) * a.H + g * a.G + hg;
+      // The rows leave through shared memory (the Q tile's, which is done with), 16 lanes to a row: a thread's own stores
+      // would touch 32 lines each.
+      const uint32_t stage = base + t * kQBytes + row * 256;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t sv[32];
         tc_ld32(to + 32 * c, sv);
         tc_wait_ld();
-        if (!valid) continue;
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + at * kHeadDim + 32 * c);
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
+        for (int e = 0; e < 4; ++e) {
           uint32_t w[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            w[x] = pack2<DT>(__uint_as_float(sv[e + 2 * x]) * inv, __uint_as_float(sv[e + 2 * x + 1]) * inv);
-          dst[e / 8] = uint4{w[0], w[1], w[2], w[3]};
+            w[x] = pack2<DT>(__uint_as_float(sv[8 * e + 2 * x]) * inv, __uint_as_float(sv[8 * e + 2 * x + 1]) * inv);
+          sts128(stage + (((4 * c + e) ^ (row & 15)) << 4), uint4{w[0], w[1], w[2], w[3]});
         }
+      }
+      __syncwarp();
+#pragma unroll 4
+      for (int r = 0; r < 32; r += 2) {
+        const int from = r + (lane >> 4);
+        const int64_t to_row = __shfl_sync(0xffffffffu, valid ? at : -1, from);
+        const uint4 w = lds128(base + t * kQBytes + ((warp & 3) * 32 + from) * 256 + (((lane ^ from) & 15) << 4));
+        if (to_row >= 0) reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + to_row * kHeadDim)[lane & 15] = w;
       }
       if (a.lse && valid) a.lse[at] = sees_any ? fmaf(m, 0.69314718f, logf(l)) : -INFINITY;
     }

@@ -127,10 +127,6 @@ __device__ __forceinline__ __half2 high_twice(uint32_t v) {   // the high half i
   return *reinterpret_cast<const __half2*>(&d);
 }
 
-__device__ __forceinline__ void sts128(uint32_t addr, const uint4& v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
-
 // CL: a cluster of CTAs takes one (row, KV head, pass).
 template <int DT, bool Q4, int HC, bool CL>
 __global__ void __launch_bounds__(Cfg<Q4, HC>::kNW * 32, 1) hill_window_attn_kernel(const __grid_constant__ WindowArgs a) {
