@@ -13,9 +13,10 @@
 // block x that CTA c has go to segment x + c of the workspace: runs are in order, so no two parts share one.  A second
 // kernel adds a block's segments, and the KV heads, in a fixed order.
 //
-// 12 warps: sums (0-3, 4-7: a key tile each), loads (8: K of two blocks, Q tiles in a ring, by TMA), products (9, 10: one
-// thread for each key tile: issuing takes as long as the tensor cores take the products, so what a thread does besides
-// would be time in which they stand still), statistics (11).  Tensor memory holds two S^T for each key tile, all 512 columns.
+// 20 warps: sums (0-15: four for each of the two S^T of each key tile), loads (16: K of two blocks, Q tiles in a ring, by
+// TMA), products (17, 18: one thread for each key tile: issuing takes as long as the tensor cores take the products, so
+// what a thread does besides would be time in which they stand still), statistics (19).  Tensor memory holds the four
+// S^T, all 512 columns.
 #include <algorithm>
 #include <type_traits>
 
@@ -33,10 +34,10 @@ struct BlockInfo {
 namespace {
 
 constexpr int kRows = 128, kKeys = 128, kTiles = 2, kBlock = kTiles * kKeys;
-constexpr int kStages = 3, kStats = 3;           // rings of Q tiles and of their statistics
+constexpr int kStages = 3, kStats = 4;           // rings of Q tiles and of their statistics
 constexpr int kHalf = 128 * 128, kTileBytes = 2 * kHalf;
-constexpr int kSumWarps = 4 * kTiles, kLoadWarp = kSumWarps, kMmaWarp = kLoadWarp + 1, kStatWarp = kMmaWarp + kTiles;
-constexpr int kWarps = 12, kThreads = kWarps * 32;
+constexpr int kSumWarps = 8 * kTiles, kLoadWarp = kSumWarps, kMmaWarp = kLoadWarp + 1, kStatWarp = kMmaWarp + kTiles;
+constexpr int kWarps = kStatWarp + 1, kThreads = kWarps * 32;
 
 constexpr int kOffK = 0, kOffQ = 2 * kTiles * kTileBytes, kOffStats = kOffQ + kStages * kTileBytes;
 constexpr int kOffBars = kOffStats + kStats * kRows * 4;
@@ -44,7 +45,7 @@ constexpr int kBKFull = 0, kBKEmpty = 2, kBQFull = 4, kBQEmpty = kBQFull + kStag
               kBLEmpty = kBLFull + kStats, kBSFull = kBLEmpty + kStats, kBSEmpty = kBSFull + 4, kBDone = kBSEmpty + 4,
               kBars = kBDone + kTiles;
 constexpr int kOffMisc = kOffBars + kBars * 8;   // tensor memory address, abort flag
-constexpr int kSmem = kOffMisc + 16 + 1024;
+constexpr int kSmem = kOffMisc + 16;
 static_assert(kSmem <= 232448, "shared memory");
 
 // The queries that count for keys [j0, j0 + kBlock): the first of them, and how many tiles they make.
@@ -65,9 +66,8 @@ struct Cursor {
 
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(const __grid_constant__ PromptArgs a) {
-  extern __shared__ unsigned char ism_raw[];
-  const uint32_t base = (smem_addr(ism_raw) + 1023u) & ~1023u;
-  unsigned char* const mem = ism_raw + (base - smem_addr(ism_raw));
+  extern __shared__ __align__(1024) unsigned char mem[];
+  const uint32_t base = smem_addr(mem);
   volatile int* const misc = reinterpret_cast<int*>(mem + kOffMisc);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, tid = threadIdx.x;
   auto bar = [&](int i) { return base + kOffBars + (uint32_t)(i * 8); };
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
     init(kBQFull, kStages, 1);
     init(kBQEmpty, kStages, kTiles);
     init(kBLFull, kStats, 1);
-    init(kBLEmpty, kStats, kSumWarps);
+    init(kBLEmpty, kStats, kSumWarps / 2);
     init(kBSFull, 4, 1);
     init(kBSEmpty, 4, 4);
     init(kBDone, kTiles, 1);
@@ -230,7 +230,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
 
   if (warp < kSumWarps) {
     // ------------------------------------------------------------ sums of a key tile
-    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
+    // (the two S^T of a key tile have their own warps)
+    const int t = warp >> 3, buf = (warp >> 2) & 1, row = (warp & 3) * 32 + lane;
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16) + t * 2 * kRows;
     const float2 c2 = both(kLog2eInvSqrtD);
     int n = 0;
@@ -239,32 +240,33 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
       float total = 0.f;
       bool ok = true;
       for (int x = 0; x < tiles; ++x, ++n) {
+        if ((n & 1) != buf) continue;
         const int token = tile_token(c, first, x), heads = min(a.G - tile_pass(c, x) * a.q_heads, a.q_heads);
         const int p0 = token + s.shift(), p1 = min(token + a.q_tokens, s.n) - 1 + s.shift();   // positions
         const bool whole = token + a.q_tokens <= s.n && heads == a.q_heads && k0 + kKeys - 1 <= p0 &&
                            (k0 + kKeys - 1 < a.sinks || k0 > p1 - a.window);
-        ok = wait(kBSFull + t * 2 + (n & 1), (uint32_t)(n >> 1) & 1u) && wait(kBLFull + n % kStats, (uint32_t)(n / kStats) & 1u);
+        ok = wait(kBSFull + t * 2 + buf, (uint32_t)(n >> 1) & 1u) && wait(kBLFull + n % kStats, (uint32_t)(n / kStats) & 1u);
         if (!__all_sync(0xffffffffu, ok)) return false;
         tc_fence_after();
-        const uint32_t st = base + kOffStats + (n % kStats) * kRows * 4, ts = lanes + (n & 1) * kRows;
+        const uint32_t st = base + kOffStats + (n % kStats) * kRows * 4, ts = lanes + buf * kRows;
         float2 sum[2] = {both(0.f), both(0.f)};
         uint32_t vis[4];   // the tile's rows that see the key
         auto add = [&](auto masked_tag) {
           constexpr bool kMasked = decltype(masked_tag)::value;
-          uint32_t sv[2][32];
-          tc_ld32(ts, sv[0]);
+          uint32_t sv[2][16];
+          tc_ld16(ts, sv[0]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            tc_landed(sv[q & 1]);
-            if (q < 3) tc_ld32(ts + 32 * (q + 1), sv[(q + 1) & 1]);
+          for (int q = 0; q < 8; ++q) {
+            tc_wait_ld();
+            if (q < 7) tc_ld16(ts + 16 * (q + 1), sv[(q + 1) & 1]);
             else {   // S^T has been read
               tc_fence_before();
               __syncwarp();
-              if (lane == 0) mbar_arrive(bar(kBSEmpty + t * 2 + (n & 1)));
+              if (lane == 0) mbar_arrive(bar(kBSEmpty + t * 2 + buf));
             }
 #pragma unroll
-            for (int k = 0; k < 32; k += 4) {
-              const uint4 l4 = lds128(st + (32 * q + k) * 4);
+            for (int k = 0; k < 16; k += 4) {
+              const uint4 l4 = lds128(st + (16 * q + k) * 4);
               const float2 l2[2] = {{__uint_as_float(l4.x), __uint_as_float(l4.y)}, {__uint_as_float(l4.z), __uint_as_float(l4.w)}};
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
@@ -272,8 +274,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
                 const float2 y = fma2(z, c2, l2[e]);
                 float2 w{ex2(y.x), ex2(y.y)};
                 if (kMasked) {
-                  w.x = (vis[q] >> (k + 2 * e)) & 1u ? w.x : 0.f;
-                  w.y = (vis[q] >> (k + 2 * e + 1)) & 1u ? w.y : 0.f;
+                  w.x = (vis[q >> 1] >> (16 * (q & 1) + k + 2 * e)) & 1u ? w.x : 0.f;
+                  w.y = (vis[q >> 1] >> (16 * (q & 1) + k + 2 * e + 1)) & 1u ? w.y : 0.f;
                 }
                 sum[e] = add2(sum[e], w);
               }
@@ -295,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
           } else {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBSEmpty + t * 2 + (n & 1)));
+            if (lane == 0) mbar_arrive(bar(kBSEmpty + t * 2 + buf));
           }
         }
         __syncwarp();
@@ -303,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
         const float2 both_sums = add2(sum[0], sum[1]);
         total += both_sums.x + both_sums.y;
       }
-      a.part[((int64_t)c.g * nblk + c.blk + blockIdx.x) * kBlock + t * kKeys + row] = total;
+      a.part[(((int64_t)c.g * nblk + c.blk + blockIdx.x) * 2 + buf) * kBlock + t * kKeys + row] = total;
       return true;
     });
   } else if (warp == kLoadWarp) {
@@ -418,7 +420,10 @@ __global__ void __launch_bounds__(kBlock) hill_prompt_importance_sum_kernel(cons
   for (int g = a.kvh ? blockIdx.y : 0; g < (a.kvh ? (int)blockIdx.y + 1 : a.Hkv); ++g) {
     const int64_t w = g * all + f.before;
     const int c0 = (int)(w / per), c1 = (int)((w + f.tiles - 1) / per);
-    for (int c = c0; c <= c1; ++c) sum += a.part[((int64_t)g * totals.x + blk + c) * kBlock + threadIdx.x];
+    for (int c = c0; c <= c1; ++c) {
+      const float* p = a.part + ((int64_t)g * totals.x + blk + c) * 2 * kBlock + threadIdx.x;
+      sum += p[0] + p[kBlock];
+    }
   }
   a.accum[((int64_t)f.b * (a.kvh ? a.Hkv : 1) + blockIdx.y) * a.cap + f.j0 + threadIdx.x] += sum;
 }
@@ -431,7 +436,7 @@ int importance_tile_keys() { return kKeys; }
 
 ImportanceSpace importance_space(int B, int Hkv, int64_t k_rows, int sms) {
   ImportanceSpace s;
-  s.part = (size_t)(Hkv * most_blocks(B, k_rows) + sms) * kBlock * sizeof(float);
+  s.part = (size_t)(Hkv * most_blocks(B, k_rows) + sms) * 2 * kBlock * sizeof(float);
   s.info = (size_t)most_blocks(B, k_rows) * sizeof(BlockInfo);
   return s;
 }
