@@ -26,6 +26,11 @@
 // with two S a tile so that the next is issued before P V: 1857, the steps from barrier to barrier are twice as many.
 // What bounds it now is the chain of a tile, S to softmax (about 1300 cycles) to P V and S.
 //
+// Few rows behind many keys leave most SMs without a unit: then a cluster of CTAs shares each, every CTA an even part of
+// its key tiles, and they merge their (maximum, sum, O) through one another's shared memory, a CTA every so many rows.
+// 32 heads in 8 groups, one CTA to a unit / clusters (us): 2 x 8 tokens behind 9000 110 / 49, one token behind 16000
+// 185 / 38, 200 tokens behind 4000 65 / 36, 64 behind 1000 27.7 / 25.6, 64 behind 500 (in two parts) 21.6 / 29.8.
+//
 // The running maximum m of a row is set 7 below its largest logit (base 2) and raised only when the weights of a
 // tile sum to more than 2^15: no maximum is searched for, and O is not rescaled, until then.  Since S of a tile is
 // complete only after the P V before it, a thread that holds S may rescale O.  The sums l and O are float32; the only
@@ -35,10 +40,15 @@
 // A hidden key has p = 0, and a hidden value must not reach O by 0 * NaN.  In tiles that some row does not see whole, rows
 // of V that are not finite are set to zero in shared memory before the product, and the rows that see them add
 // p v themselves.
+#include <cooperative_groups.h>
+
+#include <algorithm>
 #include <type_traits>
 
 #include "prompt_common.cuh"
 #include "tc_common.cuh"
+
+namespace cg = cooperative_groups;
 
 namespace hill {
 namespace {
@@ -62,13 +72,21 @@ constexpr int kOffMisc = kOffMasks + kMasks * 16;   // tensor memory address, ab
 constexpr int kSmem = kOffMisc + 16;
 static_assert(kSmem <= 232448, "shared memory");
 
+// a split unit's O in float32, where the ring was, and its rows' (maximum, sum)
+constexpr int kOffPartO = kOffRing, kOffPartMl = kOffPartO + kTiles * kRows * kHeadDim * 4;
+static_assert(kOffPartMl + kTiles * kRows * 8 <= kOffBars, "room for the parts");
+
 constexpr uint32_t kColS = 0, kColO = kTiles * kKeys, kCols = 512;
 
 // What a unit's rows see, in key tiles.
 struct Plan {
   int first[kTiles], last[kTiles];   // positions of a tile's first and last token (last < first: no such tile)
-  int sinks, window, nsink, wfirst, count;
-  __device__ __forceinline__ int key(int i) const { return kKeys * (i < nsink ? i : wfirst + i - nsink); }
+  int sinks, window, nsink, wfirst;
+  int begin, count;                  // the CTA's part of the key tiles
+  __device__ __forceinline__ int key(int i) const {
+    i += begin;
+    return kKeys * (i < nsink ? i : wfirst + i - nsink);
+  }
   __device__ __forceinline__ bool active(int t, int j0) const {
     return first[t] <= last[t] && j0 <= last[t] && (j0 < sinks || j0 + kKeys - 1 > first[t] - window);
   }
@@ -98,14 +116,15 @@ struct Ahead {
 };
 
 template <int DT>
-__global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units) {
+__global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units, int parts) {
   extern __shared__ __align__(1024) unsigned char mem[];
   const uint32_t base = smem_addr(mem);
   uint32_t* const masks = reinterpret_cast<uint32_t*>(mem + kOffMasks);
   volatile int* const misc = reinterpret_cast<int*>(mem + kOffMisc);   // 0: tensor memory, 1: abort, 2: sequence, 3: unit in it
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return base + kOffBars + (uint32_t)(i * 8); };
-  const int gp = blockIdx.x / units, u = blockIdx.x - gp * units, g = gp / a.passes, pass = gp - g * a.passes;
+  const int share = blockIdx.x % parts, index = blockIdx.x / parts;   // (a cluster: consecutive CTAs)
+  const int gp = index / units, u = index - gp * units, g = gp / a.passes, pass = gp - g * a.passes;
 
   if (warp == 0) {
     pdl_wait();
@@ -175,7 +194,9 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   plan.wfirst = max(0, lowest - a.window + 1) / kKeys;
   const int end = highest < 0 ? 0 : highest / kKeys + 1;   // key tiles up to the diagonal
   plan.nsink = min(min((a.sinks + kKeys - 1) / kKeys, plan.wfirst), end);
-  plan.count = b >= 0 ? plan.nsink + max(0, end - plan.wfirst) : 0;
+  const int all = b >= 0 ? plan.nsink + max(0, end - plan.wfirst) : 0;   // key tiles of the unit
+  plan.begin = (int)((int64_t)all * share / parts);
+  plan.count = (int)((int64_t)all * (share + 1) / parts) - plan.begin;
 
   auto wait = [&](int i, uint32_t parity) {
     if (mbar_try_wait_long(bar(i), parity)) return true;
@@ -326,7 +347,22 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       ++n;
     }
     if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(kBEnd + t, 0u));
-    if (ok && b >= 0) {
+    if (parts > 1 && b >= 0) {
+      // (the other tile's products may still read the ring)
+      if (ok && plan.count > 0) ok = __all_sync(0xffffffffu, wait(kBEnd + (t ^ 1), 0u));
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t sv[32];
+        tc_ld32(to + 32 * c, sv);
+        tc_wait_ld();
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          sts128(base + kOffPartO + (t * kRows + row) * 512 + (((8 * c + e) ^ lane) << 4),
+                 uint4{sv[4 * e], sv[4 * e + 1], sv[4 * e + 2], sv[4 * e + 3]});
+      }
+      reinterpret_cast<float2*>(mem + kOffPartMl)[t * kRows + row] = float2{m, l};
+    } else if (ok && b >= 0) {
       tc_fence_after();
       // does the row see anything?
       const bool sees_any = pos >= 0 && (a.window > 0 || a.sinks > 0);
@@ -499,9 +535,38 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     tc_fence_after();
     tmem_dealloc(tmem, kCols);
   }
+  if (parts == 1 || b < 0) return;
+  cg::cluster_group cluster = cg::this_cluster();
+  cluster.sync();
+  for (int x = share + parts * warp; x < kTiles * kRows; x += parts * (kThreads / 32)) {
+    const int t = x / kRows, row = x - t * kRows, tok = row / a.q_heads, hg = pass * a.q_heads + row - tok * a.q_heads;
+    const int i_tok = token0 + t * a.q_tokens + tok, pos = i_tok + shift;
+    if (tok >= a.q_tokens || hg >= a.G || i_tok >= s.n) continue;
+    float m = kNegHuge, l = 0.f;
+    for (int r = 0; r < parts; ++r)
+      m = fmaxf(m, reinterpret_cast<const float2*>(cluster.map_shared_rank(mem, r) + kOffPartMl)[x].x);
+    float4 o{0.f, 0.f, 0.f, 0.f};   // channels 4 lane ..
+    for (int r = 0; r < parts; ++r) {
+      const unsigned char* from = cluster.map_shared_rank(mem, r);
+      const float2 ml = reinterpret_cast<const float2*>(from + kOffPartMl)[x];
+      const float4 v = *reinterpret_cast<const float4*>(from + kOffPartO + x * 512 + ((lane ^ (row & 31)) << 4));
+      const float f = ex2(ml.x - m);
+      l = fmaf(ml.y, f, l);
+      o = float4{fmaf(v.x, f, o.x), fmaf(v.y, f, o.y), fmaf(v.z, f, o.z), fmaf(v.w, f, o.w)};
+    }
+    const bool sees_any = pos >= 0 && (a.window > 0 || a.sinks > 0);
+    const float inv = sees_any ? 1.f / l : 0.f;
+    const int64_t at = (int64_t)(s.q0 + i_tok) * a.H + g * a.G + hg;
+    reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + at * kHeadDim)[lane] =
+        uint2{pack2<DT>(o.x * inv, o.y * inv), pack2<DT>(o.z * inv, o.w * inv)};
+    if (a.lse && lane == 0) a.lse[at] = sees_any ? fmaf(m, 0.69314718f, logf(l)) : -INFINITY;
+  }
+  cluster.sync();   // no CTA leaves while another reads its part
 }
 
 }  // namespace
+
+constexpr int kSplitMost = 8, kSplitTiles = 4;
 
 int prompt_tile_keys() { return kKeys; }
 
@@ -513,7 +578,12 @@ cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStre
   static int cache[2][64] = {{0}};
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), kSmem, cache[dtype ? 1 : 0]);
   if (e != cudaSuccess) return e;
-  return launch_pdl(kern, dim3((unsigned)units * a.Hkv * a.passes), dim3(kThreads), kSmem, st, 0, a, units);
+  // CTAs that share a unit: as many as leave no SM with two, and each at least kSplitTiles key tiles of an average sequence
+  const int64_t ctas = (int64_t)units * a.Hkv * a.passes;
+  const int64_t keys = std::min<int64_t>(a.k_rows / a.B, (int64_t)a.sinks + a.window + a.q_rows / a.B);
+  int parts = 1;
+  while (parts < kSplitMost && ctas * parts * 2 <= sms && keys >= (int64_t)parts * 2 * kSplitTiles * kKeys) parts *= 2;
+  return launch_pdl(kern, dim3((unsigned)(ctas * parts)), dim3(kThreads), kSmem, st, parts > 1 ? parts : 0, a, units, parts);
 }
 
 }  // namespace hill

@@ -121,6 +121,27 @@ def test_long(H):
     Case(H, [(300, 3300)], 6, 2, seed=3).verify(150, 700)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("heads,seqs", [((4, 1), [(1, 5000)]), ((8, 2), [(40, 4000), (3, 9000)]), ((8, 8), [(9, 2500)]),
+                                        ((16, 2), [(5, 9000), (7, 20), (0, 30), (2, -2)]), ((14, 2), [(90, 3000)])])
+def test_few_rows_behind_many_keys(H, heads, seqs, dtype):
+    """Clusters share a unit's key tiles; parts without any, of short sequences and windows, among them."""
+    c = Case(H, seqs, *heads, dtype, seed=sum(heads), spare=2)
+    for sinks, window in [(0, ALL), (4, 1000), (300, 200), (0, 0), (0, 4000)]:
+        out, lse = c.verify(sinks, window)
+        again, lse2 = c.attend(sinks, window)
+        assert np.array_equal(out, again) and np.array_equal(lse, lse2)
+    want, wl = c.attend(0, 2000)
+    b = max(range(len(seqs)), key=lambda i: seqs[i][0] + seqs[i][1])
+    last = c.q_start[b + 1] - 1      # the newest query sees key 100 under no window of 2000
+    c.v[c.k_start[b] + 100] = float("nan")
+    c.k[c.k_start[b] + 100] = float("nan")
+    out, lse = c.attend(0, 2000)
+    assert np.array_equal(out, want) and np.array_equal(lse, wl)
+    out, _ = c.attend(0, ALL)
+    assert np.isnan(out[last]).all()
+
+
 def test_groups_past_a_tile(H):
     """More query heads to a KV head than a tile has rows."""
     Case(H, [(3, 20), (130, 0)], 130, 1, seed=4).verify(0, ALL)
