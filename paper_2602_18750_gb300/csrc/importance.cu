@@ -57,6 +57,7 @@ __device__ __forceinline__ int block_tiles(const PromptArgs& a, const Seq& s, in
   first = (int)min(lo, (int64_t)s.n);
   return hi > lo ? (int)((hi - lo + a.q_tokens - 1) / a.q_tokens) * a.passes : 0;
 }
+__host__ __device__ inline int64_t most_blocks(int B, int64_t k_rows) { return k_rows / kBlock + B; }   // of all sequences
 __device__ __forceinline__ int seq_blocks(const PromptArgs& a, const Seq& s) { return (min(s.m, a.cap) + kBlock - 1) / kBlock; }
 
 // Where a CTA stands: tile x of `tiles` of block (g, blk), whose keys begin at j0 of sequence b.
@@ -123,7 +124,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
   }
   __syncthreads();
   // every thread counts the tiles of a run of blocks
-  const int nblk = first_blk[a.B], each = (nblk + kThreads - 1) / kThreads;
+  // (offsets that descend may make more blocks than there is room for: an error by then, the rest is left out)
+  const int nblk = min(first_blk[a.B], (int)most_blocks(a.B, a.k_rows)), each = (nblk + kThreads - 1) / kThreads;
   const int blk0 = min(nblk, tid * each), blk1 = min(nblk, blk0 + each);
   int b0 = 0;
   if (blk0 < blk1) {   // the last sequence that begins at or before blk0
@@ -212,9 +214,9 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
       do {
         ++c.blk;
         c.j0 += kBlock;
-        while (c.j0 >= min(seq_at(a, c.b).m, a.cap)) {
+        while (c.blk == nblk || c.j0 >= min(seq_at(a, c.b).m, a.cap)) {
           c.j0 = 0;
-          if (++c.b == a.B) {
+          if (c.blk == nblk || ++c.b == a.B) {
             c.b = 0;
             c.blk = 0;
             ++c.g;
@@ -428,7 +430,6 @@ __global__ void __launch_bounds__(kBlock) hill_prompt_importance_sum_kernel(cons
   a.accum[((int64_t)f.b * (a.kvh ? a.Hkv : 1) + blockIdx.y) * a.cap + f.j0 + threadIdx.x] += sum;
 }
 
-int64_t most_blocks(int B, int64_t k_rows) { return k_rows / kBlock + B; }
 
 }  // namespace
 

@@ -69,7 +69,7 @@ constexpr int kBQ = 0, kBFull = 1, kBDone = kBFull + kRounds, kBS = kBDone + kRo
               kBCheck = kBP + kTiles, kBEnd = kBCheck + kMasks, kBTurn = kBEnd + kTiles, kBars = kBTurn + kTiles;
 constexpr int kOffMasks = kOffBars + ((kBars * 8 + 15) & ~15);
 constexpr int kOffMisc = kOffMasks + kMasks * 16;   // tensor memory address, abort flag, unit
-constexpr int kSmem = kOffMisc + 16;
+constexpr int kSmem = kOffMisc + 32;
 static_assert(kSmem <= 232448, "shared memory");
 
 // a split unit's O in float32, where the ring was, and its rows' (maximum, sum)
@@ -120,7 +120,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   extern __shared__ __align__(1024) unsigned char mem[];
   const uint32_t base = smem_addr(mem);
   uint32_t* const masks = reinterpret_cast<uint32_t*>(mem + kOffMasks);
-  volatile int* const misc = reinterpret_cast<int*>(mem + kOffMisc);   // 0: tensor memory, 1: abort, 2: sequence, 3: unit in it
+  volatile int* const misc = reinterpret_cast<int*>(mem + kOffMisc);   // 0: tensor memory, 1: abort, 2: is there a unit, 3: its
+                                                                       // place in its sequence, 4 to 7: the sequence
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return base + kOffBars + (uint32_t)(i * 8); };
   const int share = blockIdx.x % parts, index = blockIdx.x / parts;   // (a cluster: consecutive CTAs)
@@ -132,7 +133,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
     int seq = -1, in_seq = 0, before = 0;
     for (int b0 = 0; b0 < a.B && seq < 0; b0 += 32) {
       const int b = b0 + lane;
-      const int mine = b < a.B ? (seq_at(a, b).n + 2 * a.q_tokens - 1) / (2 * a.q_tokens) : 0;
+      const Seq s = b < a.B ? seq_at(a, b) : Seq{0, 0, 0, 0};
+      const int mine = (s.n + 2 * a.q_tokens - 1) / (2 * a.q_tokens);
       int inc = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -145,6 +147,12 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
         seq = b0 + at;
         // the last tokens of a sequence, which see the most keys, go first
         in_seq = before + __shfl_sync(0xffffffffu, inc, at) - 1 - u;
+        if (lane == at) {
+          misc[4] = s.q0;
+          misc[5] = s.n;
+          misc[6] = s.k0;
+          misc[7] = s.m;
+        }
       }
       before += __shfl_sync(0xffffffffu, inc, 31);
     }
@@ -180,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   pdl_wait();
   const uint32_t tmem = (uint32_t)misc[0];
   const int b = misc[2];
-  const Seq s = b >= 0 ? seq_at(a, b) : Seq{0, 0, 0, 0};
+  const Seq s = b >= 0 ? Seq{misc[4], misc[5], misc[6], misc[7]} : Seq{0, 0, 0, 0};
   const int token0 = misc[3] * 2 * a.q_tokens, shift = s.shift();
   Plan plan;
   plan.sinks = a.sinks;
@@ -250,60 +258,62 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       if (!ok) break;
       tc_fence_after();
       uint32_t p[64];
-      float sum;
-      for (int again = 0;; ++again) {
-        auto weights = [&](auto masked_tag) {
-          constexpr bool kMasked = decltype(masked_tag)::value;
-          const float2 m2 = both(-m);
-          float2 sums[2] = {both(0.f), both(0.f)};
-          uint32_t sv[2][32];
-          tc_ld32(ts, sv[0]);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            tc_wait_ld();
-            if (c < 3) tc_ld32(ts + 32 * (c + 1), sv[(c + 1) & 1]);
-#pragma unroll
-            for (int k = 0; k < 32; k += 2) {
-              float2 z{__uint_as_float(sv[c & 1][k]), __uint_as_float(sv[c & 1][k + 1])};
-              if (kMasked) {
-                z.x = (vis[c] >> k) & 1u ? z.x : -INFINITY;
-                z.y = (vis[c] >> (k + 1)) & 1u ? z.y : -INFINITY;
-              }
-              const float2 x = fma2(z, c2, m2);
-              const float2 e{ex2(x.x), ex2(x.y)};
-              sums[(k >> 1) & 1] = add2(sums[(k >> 1) & 1], e);
-              p[c * 16 + (k >> 1)] = pack2<DT>(e.x, e.y);
-            }
-          }
-          const float2 s2 = add2(sums[0], sums[1]);
-          sum = s2.x + s2.y;
-        };
-        if (whole) weights(std::false_type{});
-        else weights(std::true_type{});
-        if (again || !__any_sync(0xffffffffu, sum > 32768.f)) break;
-        // a weight may be past 2^15: the maximum is raised, what the old one has given shrinks (all of it is there: S of
-        // this key tile came after the P V before it).  A row whose weights are within keeps its maximum: what one row sees
-        // changes no bit of another's.
-        float top = -INFINITY;
-        uint32_t sv[32];
+      float sum = 0.f;
+      auto weights = [&](auto masked_tag) {
+        constexpr bool kMasked = decltype(masked_tag)::value;
+        const float2 m2 = both(-m);
+        float2 sums[2] = {both(0.f), both(0.f)};
+        uint32_t sv[2][32];
+        tc_ld32(ts, sv[0]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          tc_ld32(ts + 32 * c, sv);
           tc_wait_ld();
+          if (c < 3) tc_ld32(ts + 32 * (c + 1), sv[(c + 1) & 1]);
 #pragma unroll
-          for (int k = 0; k < 32; ++k)
-            if ((vis[c] >> k) & 1u) top = fmaxf(top, __uint_as_float(sv[k]) * c2.x);
+          for (int k = 0; k < 32; k += 2) {
+            float2 z{__uint_as_float(sv[c & 1][k]), __uint_as_float(sv[c & 1][k + 1])};
+            if (kMasked) {
+              z.x = (vis[c] >> k) & 1u ? z.x : -INFINITY;
+              z.y = (vis[c] >> (k + 1)) & 1u ? z.y : -INFINITY;
+            }
+            const float2 x = fma2(z, c2, m2);
+            const float2 e{ex2(x.x), ex2(x.y)};
+            sums[(k >> 1) & 1] = add2(sums[(k >> 1) & 1], e);
+            p[c * 16 + (k >> 1)] = pack2<DT>(e.x, e.y);
+          }
         }
-        const float mn = sum > 32768.f ? fmaxf(m, top - 7.f) : m, f = ex2(m - mn);
-        m = mn;
-        l *= f;
-        for (int c = 0; c < 4 && n > 0; ++c) {
-          tc_ld32(to + 32 * c, sv);
-          tc_wait_ld();
+        const float2 s2 = add2(sums[0], sums[1]);
+        sum = s2.x + s2.y;
+      };
+      // The maximum is raised where a weight may be past 2^15 (and set with the first key tile): what the old one has
+      // given shrinks -- all of it is there, S of this key tile came after the P V before it.  A row whose weights are
+      // within keeps its maximum: what one row sees changes no bit of another's.
+      for (bool raise = n == 0;; raise = true) {
+        if (raise) {
+          float top = -INFINITY;
+          uint32_t sv[32];
 #pragma unroll
-          for (int k = 0; k < 32; ++k) sv[k] = __float_as_uint(__uint_as_float(sv[k]) * f);
-          tc_st32(to + 32 * c, sv);
+          for (int c = 0; c < 4; ++c) {
+            tc_ld32(ts + 32 * c, sv);
+            tc_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k)
+              if ((vis[c] >> k) & 1u) top = fmaxf(top, __uint_as_float(sv[k]) * c2.x);
+          }
+          const float mn = n == 0 || sum > 32768.f ? fmaxf(m, top - 7.f) : m, f = ex2(m - mn);
+          m = mn;
+          l *= f;
+          for (int c = 0; c < 4 && n > 0; ++c) {
+            tc_ld32(to + 32 * c, sv);
+            tc_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; ++k) sv[k] = __float_as_uint(__uint_as_float(sv[k]) * f);
+            tc_st32(to + 32 * c, sv);
+          }
         }
+        if (whole) weights(std::false_type{});
+        else weights(std::true_type{});
+        if (raise || !__any_sync(0xffffffffu, sum > 32768.f)) break;
       }
       l += sum;
       tc_st32(ts, p);

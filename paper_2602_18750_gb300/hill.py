@@ -490,8 +490,11 @@ def make_packed(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, batch: int) -
         raise ValueError(f"q, K and V must share fp16 or bf16; got {q.dtype}, {k.dtype}, {v.dtype}")
     if q.stride(2) != 1 or k.stride(2) != 1 or v.stride(2) != 1:
         raise ValueError("head dimension must be contiguous")
-    return hill_packed(int(batch), q.shape[1], k.shape[1], q.shape[2], _DTYPES[q.dtype], q.shape[0], k.shape[0],
+    desc = hill_packed(int(batch), q.shape[1], k.shape[1], q.shape[2], _DTYPES[q.dtype], q.shape[0], k.shape[0],
                        q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+    # what a call's tensors are held against (told apart field by field they would take as long as the launch)
+    desc.made_for = tuple((t.dtype, t.shape, t.stride()) for t in (q, k, v)), torch.Size((q.shape[0], q.shape[1])), torch.Size((int(batch) + 1,))
+    return desc
 
 
 def hill_prompt_workspace_bytes(desc: hill_packed) -> int:
@@ -505,56 +508,47 @@ def alloc_prompt_workspace(desc: hill_packed, device="cuda") -> torch.Tensor:
     return torch.empty(n, dtype=torch.uint8, device=device)
 
 
-def _packed_rows(t, dtype, rows, heads, st, sh, what: str):
+def _packed_rows(t, like, what: str):
     """The pointer of packed rows that a descriptor was made for."""
     if t is None or isinstance(t, int):
         return t
-    if t.dtype != dtype or t.shape != (rows, heads, 128) or (t.numel() and t.stride() != (st, sh, 1)):
-        raise ValueError(f"{what} must be [{rows}][{heads}][128] of {dtype}, strides ({st}, {sh}, 1), as the descriptor has "
-                         f"it; got {tuple(t.shape)}, {t.dtype}, strides {t.stride()}")
+    if t.dtype is not like[0] or t.shape != like[1] or t.stride() != like[2]:
+        raise ValueError(f"{what} must be {list(like[1])} of {like[0]}, strides {like[2]}, as the descriptor was made for; "
+                         f"got {list(t.shape)} of {t.dtype}, strides {t.stride()}")
     return t.data_ptr()
 
 
-def _starts(t, batch, what: str):
-    p = _typed(t, _I32, what)
-    if p is not t and t.numel() != batch + 1:
-        raise ValueError(f"{what} must be [{batch + 1}], got {tuple(t.shape)}")
-    return p
+def _dense(t, dtype, shape, what: str):
+    """The pointer of a contiguous tensor of this type and shape."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be {list(shape)} of {dtype}, contiguous; got {list(t.shape)} of {t.dtype}, strides "
+                         f"{t.stride()}")
+    return t.data_ptr()
 
 
 def hill_prompt_attn(desc, q, k, v, q_start, k_start, sinks, window, out, lse=None, stream=None) -> None:
     """Causal attention over packed prompts into out (desc's type); lse: the log of every query's sum of exponentials."""
-    T, dt, B = desc.q_rows, _dtype_of(desc), desc.batch
-    op = _typed(out, dt, "out")
-    if op is not out and out.shape != (T, desc.num_q_heads, desc.head_dim):
-        raise ValueError(f"out must be [{T}][{desc.num_q_heads}][{desc.head_dim}], got {tuple(out.shape)}")
-    lp = _typed(lse, _F32, "lse")
-    if lp is not lse and lse.shape != (T, desc.num_q_heads):
-        raise ValueError(f"lse must be [{T}][{desc.num_q_heads}], got {tuple(lse.shape)}")
-    _check(load().hill_prompt_attn(ctypes.byref(desc),
-                                   _packed_rows(q, dt, T, desc.num_q_heads, desc.q_st, desc.q_sh, "q"),
-                                   _packed_rows(k, dt, desc.k_rows, desc.num_kv_heads, desc.k_st, desc.k_sh, "K"),
-                                   _packed_rows(v, dt, desc.k_rows, desc.num_kv_heads, desc.v_st, desc.v_sh, "V"),
-                                   _starts(q_start, B, "q_start"), _starts(k_start, B, "k_start"), int(sinks), int(window),
-                                   op, lp, _stream(stream)), "hill_prompt_attn")
+    (lq, lk, lv), heads, offsets = desc.made_for
+    _check(load().hill_prompt_attn(desc, _packed_rows(q, lq, "q"), _packed_rows(k, lk, "K"), _packed_rows(v, lv, "V"),
+                                   _dense(q_start, _I32, offsets, "q_start"), _dense(k_start, _I32, offsets, "k_start"),
+                                   int(sinks), int(window), _dense(out, lq[0], lq[1], "out"),
+                                   _dense(lse, _F32, heads, "lse"), _stream(stream)), "hill_prompt_attn")
 
 
 def hill_prompt_importance(desc, q, k, lse, q_start, k_start, sinks, window, newest, accum, kvh=False, ws=None,
                            stream=None) -> None:
     """accum [B][cap] (kvh: [B][Hkv][cap]) += the weights that the prompts' tokens receive from the newest queries."""
     wp, wn = _ws(ws)
-    T, dt, B = desc.q_rows, _dtype_of(desc), desc.batch
-    lp = _typed(lse, _F32, "lse")
-    if lse.shape != (T, desc.num_q_heads):
-        raise ValueError(f"lse must be [{T}][{desc.num_q_heads}], got {tuple(lse.shape)}")
-    ap, rows = _typed(accum, _F32, "accum"), (B, desc.num_kv_heads) if kvh else (B,)
+    (lq, lk, _), heads, offsets = desc.made_for
+    rows = (desc.batch, desc.num_kv_heads) if kvh else (desc.batch,)
     if accum.shape[:-1] != rows:
         raise ValueError(f"accum must be {list(rows)}[cap], got {tuple(accum.shape)}")
-    _check(load().hill_prompt_importance(ctypes.byref(desc),
-                                         _packed_rows(q, dt, T, desc.num_q_heads, desc.q_st, desc.q_sh, "q"),
-                                         _packed_rows(k, dt, desc.k_rows, desc.num_kv_heads, desc.k_st, desc.k_sh, "K"),
-                                         lp, _starts(q_start, B, "q_start"), _starts(k_start, B, "k_start"), int(sinks),
-                                         int(window), int(newest), int(bool(kvh)), ap, accum.shape[-1], wp, wn,
+    _check(load().hill_prompt_importance(desc, _packed_rows(q, lq, "q"), _packed_rows(k, lk, "K"),
+                                         _dense(lse, _F32, heads, "lse"), _dense(q_start, _I32, offsets, "q_start"),
+                                         _dense(k_start, _I32, offsets, "k_start"), int(sinks), int(window), int(newest),
+                                         1 if kvh else 0, _typed(accum, _F32, "accum"), accum.shape[-1], wp, wn,
                                          _stream(stream)), "hill_prompt_importance")
 
 
@@ -580,11 +574,12 @@ def make_pages(k_pool: torch.Tensor, v_pool: torch.Tensor, table: torch.Tensor, 
                    k_pool.shape[0], k_pool.shape[2], table.shape[1])
     p.tensors = (k_pool, v_pool, table, scales)
     p.kv_heads, p.batch, p.dtype = k_pool.shape[1], table.shape[0], None if scales is not None else k_pool.dtype
+    p.offsets, p.rows = torch.Size((p.batch + 1,)), torch.Size((p.batch,))
     return p
 
 
 def _fits(desc, pages) -> None:
-    if desc.num_kv_heads != pages.kv_heads or desc.batch != pages.batch or (pages.dtype and pages.dtype != _dtype_of(desc)):
+    if desc.num_kv_heads != pages.kv_heads or desc.batch != pages.batch or (pages.dtype and pages.dtype is not _dtype_of(desc)):
         raise ValueError(f"pages of {pages.batch} sequences, {pages.kv_heads} KV heads{f', {pages.dtype}' if pages.dtype else ''} "
                          f"do not fit a descriptor of {desc.batch}, {desc.num_kv_heads}, {_dtype_of(desc)}")
 
@@ -598,16 +593,15 @@ def make_desc_paged(q: torch.Tensor, pages: hill_pages) -> hill_desc:
         raise ValueError(f"unsupported dtype {q.dtype}")
     desc = hill_desc(B, H, pages.kv_heads, d, pages.cols * pages.page, _DTYPES[q.dtype], q.stride(0), q.stride(1))
     _fits(desc, pages)
+    desc.made_for = q.dtype, q.shape, q.stride()
     return desc
 
 
 def hill_paged_attn(desc, q, pages, lens, sinks, window, out, accum=None, kvh=False, ws=None, stream=None) -> None:
-    """hill_window_attn over a cache in pages."""
+    """hill_window_attn over a cache in pages; desc is make_desc_paged's."""
     _fits(desc, pages)
-    if not isinstance(q, int) and q.dtype != _dtype_of(desc):
-        raise ValueError(f"q must be {_dtype_of(desc)}, got {q.dtype}")
     wp, wn = _ws(ws)
-    _check(load().hill_paged_attn(desc, _ptr(q), pages, _typed(lens, _I32, "lens"), int(sinks), int(window), 1 if kvh else 0,
+    _check(load().hill_paged_attn(desc, _packed_rows(q, desc.made_for, "q"), pages, _typed(lens, _I32, "lens"), int(sinks), int(window), 1 if kvh else 0,
                                   _typed(accum, _F32, "accum"), _typed(out, _F32, "out"), wp, wn, _stream(stream)),
            "hill_paged_attn")
 
@@ -616,18 +610,15 @@ def hill_paged_write(desc, pages, k_new, v_new, starts, begin, stream=None) -> N
     """New rows [rows][Hkv][d] of several sequences into their pages; E4M3 caches quantise them."""
     _fits(desc, pages)
     shape, dt = k_new.shape, _dtype_of(desc)
-    if len(shape) != 3 or v_new.shape != shape or shape[1] != pages.kv_heads or shape[2] != 128 or k_new.dtype != dt or v_new.dtype != dt:
+    if len(shape) != 3 or v_new.shape != shape or shape[1] != pages.kv_heads or shape[2] != 128 or k_new.dtype is not dt or v_new.dtype is not dt:
         raise ValueError(f"new rows must be [rows][{pages.kv_heads}][128] of {dt}, K and V alike; got {tuple(shape)} of "
                          f"{k_new.dtype}, {tuple(v_new.shape)} of {v_new.dtype}")
     (kt, kh, k1), (vt, vh, v1) = k_new.stride(), v_new.stride()
     if k1 != 1 or v1 != 1:
         raise ValueError("head dimension must be contiguous")
-    b = _typed(begin, _I32, "begin")
-    if b is not begin and begin.numel() != desc.batch:
-        raise ValueError(f"begin must be [{desc.batch}], got {tuple(begin.shape)}")
     rows = _pack_packed_rows(k_new.data_ptr(), v_new.data_ptr(), kt, kh, vt, vh, shape[0])
-    _check(load().hill_paged_write(desc, pages, rows, _starts(starts, desc.batch, "starts"), b, _stream(stream)),
-           "hill_paged_write")
+    _check(load().hill_paged_write(desc, pages, rows, _dense(starts, _I32, pages.offsets, "starts"),
+                                   _dense(begin, _I32, pages.rows, "begin"), _stream(stream)), "hill_paged_write")
 
 
 def hill_paged_read(desc, pages, row_begin, row_end, max_rows, k_cache, v_cache, stream=None) -> None:

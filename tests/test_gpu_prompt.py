@@ -354,6 +354,23 @@ def test_importance_hidden_places(H):
         assert hit[1, 89] and hit.sum() == 1
 
 
+def test_importance_bad_offsets_are_an_error(H):
+    """Offsets that descend name more keys than there are: recorded, and nothing outside accum is written."""
+    B = 40
+    c = Case(H, [(8, 100)] * B, 4, 2, seed=23)
+    n = 108 * B
+    c.attend(0, ALL)
+    ws = H.alloc_prompt_workspace(c.desc)
+    guarded = torch.full((3, B, n + 50), 5.0, device="cuda")
+    for ks in ([0, n] * (B // 2) + [0], list(range(B, -1, -1)), [0] * B + [1 << 30], [-7] + [108 * b for b in range(1, B + 1)]):
+        H.hill_prompt_importance(c.desc, c.q, c.k, c.lse, c.qs, ints(ks), 0, ALL, ALL, guarded[1], ws=ws)
+        with pytest.raises(H.HillError) as e:
+            H.hill_sync_status()
+        assert e.value.status == H.HILL_ERR_DEVICE
+        assert torch.all(guarded[0] == 5) and torch.all(guarded[2] == 5)
+    verify_importance(H, c, 0, ALL, ALL, False)
+
+
 def test_importance_past_the_capacity(H):
     c = Case(H, [(100, 0), (40, 0)], 4, 2, seed=22)
     c.attend(0, ALL)
