@@ -65,7 +65,7 @@ constexpr int kRounds = 4;                       // rounds whose barriers are to
 constexpr int kOffRing = kTiles * kQBytes;
 constexpr int kOffBars = kOffRing + kStages * kTileBytes;
 // barriers: Q; a round's K and V there, given back; S full, P ready of each tile; checks; the end; turns
-constexpr int kBQ = 0, kBFull = 1, kBDone = kBFull + kRounds, kBS = kBDone + kRounds, kBP = kBS + kTiles,
+constexpr int kBQ = 0, kBFull = kTiles, kBDone = kBFull + kRounds, kBS = kBDone + kRounds, kBP = kBS + kTiles,
               kBCheck = kBP + kTiles, kBEnd = kBCheck + kMasks, kBTurn = kBEnd + kTiles, kBars = kBTurn + kTiles;
 constexpr int kOffMasks = kOffBars + ((kBars * 8 + 15) & ~15);
 constexpr int kOffMisc = kOffMasks + kMasks * 16;   // tensor memory address, abort flag, unit
@@ -78,27 +78,28 @@ static_assert(kOffPartMl + kTiles * kRows * 8 <= kOffBars, "room for the parts")
 
 constexpr uint32_t kColS = 0, kColO = kTiles * kKeys, kCols = 512;
 
-// What a unit's rows see, in key tiles.
+// What a unit's rows see, in key tiles.  (No arrays: one that a variable indexes lies in local memory, and the first touch
+// of that cost a unit 2700 cycles between its Q and its first S.)
+static_assert(kTiles == 2, "first and last of each tile");
 struct Plan {
-  int first[kTiles], last[kTiles];   // positions of a tile's first and last token (last < first: no such tile)
+  int first0, first1, last0, last1;   // positions of a tile's first and last token (last < first: no such tile)
   int sinks, window, nsink, wfirst;
-  int begin, count;                  // the CTA's part of the key tiles
+  int begin, count;                   // the CTA's part of the key tiles
+  __device__ __forceinline__ int first(int t) const { return t ? first1 : first0; }
+  __device__ __forceinline__ int last(int t) const { return t ? last1 : last0; }
   __device__ __forceinline__ int key(int i) const {
     i += begin;
     return kKeys * (i < nsink ? i : wfirst + i - nsink);
   }
   __device__ __forceinline__ bool active(int t, int j0) const {
-    return first[t] <= last[t] && j0 <= last[t] && (j0 < sinks || j0 + kKeys - 1 > first[t] - window);
+    return first(t) <= last(t) && j0 <= last(t) && (j0 < sinks || j0 + kKeys - 1 > first(t) - window);
   }
   __device__ __forceinline__ bool full(int t, int j0) const {
     const int j1 = j0 + kKeys - 1;
-    return j1 <= first[t] && (j1 < sinks || j0 > last[t] - window);
+    return j1 <= first(t) && (j1 < sinks || j0 > last(t) - window);
   }
   __device__ __forceinline__ bool partial(int j0) const {
-    bool p = false;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) p = p || (active(t, j0) && !full(t, j0));
-    return p;
+    return (active(0, j0) && !full(0, j0)) || (active(1, j0) && !full(1, j0));
   }
 };
 
@@ -162,7 +163,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       misc[3] = in_seq;
     }
   } else if (warp == kLoadWarp && lane == 0) {
-    mbar_init(bar(kBQ), 1);
+    for (int t = 0; t < kTiles; ++t) mbar_init(bar(kBQ + t), 1);
     for (int i = 0; i < kRounds; ++i) {
       mbar_init(bar(kBFull + i), 1);
       mbar_init(bar(kBDone + i), kTiles + 1);   // both tiles' products, and the checks
@@ -193,12 +194,11 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   Plan plan;
   plan.sinks = a.sinks;
   plan.window = a.window;
-#pragma unroll
-  for (int t = 0; t < kTiles; ++t) {
-    plan.first[t] = token0 + t * a.q_tokens + shift;
-    plan.last[t] = min(token0 + (t + 1) * a.q_tokens, s.n) - 1 + shift;
-  }
-  const int lowest = plan.first[0], highest = max(plan.last[0], plan.last[1]);
+  plan.first0 = token0 + shift;
+  plan.first1 = plan.first0 + a.q_tokens;
+  plan.last0 = min(token0 + a.q_tokens, s.n) - 1 + shift;
+  plan.last1 = min(token0 + 2 * a.q_tokens, s.n) - 1 + shift;
+  const int lowest = plan.first0, highest = max(plan.last0, plan.last1);
   plan.wfirst = max(0, lowest - a.window + 1) / kKeys;
   const int end = highest < 0 ? 0 : highest / kKeys + 1;   // key tiles up to the diagonal
   plan.nsink = min(min((a.sinks + kKeys - 1) / kKeys, plan.wfirst), end);
@@ -408,13 +408,15 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   } else if (warp == kLoadWarp) {
     // ------------------------------------------------------------ loads
     if (lane == 0 && plan.count > 0) {
-      const int tiles = plan.last[1] >= plan.first[1] ? 2 : 1;
+      const int tiles = plan.last1 >= plan.first1 ? 2 : 1;
       const uint32_t q_bytes = (uint32_t)(a.q_heads * a.q_tokens * 128);
-      mbar_arrive_expect_tx(bar(kBQ), tiles * 2 * q_bytes);
-      for (int t = 0; t < tiles; ++t)
+      auto load_q = [&](int t) {
+        mbar_arrive_expect_tx(bar(kBQ + t), 2 * q_bytes);
         for (int h = 0; h < 2; ++h)
           tma_tile_3d(base + t * kQBytes + h * kQHalf, &a.qmap, 64 * h, g * a.G + pass * a.q_heads,
-                      s.q0 + token0 + t * a.q_tokens, bar(kBQ));
+                      s.q0 + token0 + t * a.q_tokens, bar(kBQ + t));
+      };
+      load_q(0);
       // round i brings V of key tile i - 1 (tile 2 i - 1 of the ring) and K of key tile i (2 i); a tile of the ring is
       // free when the round that used it last is done
       int done = 0, i = 0;
@@ -428,9 +430,10 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
           // (on a wait that ran out the tile comes all the same: its barrier has been told of it)
           for (int h = 0; h < 2; ++h) tma_tile_3d(ring(n) + h * kHalf, map, 64 * h, g, s.k0 + plan.key(n >> 1), full_bar);
         }
+        if (i == 0 && tiles > 1) load_q(1);
       }
       if (misc[1]) {   // what is under way has to land before the CTA goes
-        mbar_wait(bar(kBQ), 0u, a.err);
+        for (int t = 0; t < tiles; ++t) mbar_wait(bar(kBQ + t), 0u, a.err);
         for (int x = max(0, i - kRounds); x < i; ++x) mbar_wait(bar(kBFull + x % kRounds), (uint32_t)(x / kRounds) & 1u, a.err);
       }
     }
@@ -447,10 +450,11 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       auto step = [&](int& slot) { slot = slot + 2 >= kStages ? slot + 2 - kStages : slot + 2; };
       int checked = 0;
       Ahead ahead;
+      ahead.look(plan, t, 0, lane);
       uint32_t act_before = 0u, cut_before = 0u;
-      bool ok = lane != 0 || wait(kBQ, 0u);
+      bool ok = lane != 0 || plan.first(t) > plan.last(t) || wait(kBQ + t, 0u);
       for (int i = 0; i <= plan.count; ++i) {
-        if ((i & 31) == 0) {
+        if ((i & 31) == 0 && i > 0) {
           __syncwarp();
           ahead.look(plan, t, i, lane);
         }
