@@ -60,6 +60,11 @@ __device__ __forceinline__ int block_tiles(const PromptArgs& a, const Seq& s, in
 __host__ __device__ inline int64_t most_blocks(int B, int64_t k_rows) { return k_rows / kBlock + B; }   // of all sequences
 __device__ __forceinline__ int seq_blocks(const PromptArgs& a, const Seq& s) { return (min(s.m, a.cap) + kBlock - 1) / kBlock; }
 
+// x / y of numbers that are not negative, by the short division where they are short.
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  return (uint64_t)(x | y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
+}
+
 // Where a CTA stands: tile x of `tiles` of block (g, blk), whose keys begin at j0 of sequence b.
 struct Cursor {
   int g, blk, b, j0, x;
@@ -155,9 +160,9 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
     if (w < warp) before += sums[w];
     all += sums[w];
   }
-  const int64_t total = all * a.Hkv, per = (total + gridDim.x - 1) / gridDim.x;
+  const int64_t total = all * a.Hkv, per = quotient(total + gridDim.x - 1, gridDim.x);
   const int64_t w0 = min(total, blockIdx.x * per), w1 = min(total, w0 + per);
-  const int g0 = all ? (int)(w0 / all) : 0;
+  const int g0 = all ? (int)quotient(w0, all) : 0;
   const int64_t at0 = w0 - g0 * all;
   if (blk0 < blk1 && (blockIdx.x == 0 || (at0 >= before && at0 < before + mine))) {
     int64_t at = before;
@@ -417,11 +422,11 @@ __global__ void __launch_bounds__(kBlock) hill_prompt_importance_sum_kernel(cons
   if (blk >= totals.x) return;
   const BlockInfo f = a.info[blk];
   if (f.tiles == 0 || (int)threadIdx.x >= f.keys) return;
-  const int64_t all = *a.tiles, total = all * a.Hkv, per = (total + totals.y - 1) / totals.y;
+  const int64_t all = *a.tiles, total = all * a.Hkv, per = quotient(total + totals.y - 1, totals.y);
   float sum = 0.f;
   for (int g = a.kvh ? blockIdx.y : 0; g < (a.kvh ? (int)blockIdx.y + 1 : a.Hkv); ++g) {
     const int64_t w = g * all + f.before;
-    const int c0 = (int)(w / per), c1 = (int)((w + f.tiles - 1) / per);
+    const int c0 = (int)quotient(w, per), c1 = (int)quotient(w + f.tiles - 1, per);
     for (int c = c0; c <= c1; ++c) {
       const float* p = a.part + ((int64_t)g * totals.x + blk + c) * 2 * kBlock + threadIdx.x;
       sum += p[0] + p[kBlock];

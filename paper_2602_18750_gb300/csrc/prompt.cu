@@ -117,7 +117,8 @@ struct Ahead {
 };
 
 template <int DT>
-__global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units, int parts) {
+__global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units,
+                                                                        int log_parts) {
   extern __shared__ __align__(1024) unsigned char mem[];
   const uint32_t base = smem_addr(mem);
   uint32_t* const masks = reinterpret_cast<uint32_t*>(mem + kOffMasks);
@@ -125,7 +126,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
                                                                        // place in its sequence, 4 to 7: the sequence
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return base + kOffBars + (uint32_t)(i * 8); };
-  const int share = blockIdx.x % parts, index = blockIdx.x / parts;   // (a cluster: consecutive CTAs)
+  const int parts = 1 << log_parts, share = blockIdx.x & (parts - 1), index = blockIdx.x >> log_parts;   // (a cluster: consecutive CTAs)
   const int gp = index / units, u = index - gp * units, g = gp / a.passes, pass = gp - g * a.passes;
 
   if (warp == 0) {
@@ -203,8 +204,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   const int end = highest < 0 ? 0 : highest / kKeys + 1;   // key tiles up to the diagonal
   plan.nsink = min(min((a.sinks + kKeys - 1) / kKeys, plan.wfirst), end);
   const int all = b >= 0 ? plan.nsink + max(0, end - plan.wfirst) : 0;   // key tiles of the unit
-  plan.begin = (int)((int64_t)all * share / parts);
-  plan.count = (int)((int64_t)all * (share + 1) / parts) - plan.begin;
+  plan.begin = (all * share) >> log_parts;
+  plan.count = ((all * (share + 1)) >> log_parts) - plan.begin;
 
   auto wait = [&](int i, uint32_t parity) {
     if (mbar_try_wait_long(bar(i), parity)) return true;
@@ -580,7 +581,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
 
 }  // namespace
 
-constexpr int kSplitMost = 8, kSplitTiles = 4;
+constexpr int kLogSplitMost = 3, kSplitTiles = 4;
 
 int prompt_tile_keys() { return kKeys; }
 
@@ -595,9 +596,11 @@ cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStre
   // CTAs that share a unit: as many as leave no SM with two, and each at least kSplitTiles key tiles of an average sequence
   const int64_t ctas = (int64_t)units * a.Hkv * a.passes;
   const int64_t keys = std::min<int64_t>(a.k_rows / a.B, (int64_t)a.sinks + a.window + a.q_rows / a.B);
-  int parts = 1;
-  while (parts < kSplitMost && ctas * parts * 2 <= sms && keys >= (int64_t)parts * 2 * kSplitTiles * kKeys) parts *= 2;
-  return launch_pdl(kern, dim3((unsigned)(ctas * parts)), dim3(kThreads), kSmem, st, parts > 1 ? parts : 0, a, units, parts);
+  int log_parts = 0;
+  while (log_parts < kLogSplitMost && ctas << (log_parts + 1) <= sms && keys >= (int64_t)(2 << log_parts) * kSplitTiles * kKeys)
+    ++log_parts;
+  return launch_pdl(kern, dim3((unsigned)(ctas << log_parts)), dim3(kThreads), kSmem, st, log_parts ? 1 << log_parts : 0, a, units,
+                    log_parts);
 }
 
 }  // namespace hill
