@@ -19,12 +19,13 @@
 // given back, together.
 //
 // Measured, 16K tokens of 32 heads (1183 us at the rate of a library product; both tiles' products of a round are 2048 cycles):
-// 1667 us, 1.32 PFLOP/s.  Issuing takes as long as the tensor cores take the products, so whatever else an issuing
+// 1581 us, 1.39 PFLOP/s; of the steps here, by which the way to it was chosen, 1667.  Issuing takes as long as the tensor cores take the products, so whatever else an issuing
 // thread does (waits, commits: 1400 cycles a round) is time in which they stand still: one thread for both tiles 1920 us,
 // two without turns 2170 (the tiles fall into step, and both softmaxes run while nothing is there to multiply).  Half a
 // row to a thread, 16 softmax warps: 1770, a vote of the halves on the maximum costs what it gains.  Key tiles of 64,
-// with two S a tile so that the next is issued before P V: 1857, the steps from barrier to barrier are twice as many.
-// What bounds it now is the chain of a tile, S to softmax (about 1300 cycles) to P V and S.
+// with two S a tile so that the next is issued before P V: 1857, the steps from barrier to barrier are twice as many.  P of
+// the first half of the keys given before the second is formed: 1680 against 1635.
+// What bounds it now is the chain of a tile, S to softmax (about 1300 cycles) to P V and S: a round takes 3050.
 //
 // Few rows behind many keys leave most SMs without a unit: then a cluster of CTAs shares each, every CTA an even part of
 // its key tiles, and they merge their (maximum, sum, O) through one another's shared memory, a CTA every so many rows.
@@ -118,7 +119,7 @@ struct Ahead {
 
 template <int DT>
 __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __grid_constant__ PromptArgs a, int units,
-                                                                        int log_parts) {
+                                                                        int heads, int log_parts) {
   extern __shared__ __align__(1024) unsigned char mem[];
   const uint32_t base = smem_addr(mem);
   uint32_t* const masks = reinterpret_cast<uint32_t*>(mem + kOffMasks);
@@ -127,36 +128,67 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto bar = [&](int i) { return base + kOffBars + (uint32_t)(i * 8); };
   const int parts = 1 << log_parts, share = blockIdx.x & (parts - 1), index = blockIdx.x >> log_parts;   // (a cluster: consecutive CTAs)
-  const int gp = index / units, u = index - gp * units, g = gp / a.passes, pass = gp - g * a.passes;
+  // heads go in groups of `heads`, and of a group the units that see the most keys first, all heads' in turn
+  const int group = index / (heads * units), in_group = index - group * heads * units;
+  const int here = min(heads, a.Hkv * a.passes - group * heads), u = in_group / here;
+  const int gp = group * heads + in_group - u * here, g = gp / a.passes, pass = gp - g * a.passes;
 
   if (warp == 0) {
     pdl_wait();
     // the unit's sequence: 2 * q_tokens tokens to a unit
-    int seq = -1, in_seq = 0, before = 0;
-    for (int b0 = 0; b0 < a.B && seq < 0; b0 += 32) {
-      const int b = b0 + lane;
-      const Seq s = b < a.B ? seq_at(a, b) : Seq{0, 0, 0, 0};
-      const int mine = (s.n + 2 * a.q_tokens - 1) / (2 * a.q_tokens);
-      int inc = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, o);
-        if (lane >= o) inc += y;
-      }
-      const unsigned past = __ballot_sync(0xffffffffu, before + inc > u);
-      if (past) {
-        const int at = __ffs(past) - 1;
-        seq = b0 + at;
-        // the last tokens of a sequence, which see the most keys, go first
-        in_seq = before + __shfl_sync(0xffffffffu, inc, at) - 1 - u;
-        if (lane == at) {
-          misc[4] = s.q0;
-          misc[5] = s.n;
-          misc[6] = s.k0;
-          misc[7] = s.m;
+    int seq = -1, in_seq = 0;
+    auto keep = [&](const Seq& s) {
+      misc[4] = s.q0;
+      misc[5] = s.n;
+      misc[6] = s.k0;
+      misc[7] = s.m;
+    };
+    auto count = [&](const Seq& s) { return (s.n + 2 * a.q_tokens - 1) / (2 * a.q_tokens); };
+    if (a.B <= 32) {
+      // in the order of descending places within their sequences, whatever the sequence: place i is the last one that
+      // more than u units have or pass
+      const Seq s = lane < a.B ? seq_at(a, lane) : Seq{0, 0, 0, 0};
+      const int mine = count(s);
+      auto from = [&](int i) { return (int)__reduce_add_sync(0xffffffffu, max(0, mine - i)); };
+      int lo = 0, hi = (int)__reduce_max_sync(0xffffffffu, mine), beyond = 0;   // beyond: units from place hi on
+      if (from(0) > u) {
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1, n = from(mid);
+          if (n > u) {
+            lo = mid;
+          } else {
+            hi = mid;
+            beyond = n;
+          }
         }
+        const unsigned have = __ballot_sync(0xffffffffu, mine > lo);
+        const bool me = mine > lo && __popc(have & ((1u << lane) - 1u)) == u - beyond;
+        seq = __ffs(__ballot_sync(0xffffffffu, me)) - 1;
+        in_seq = lo;
+        if (me) keep(s);
       }
-      before += __shfl_sync(0xffffffffu, inc, 31);
+    } else {
+      int before = 0;
+      for (int b0 = 0; b0 < a.B && seq < 0; b0 += 32) {
+        const int b = b0 + lane;
+        const Seq s = b < a.B ? seq_at(a, b) : Seq{0, 0, 0, 0};
+        const int mine = count(s);
+        int inc = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, inc, o);
+          if (lane >= o) inc += y;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, before + inc > u);
+        if (past) {
+          const int at = __ffs(past) - 1;
+          seq = b0 + at;
+          // the last tokens of a sequence, which see the most keys, go first
+          in_seq = before + __shfl_sync(0xffffffffu, inc, at) - 1 - u;
+          if (lane == at) keep(s);
+        }
+        before += __shfl_sync(0xffffffffu, inc, 31);
+      }
     }
     if (lane == 0) {
       misc[1] = 0;
@@ -581,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
 
 }  // namespace
 
-constexpr int kLogSplitMost = 3, kSplitTiles = 4;
+constexpr int kLogSplitMost = 3, kSplitTiles = 4, kGroupUnits = 5;
 
 int prompt_tile_keys() { return kKeys; }
 
@@ -599,8 +631,13 @@ cudaError_t launch_prompt_attn(const PromptArgs& a, int dtype, int sms, cudaStre
   int log_parts = 0;
   while (log_parts < kLogSplitMost && ctas << (log_parts + 1) <= sms && keys >= (int64_t)(2 << log_parts) * kSplitTiles * kKeys)
     ++log_parts;
+  // Heads whose units go side by side: enough that the units begun last, of the last group, are the short ones of many
+  // (head after head, the SMs stood still for 15 % of 8K tokens of 32 heads), and few, whose K and V stay in L2.  One head
+  // / groups of 2, 3, 5 units to an SM (us): 16K tokens of 32 heads 1668 / 1688, 1639, 1581; 8 ragged prompts 191 / 184, 185,
+  // 186; chunks of 2K behind 14K tokens, window 4K, all units alike, 470 / 486, 477, 477.
+  const int heads = (int)std::min<int64_t>(std::max<int64_t>(1, (kGroupUnits * sms + units - 1) / units), (int64_t)a.Hkv * a.passes);
   return launch_pdl(kern, dim3((unsigned)(ctas << log_parts)), dim3(kThreads), kSmem, st, log_parts ? 1 << log_parts : 0, a, units,
-                    log_parts);
+                    heads, log_parts);
 }
 
 }  // namespace hill
