@@ -18,19 +18,20 @@
 // Round i of a tile is O += P V of key tile i - 1 and S of key tile i; V of the one and K of the other come, and are
 // given back, together.
 //
-// Measured, 16K tokens of 32 heads (1183 us at the rate of a library product; both tiles' products of a round are 2048 cycles):
-// 1581 us, 1.39 PFLOP/s; of the steps here, by which the way to it was chosen, 1667.  Issuing takes as long as the tensor cores take the products, so whatever else an issuing
-// thread does (waits, commits: 1400 cycles a round) is time in which they stand still: one thread for both tiles 1920 us,
-// two without turns 2170 (the tiles fall into step, and both softmaxes run while nothing is there to multiply).  Half a
-// row to a thread, 16 softmax warps: 1770, a vote of the halves on the maximum costs what it gains.  Key tiles of 64,
-// with two S a tile so that the next is issued before P V: 1857, the steps from barrier to barrier are twice as many.  P of
-// the first half of the keys given before the second is formed: 1680 against 1635.
-// What bounds it now is the chain of a tile, S to softmax (about 1300 cycles) to P V and S: a round takes 3050.
+// Measured, 16K tokens of 32 heads (1183 us at the rate of a library product; both tiles' products of a round are 2048
+// cycles): 1581 us, 1.39 PFLOP/s.  On the way to it, from 1667 us before the order of the units was changed: issuing takes
+// as long as the tensor cores take the products, so whatever else an issuing thread does (waits, commits: 1400 cycles a
+// round) is time in which they stand still: one thread for both tiles 1920, two without turns 2170 (the tiles fall into
+// step, and both softmaxes run while nothing is there to multiply).  Half a row to a thread, 16 softmax warps: 1770, a
+// vote of the halves on the maximum costs what it gains.  Key tiles of 64, with two S a tile so that the next is issued
+// before P V: 1857, the steps from barrier to barrier are twice as many.  P of the first half of the keys given before the
+// second is formed: 1680 against 1635.  What bounds it now is the chain of a tile, S to softmax (about 1300 cycles) to P V
+// and S: a round takes 3050.
 //
 // Few rows behind many keys leave most SMs without a unit: then a cluster of CTAs shares each, every CTA an even part of
 // its key tiles, and they merge their (maximum, sum, O) through one another's shared memory, a CTA every so many rows.
-// 32 heads in 8 groups, one CTA to a unit / clusters (us): 2 x 8 tokens behind 9000 110 / 49, one token behind 16000
-// 185 / 38, 200 tokens behind 4000 65 / 36, 64 behind 1000 27.7 / 25.6, 64 behind 500 (in two parts) 21.6 / 29.8.
+// 32 heads in 8 groups, one CTA to a unit / clusters (us): 2 x 8 tokens behind 9000 110 / 46, one token behind 16000
+// 185 / 36, 200 tokens behind 4000 65 / 34; in two parts 64 tokens behind 1000 27.7 / 29.9, behind 500 21.6 / 29.8.
 //
 // The running maximum m of a row is set 7 below its largest logit (base 2) and raised only when the weights of a
 // tile sum to more than 2^15: no maximum is searched for, and O is not rescaled, until then.  Since S of a tile is
@@ -613,7 +614,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
 
 }  // namespace
 
-constexpr int kLogSplitMost = 3, kSplitTiles = 4, kGroupUnits = 5;
+constexpr int kLogSplitMost = 3, kSplitTiles = 6, kGroupUnits = 5;
 
 int prompt_tile_keys() { return kKeys; }
 

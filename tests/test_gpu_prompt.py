@@ -142,6 +142,18 @@ def test_few_rows_behind_many_keys(H, heads, seqs, dtype):
     assert np.isnan(out[last]).all()
 
 
+@pytest.mark.parametrize("B", [31, 32, 33, 70])
+def test_many_sequences(H, B):
+    """Up to a warp's lanes of sequences, and more; lengths all over, empty ones among them."""
+    r = np.random.RandomState(B)
+    seqs = [(int(n), int(p)) for n, p in zip(r.choice([0, 1, 2, 30, 64, 65, 150], B), r.choice([0, 0, 5, 140], B))]
+    for heads in ((4, 4), (8, 2)):
+        c = Case(H, seqs, *heads, seed=B, spare=1)
+        c.verify(0, ALL)
+        c.verify(3, 50)
+    verify_importance(H, c, 0, ALL, 40, True)
+
+
 def test_groups_past_a_tile(H):
     """More query heads to a KV head than a tile has rows."""
     Case(H, [(3, 20), (130, 0)], 130, 1, seed=4).verify(0, ALL)
