@@ -289,6 +289,15 @@ def test_another_stream_and_a_graph(H):
         side.synchronize()
         got = f64(c.out)
         assert np.array_equal(got, c.attend(0, ALL)[0]) and not np.array_equal(got, want)
+        c.qs.copy_(ints([0, 17, 231]))       # other lengths of the same rows
+        c.ks.copy_(ints([0, 100, 281]))
+        accum.zero_()
+        graph.replay()
+        side.synchronize()
+        ref, rl, bound, lbound = prompt(f64(c.q), f64(c.k), f64(c.v), [0, 17, 231], [0, 100, 281], 0, ALL, HALF[c.dt])
+        check(f64(c.out), ref, bound)
+        seen = [17, 231 - 17 - max(0, 231 - 17 - 181)]     # queries that see a key give 1 per head
+        np.testing.assert_allclose(f64(accum).sum(1), [8 * n for n in seen], rtol=1e-4)
 
 
 # ---------------------------------------------------------------- importance
