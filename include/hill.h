@@ -433,6 +433,7 @@ hill_status hill_cache_read_q4(const hill_desc* desc, const uint8_t* k4, const u
  * HILL_ERR_DEVICE.
  *     q [q_rows][H][d], k and v [k_rows][Hkv][d], strides *_st (row), *_sh (head)
  * in elements, multiples of 8; 16-byte aligned; d contiguous.  At most 2^30 rows, 512 sequences.
+ * (A stride of 0, of rows or heads that are one and the same, is HILL_ERR_UNSUPPORTED.)
  * These calls read all their inputs after the dependency wait (see above). */
 typedef struct {
   int32_t batch;         /* B >= 0, at most 512                       */

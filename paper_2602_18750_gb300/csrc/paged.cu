@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(Cfg<F8, HC>::kNW * 32, 1) hill_paged_attn_kern
   int2 place{0, 0}, place_next{0, 0};
   auto look_up = [&](int first) {
     const int t = first + lane * G16;
-    int2 at{pa.pages * a.Hkv, 0};
+    int2 at{max(pa.pages, 1) * a.Hkv, 0};   // past the map, whose extent is at least 1
     const int c = t / pa.page;
     if (t < a.cap) {
       const int page = pa.table[(int64_t)ask_b * pa.cols + c];

@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(kWarps * 32) hill_paged_write_kernel(const Pag
 #pragma unroll
   for (int u = 0; u < kU; ++u) {
     const int64_t r = r0 + u;
-    tok[u] = r < rows ? (int)(r / a.Hkv) : -1;
+    tok[u] = r >= rows ? -1 : r >> 32 ? (int)(r / a.Hkv) : (int)((uint32_t)r / (uint32_t)a.Hkv);   // (mostly the short division)
     head[u] = r < rows ? (int)(r - (int64_t)tok[u] * a.Hkv) : 0;
     raw[u][0] = raw[u][1] = Dims16{};
     if (tok[u] < 0) continue;

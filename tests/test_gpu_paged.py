@@ -239,6 +239,30 @@ def test_pages_outside_the_pool(H, e4m3):
 
 
 @FORMS
+def test_no_pages_at_all(H, e4m3):
+    """A pool without a page: nothing is read or written; what is looked at counts as zeros, and is an error."""
+    pool = torch.zeros(0, 2, 16, 128, device="cuda").to(F8 if e4m3 else torch.bfloat16)
+    sc = torch.zeros(0, 2, 16, 2, device="cuda") if e4m3 else None
+    table = ints([[0, -1, 5], [1 << 30, 0, 0]])
+    pages = H.make_pages(pool, pool.clone(), table, sc)
+    q = torch.randn(2, 8, 128, generator=gen(30), device="cuda").bfloat16()
+    desc, out, accum = H.make_desc_paged(q, pages), torch.full((2, 8, 128), 7.0, device="cuda"), torch.zeros(2, 48, device="cuda")
+    ws = H.alloc_window_workspace(desc, True)
+    H.hill_paged_attn(desc, q, pages, ints([0, 0]), 0, ALL, out, accum=accum, ws=ws)
+    H.hill_sync_status()
+    assert torch.all(out == 0) and torch.all(accum == 0)
+    H.hill_paged_attn(desc, q, pages, ints([40, 3]), 0, ALL, out, accum=accum, ws=ws)
+    with pytest.raises(H.HillError):
+        H.hill_sync_status()
+    assert torch.all(out == 0)      # of values that are zeros
+    np.testing.assert_allclose(f64(accum)[0, :40], 8 / 40, rtol=1e-5)
+    k, v = new_rows(5, 2, torch.bfloat16, 31)
+    H.hill_paged_write(desc, pages, k, v, ints([0, 3, 5]), ints([0, 1]))
+    with pytest.raises(H.HillError):
+        H.hill_sync_status()
+
+
+@FORMS
 def test_graph_stream_and_shared_pages(H, e4m3):
     """A captured call follows its table, lengths and pools; two sequences may share pages."""
     lens = [300, 300]

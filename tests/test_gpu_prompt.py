@@ -167,6 +167,15 @@ def test_strides(H, layout):
     c.verify(0, ALL)
 
 
+def test_expanded_rows_are_refused(H):
+    c = Case(H, [(20, 10)], 4, 2, seed=6)
+    for q, k in ((c.q[:1].expand(20, -1, -1), c.k), (c.q, c.k[:, :1].expand(-1, 2, -1))):
+        desc = H.make_packed(q, k, c.v, 1)
+        with pytest.raises(H.HillError) as e:
+            H.hill_prompt_attn(desc, q, k, c.v, c.qs, c.ks, 0, ALL, c.out, lse=c.lse)
+        assert e.value.status == H.HILL_ERR_UNSUPPORTED
+
+
 def test_large_logits(H):
     """Logits of hundreds, rising and falling: the running maximum moves often."""
     for dtype in DT:
