@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
   int* const first_blk = reinterpret_cast<int*>(mem);                       // [B + 1] first block of each sequence
   int64_t* const sums = reinterpret_cast<int64_t*>(mem + 4096);             // [warps]
   Cursor* const start = reinterpret_cast<Cursor*>(mem + 4096 + 256);
+  Seq* const seqs = reinterpret_cast<Seq*>(mem + 8192);                     // [B]
   if (warp == 0) {
     int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += 32) {
@@ -121,6 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
         const Seq s = seq_at(a, b);
         if (s.m > a.cap && blockIdx.x == 0) raise_error(a.err, kErrDevArg);
         mine = seq_blocks(a, s);
+        seqs[b] = s;
       }
       int inc = mine;
 #pragma unroll
@@ -151,7 +153,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
   for (int blk = blk0, b = b0; blk < blk1; ++blk) {
     while (first_blk[b + 1] <= blk) ++b;
     int first;
-    mine += block_tiles(a, seq_at(a, b), (blk - first_blk[b]) * kBlock, first);
+    mine += block_tiles(a, seqs[b], (blk - first_blk[b]) * kBlock, first);
   }
   int64_t inc = mine;
 #pragma unroll
@@ -174,7 +176,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
     int64_t at = before;
     for (int blk = blk0, b = b0; blk < blk1; ++blk) {
       while (first_blk[b + 1] <= blk) ++b;
-      const Seq s = seq_at(a, b);
+      const Seq s = seqs[b];
       const int j0 = (blk - first_blk[b]) * kBlock;
       int first;
       const int tiles = block_tiles(a, s, j0, first);
@@ -212,8 +214,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
   auto walk = [&](auto&& f) {
     Cursor c = begin;
     int64_t left = w1 - w0;
+    Seq s = left > 0 ? seq_at(a, c.b) : Seq{0, 0, 0, 0};
     for (int part = 0; left > 0; ++part) {
-      const Seq s = seq_at(a, c.b);
       int first;
       const int tiles = block_tiles(a, s, c.j0, first), n = (int)min((int64_t)(tiles - c.x), left);
       if (!f(part, c, s, first, n)) return;
@@ -225,15 +227,16 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
       do {
         ++c.blk;
         c.j0 += kBlock;
-        while (c.blk == nblk || c.j0 >= min(seq_at(a, c.b).m, a.cap)) {
+        while (c.blk == nblk || c.j0 >= min(s.m, a.cap)) {
           c.j0 = 0;
           if (c.blk == nblk || ++c.b == a.B) {
             c.b = 0;
             c.blk = 0;
             ++c.g;
           }
+          s = seq_at(a, c.b);
         }
-        next = block_tiles(a, seq_at(a, c.b), c.j0, first);
+        next = block_tiles(a, s, c.j0, first);
       } while (next == 0);
     }
   };
