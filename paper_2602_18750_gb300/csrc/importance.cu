@@ -21,7 +21,7 @@
 // Measured, 8K tokens of 32 heads in 8 groups (148 us at the rate of a library product): 208 us, 1.32 PFLOP/s; tensor cores,
 // the exponentials' pipe (one a pair) and the issue slots are used to 60, 64 and 66 %.  Four warps for both S^T of a key tile:
 // 254, their chain from one tile to the next; one thread for all products 258; masks worked out pair by pair near the
-// diagonal, instead of as a range of columns, 724.  The newest 64 queries of 4 prompts of up to 4K tokens: 20 us, of which the
+// diagonal, instead of as a range of columns, 724.  The newest 64 queries of 4 prompts of up to 4K tokens: 18 us, of which the
 // list, the three blocks that a CTA begins and the second kernel are most.
 #include <algorithm>
 #include <type_traits>

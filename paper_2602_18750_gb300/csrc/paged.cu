@@ -778,11 +778,6 @@ __global__ void __launch_bounds__(Cfg<F8, HC>::kNW * 32, 1) hill_paged_attn_kern
   }
 }
 
-int64_t tiles_at_most(const WindowArgs& a, int T) {
-  const int64_t all = ((int64_t)a.cap + T - 1) / T;
-  return std::min<int64_t>(all, ((int64_t)a.sinks + T - 1) / T + ((int64_t)a.window + T - 1) / T + 1);
-}
-
 template <int DT, bool F8, int HC, bool CL>
 cudaError_t launch_attn_cl(const PagedArgs& a, int grid, int cluster, cudaStream_t st, int* count = nullptr) {
   using C = Cfg<F8, HC>;

@@ -390,7 +390,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       if (lane == 0) mbar_arrive(bar(kBP + t));
       ++n;
     }
-    if (ok && n > 0) ok = __all_sync(0xffffffffu, wait(kBEnd + t, 0u));
+    // (also where the tile saw nothing: its Q, whose place the rows leave through, has landed by then)
+    if (ok && plan.count > 0) ok = __all_sync(0xffffffffu, wait(kBEnd + t, 0u));
     if (parts > 1 && b >= 0) {
       // (the other tile's products may still read the ring)
       if (ok && plan.count > 0) ok = __all_sync(0xffffffffu, wait(kBEnd + (t ^ 1), 0u));

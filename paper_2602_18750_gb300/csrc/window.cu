@@ -1010,12 +1010,6 @@ cudaError_t launch_accum_t(const WindowArgs& a, int64_t tiles, cudaStream_t st) 
                     dim3(kAccWarps * 32), 0, st, 0, a);
 }
 
-// The most tiles of T tokens that a row may show.
-int64_t tiles_at_most(const WindowArgs& a, int T) {
-  const int64_t all = ((int64_t)a.cap + T - 1) / T;
-  return std::min<int64_t>(all, ((int64_t)a.sinks + T - 1) / T + ((int64_t)a.window + T - 1) / T + 1);
-}
-
 // Launch as clusters of `cluster` CTAs, or (0) as a list over `grid` CTAs.
 // count: only how many of those clusters fit the GPU at a time.
 template <int DT, bool Q4, int HC, bool CL>

@@ -3,6 +3,7 @@
 // are dealt out, powers of two, merging.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "hill_internal.h"
@@ -112,6 +113,12 @@ struct Merged {
     }
   }
 };
+
+// The most tiles of T tokens that a row may show.
+inline int64_t tiles_at_most(const WindowArgs& a, int T) {
+  const int64_t all = ((int64_t)a.cap + T - 1) / T;
+  return std::min<int64_t>(all, ((int64_t)a.sinks + T - 1) / T + ((int64_t)a.window + T - 1) / T + 1);
+}
 
 }  // namespace
 }  // namespace hill

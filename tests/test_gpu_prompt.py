@@ -258,6 +258,15 @@ def test_no_keys_and_no_queries(H):
     H.hill_prompt_attn(H.make_packed(c.q, c.k, c.v, 0), c.q, c.k, c.v, ints([0]), ints([0]), 0, ALL, c.out)
 
 
+def test_tiles_that_see_nothing_beside_ones_that_do(H):
+    """Queries before the first key, in one tile of a unit and not in the other, many units at once."""
+    for heads in ((32, 1), (64, 2), (4, 4)):
+        c = Case(H, [(40, -20)] * 24 + [(300, -130)], *heads, seed=33)
+        for _ in range(5):
+            c.out.fill_(7)
+            c.verify(0, ALL)
+
+
 def test_bad_offsets_are_an_error(H):
     c = Case(H, [(40, 0), (20, 0)], 4, 2, seed=12)
     for qs, ks in (([0, 40, 70], [0, 40, 60]), ([0, 40, 60], [0, 40, 1 << 29]), ([0, 50, 40], [0, 40, 60]), ([-3, 40, 60], [0, 40, 60])):
