@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
           tc_ld16(ts, sv[0]);
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
-            tc_wait_ld();
+            tc_landed(sv[q & 1]);
             if (q < 7) tc_ld16(ts + 16 * (q + 1), sv[(q + 1) & 1]);
             else {   // S^T has been read
               tc_fence_before();

@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
         tc_ld32(ts, sv[0]);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          tc_wait_ld();
+          tc_landed(sv[c & 1]);
           if (c < 3) tc_ld32(ts + 32 * (c + 1), sv[(c + 1) & 1]);
 #pragma unroll
           for (int k = 0; k < 32; k += 2) {
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             tc_ld32(ts + 32 * c, sv);
-            tc_wait_ld();
+            tc_landed(sv);
 #pragma unroll
             for (int k = 0; k < 32; ++k)
               if ((vis[c] >> k) & 1u) top = fmaxf(top, __uint_as_float(sv[k]) * c2.x);
@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
           l *= f;
           for (int c = 0; c < 4 && n > 0; ++c) {
             tc_ld32(to + 32 * c, sv);
-            tc_wait_ld();
+            tc_landed(sv);
 #pragma unroll
             for (int k = 0; k < 32; ++k) sv[k] = __float_as_uint(__uint_as_float(sv[k]) * f);
             tc_st32(to + 32 * c, sv);
@@ -370,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
               for (int c = 0; c < 4; ++c) {
                 uint32_t sv[32];
                 tc_ld32(to + 32 * c, sv);
-                tc_wait_ld();
+                tc_landed(sv);
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
                   if (!see) continue;
@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       for (int c = 0; c < 4; ++c) {
         uint32_t sv[32];
         tc_ld32(to + 32 * c, sv);
-        tc_wait_ld();
+        tc_landed(sv);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           sts128(base + kOffPartO + (t * kRows + row) * 512 + (((8 * c + e) ^ lane) << 4),
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_attn_kernel(const __g
       for (int c = 0; c < 4; ++c) {
         uint32_t sv[32];
         tc_ld32(to + 32 * c, sv);
-        tc_wait_ld();
+        tc_landed(sv);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           uint32_t w[4];
