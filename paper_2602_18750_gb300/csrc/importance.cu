@@ -305,7 +305,8 @@ __global__ void __launch_bounds__(kThreads, 1) hill_prompt_importance_kernel(con
           // fewer heads than q_heads has one token)
           const int from = max(0, j - p0) * a.q_heads;
           const int last = j < a.sinks ? p1 : min(p1, j + a.window - 1);
-          const int to = min(last - p0 + 1, a.q_tokens) * a.q_heads - (a.q_heads - heads);
+          // (cut off before the product: behind a long history a window's last token may be 2^30 positions before p0)
+          const int to = min(max(last - p0 + 1, 0), a.q_tokens) * a.q_heads - (a.q_heads - heads);
 #pragma unroll
           for (int q = 0; q < 4; ++q) vis[q] = bits_to(to - 1 - 32 * q) & ~bits_to(from - 1 - 32 * q);
           if (__any_sync(0xffffffffu, from < to)) {

@@ -420,3 +420,21 @@ def test_importance_past_the_capacity(H):
     assert e.value.status == H.HILL_ERR_DEVICE
     base = torch.rand(2, 100, device="cuda", generator=gen(3))
     torch.testing.assert_close(got - start, (want - base)[:, :60], rtol=0, atol=2.0 ** -15)   # sums up to 2^8, steps of 2^-16
+
+
+def test_importance_behind_a_long_history(H):
+    """128 query heads on one KV head at a position of 2^24 + 1200: the block of the last sinks is 2^31 rows of (query, head)
+    before the query, and its keys from there on are hidden by the window.
+
+    Logits of 0, so that a visible key has 128 / 1100.  A weight is off by 2^-21 of itself for lse (7.003 as a float32, times
+    log2 e: 10.1 x 2^-23 in all, and 2^-22 of ex2), its sum by 128 additions of 2^-24: below 2^-16."""
+    m, heads, sinks, window = (1 << 24) + 1200, 128, 100, 1000
+    q, k = torch.zeros(1, heads, 128, dtype=torch.bfloat16, device="cuda"), torch.zeros(m, 1, 128, dtype=torch.bfloat16, device="cuda")
+    desc = H.make_packed(q, k, k, 1)
+    lse, accum = torch.full((1, heads), float(np.log(sinks + window)), device="cuda"), torch.zeros(1, m, device="cuda")
+    H.hill_prompt_importance(desc, q, k, lse, ints([0, 1]), ints([0, m]), sinks, window, ALL, accum, ws=H.alloc_prompt_workspace(desc))
+    H.hill_sync_status()
+    want = heads / (sinks + window)
+    for seen in (accum[0, :sinks], accum[0, m - window:]):
+        assert ((seen - want).abs() <= want * 2.0 ** -16).all()
+    assert not accum[0, sinks:m - window].any()
