@@ -438,3 +438,20 @@ def test_importance_behind_a_long_history(H):
     for seen in (accum[0, :sinks], accum[0, m - window:]):
         assert ((seen - want).abs() <= want * 2.0 ** -16).all()
     assert not accum[0, sinks:m - window].any()
+
+
+@pytest.mark.parametrize("dtype,low", [("bf16", -1e30), ("fp16", -60000.0)])
+@pytest.mark.parametrize("heads", [(4, 1), (7, 1), (12, 1), (10, 2), (3, 3)], ids=lambda h: f"{h[0]}x{h[1]}")
+def test_importance_of_a_key_at_minus_infinity(H, heads, dtype, low):
+    """A seen key whose logits are all -infinity has the weight 0, whatever the size of the group: as one whose
+    logits are below -500, which changes no bit of the others (2^-720 is 0 in float32)."""
+    c = Case(H, [(300, 0)], *heads, dtype, seed=40 + heads[0])
+    c.q[:, :, 5] = c.q[:, :, 5].abs() + 0.125      # 60000 x 0.125 / sqrt(128) = 663
+    c.k[40, :, 5] = low
+    c.attend(0, ALL)
+    start, want, lse = run_importance(H, c, 0, ALL, ALL, True, 300)
+    assert torch.equal(want[:, :, 40], start[:, :, 40]) and torch.isfinite(lse).all()
+    c.k[40, :, 5] = -float("inf")
+    _, got, _ = run_importance(H, c, 0, ALL, ALL, True, 300, lse)
+    H.hill_sync_status()
+    assert torch.equal(got, want)
