@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(Cfg<F8, HC>::kNW * 32, 1) hill_paged_attn_kern
       if (page >= 0 && page < pa.pages) at.x = page * a.Hkv;
       else {   // not a page of the pool: zeros, and an error if it is looked at
         const int n = min(max(a.lens[ahead.row], 0), a.cap);
-        if (t < n && (t < a.sinks || t + G16 > n - a.window)) raise_error(a.err, kErrDevArg);
+        if (t < n && (t < a.sinks || (a.window > 0 && t + G16 > n - a.window))) raise_error(a.err, kErrDevArg);
       }
     }
     return at;

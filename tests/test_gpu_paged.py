@@ -239,6 +239,21 @@ def test_pages_outside_the_pool(H, e4m3):
 
 
 @FORMS
+@pytest.mark.parametrize("page", [16, 32])
+def test_a_window_of_nothing_looks_at_no_page(H, page, e4m3):
+    """Sinks alone are visible: the pages behind them may be gone, the last token's among them."""
+    lens, sinks = [100, 70], 3
+    c = Cache(H, lens, 8, 2, page, "bf16", e4m3, seed=32)
+    want = c.attend(lens, sinks, 0)
+    c.table[:, 1:] = -1
+    assert np.array_equal(c.attend(lens, sinks, 0), want)
+    c.table[0, 0] = -1           # the sinks' own page
+    with pytest.raises(H.HillError) as e:
+        c.attend(lens, sinks, 0)
+    assert e.value.status == H.HILL_ERR_DEVICE
+
+
+@FORMS
 def test_no_pages_at_all(H, e4m3):
     """A pool without a page: nothing is read or written; what is looked at counts as zeros, and is an error."""
     pool = torch.zeros(0, 2, 16, 128, device="cuda").to(F8 if e4m3 else torch.bfloat16)
