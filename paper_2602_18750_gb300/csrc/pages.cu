@@ -62,7 +62,9 @@ template <int DT, bool F8, int kU>
 __global__ void __launch_bounds__(kWarps * 32) hill_paged_write_kernel(const PagesArgs a) {
   const int lane = threadIdx.x & 31, l8 = lane & 7;
   pdl_wait();
-  pdl_launch_dependents();
+  // No early launch of dependents behind 16-bit pools: with one page to a sequence they are a contiguous cache, whose
+  // rows the scoring calls read before their own wait.  (Codes are read after it by every call.)
+  if (F8) pdl_launch_dependents();
   const int64_t rows = (int64_t)a.rows * a.Hkv;
   const int64_t r0 = (((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * 4 + (lane >> 3)) * kU;
   Dims16 raw[kU][2];

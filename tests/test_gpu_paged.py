@@ -360,6 +360,38 @@ def test_write_and_read(H, lens, begin, dtype, e4m3):
             assert torch.equal(bits(was)[rest], bits(now)[rest])
 
 
+def test_pages_written_before_they_are_scored(H):
+    """A 16-bit pool with one page to a sequence is a contiguous cache: scoring it behind a write sees the new rows."""
+    B, Hkv, cap, dt = 4, 8, 4096, torch.bfloat16
+    k, v = (torch.zeros(B, Hkv, cap, 128, dtype=dt, device="cuda") for _ in range(2))
+    q = torch.randn(B, 32, 128, generator=gen(41), device="cuda").to(dt)
+    pages, desc = H.make_pages(k, v, ints([[b] for b in range(B)])), H.make_desc(q, k, v)
+    new, lens = torch.zeros(B * cap, Hkv, 128, dtype=dt, device="cuda"), ints([cap] * B)
+    starts, begin, ws = ints([b * cap for b in range(B + 1)]), ints([0] * B), H.alloc_workspace(desc, H.HILL_SCORE_ATTN, 0)
+    got, want = (torch.zeros(B, cap, device="cuda") for _ in range(2))
+
+    def chain():
+        H.hill_paged_write(desc, pages, new, new, starts, begin)
+        H.hill_score(desc, q, k, lens, H.HILL_SCORE_ATTN, got, ws=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        chain()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            chain()
+        for i in range(20):
+            new.copy_(torch.randn(new.shape, generator=gen(50 + i), device="cuda"))
+            k.zero_()
+            graph.replay() if i % 2 else chain()
+            side.synchronize()
+            H.hill_score(desc, q, k, lens, H.HILL_SCORE_ATTN, want, ws=ws)     # the rows are there by now
+            H.hill_sync_status(side)
+            assert torch.equal(got, want)
+            assert torch.equal(k, new.view(B, cap, Hkv, 128).transpose(1, 2))
+
+
 def test_codes_bit_for_bit(H):
     """Codes and scales of rows at the borders: halfway values, the largest, tiny ones, all of one sign."""
     for dtype in DT:
