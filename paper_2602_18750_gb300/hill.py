@@ -212,10 +212,12 @@ def make_desc(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor | No
     v = v_cache if v_cache is not None else k_cache
     if tuple(v.shape) != tuple(k_cache.shape) or v.stride(-1) != 1 or v.dtype != q.dtype:
         raise ValueError("V must match K in shape and dtype")
-    return hill_desc(B, H, Hkv, d, cap, dt,
+    desc = hill_desc(B, H, Hkv, d, cap, dt,
                      q.stride(0), q.stride(1),
                      k_cache.stride(0), k_cache.stride(1), k_cache.stride(2),
                      v.stride(0), v.stride(1), v.stride(2))
+    desc.caches = k_cache.dtype, k_cache.shape, k_cache.stride(), v.stride()
+    return desc
 
 
 def hill_workspace_bytes(desc: hill_desc, mode: int, max_k: int) -> int:
@@ -575,6 +577,9 @@ def make_pages(k_pool: torch.Tensor, v_pool: torch.Tensor, table: torch.Tensor, 
     p.tensors = (k_pool, v_pool, table, scales)
     p.kv_heads, p.batch, p.dtype = k_pool.shape[1], table.shape[0], None if scales is not None else k_pool.dtype
     p.offsets, p.rows = torch.Size((p.batch + 1,)), torch.Size((p.batch,))
+    cap = p.cols * p.page
+    # the shapes of lens and accum: of sequences, and of KV heads
+    p.held = (p.rows, torch.Size((p.batch, cap))), (torch.Size((p.batch, p.kv_heads)), torch.Size((p.batch, p.kv_heads, cap)))
     return p
 
 
@@ -601,9 +606,10 @@ def hill_paged_attn(desc, q, pages, lens, sinks, window, out, accum=None, kvh=Fa
     """hill_window_attn over a cache in pages; desc is make_desc_paged's."""
     _fits(desc, pages)
     wp, wn = _ws(ws)
-    _check(load().hill_paged_attn(desc, _packed_rows(q, desc.made_for, "q"), pages, _typed(lens, _I32, "lens"), int(sinks), int(window), 1 if kvh else 0,
-                                  _typed(accum, _F32, "accum"), _typed(out, _F32, "out"), wp, wn, _stream(stream)),
-           "hill_paged_attn")
+    rows, held = pages.held[1 if kvh else 0]
+    _check(load().hill_paged_attn(desc, _packed_rows(q, desc.made_for, "q"), pages, _dense(lens, _I32, rows, "lens"), int(sinks), int(window), 1 if kvh else 0,
+                                  _dense(accum, _F32, held, "accum"), _dense(out, _F32, desc.made_for[1], "out"), wp, wn,
+                                  _stream(stream)), "hill_paged_attn")
 
 
 def hill_paged_write(desc, pages, k_new, v_new, starts, begin, stream=None) -> None:
@@ -621,11 +627,35 @@ def hill_paged_write(desc, pages, k_new, v_new, starts, begin, stream=None) -> N
                                    _dense(begin, _I32, pages.rows, "begin"), _stream(stream)), "hill_paged_write")
 
 
+def _cache(t, dtype, shape, strides, what: str):
+    """The pointer of a 16-bit cache that lies as the descriptor has it."""
+    if t is None or isinstance(t, int):
+        return t
+    if t.dtype is not dtype or t.shape != shape or (t.stride() != strides and any(
+            n > 1 and x != y for n, x, y in zip(shape, t.stride(), strides))):
+        raise ValueError(f"{what} must be {list(shape)} of {dtype}, strides {strides}, as the descriptor was made for; "
+                         f"got {list(t.shape)} of {t.dtype}, strides {t.stride()}")
+    return t.data_ptr()
+
+
 def hill_paged_read(desc, pages, row_begin, row_end, max_rows, k_cache, v_cache, stream=None) -> None:
-    """What positions [row_begin, row_end) of a cache in pages stand for, into 16-bit caches."""
+    """What positions [row_begin, row_end) of a cache in pages stand for, into 16-bit caches [B][Hkv][capacity][128].
+
+    desc is make_desc's of those caches, or make_desc_paged's: then the caches say how their rows lie."""
     _fits(desc, pages)
-    _check(load().hill_paged_read(desc, pages, _typed(row_begin, _I32, "row_begin"), _typed(row_end, _I32, "row_end"),
-                                  int(max_rows), _ptr(k_cache), _ptr(v_cache), _stream(stream)), "hill_paged_read")
+    caches = getattr(desc, "caches", None)
+    if caches is None:
+        if hasattr(desc, "made_for"):
+            desc = hill_desc.from_buffer_copy(desc)
+            desc.k_sb, desc.k_sh, desc.k_sn = k_cache.stride()[:3]
+            desc.v_sb, desc.v_sh, desc.v_sn = v_cache.stride()[:3]
+        caches = (_dtype_of(desc), torch.Size((desc.batch, desc.num_kv_heads, desc.capacity, 128)),
+                  (desc.k_sb, desc.k_sh, desc.k_sn, 1), (desc.v_sb, desc.v_sh, desc.v_sn, 1))
+    dtype, shape, ks, vs = caches
+    kp, vp = _cache(k_cache, dtype, shape, ks, "k_cache"), _cache(v_cache, dtype, shape, vs, "v_cache")
+    _check(load().hill_paged_read(desc, pages, _dense(row_begin, _I32, pages.rows, "row_begin"),
+                                  _dense(row_end, _I32, pages.rows, "row_end"), int(max_rows), kp, vp, _stream(stream)),
+           "hill_paged_read")
 
 
 def hill_selftest_wait(limit_us: int, stream=None) -> None:

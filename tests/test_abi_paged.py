@@ -255,6 +255,84 @@ def test_binding_of_pages(monkeypatch):
     refused(lambda: hill.hill_paged_read(other, p, bg, bg, 3, cache, cache, stream=1))
 
 
+@pytest.mark.parametrize("e4m3", [False, True], ids=["16bit", "e4m3"])
+def test_binding_of_pages_holds_shapes(monkeypatch, e4m3):
+    """Every tensor of a call over pages has the shape that the pages, the descriptor and kvh give it."""
+    torch = pytest.importorskip("torch")
+    from paper_2602_18750_gb300 import hill
+    B, HQ, HKV, page, n, cap, f16 = 2, 8, 4, 16, 5, 48, torch.float16
+    pool = torch.zeros(n, HKV, page, 128, dtype=torch.uint8 if e4m3 else f16)
+    p = hill.make_pages(pool, pool, torch.zeros(B, 3, dtype=torch.int32), torch.zeros(n, HKV, page, 2) if e4m3 else None)
+    q, ints = torch.zeros(B, HQ, 128, dtype=f16), lambda *shape: torch.zeros(*shape, dtype=torch.int32)
+    d = hill.make_desc_paged(q, p)
+    for kvh, rows in ((False, (B,)), (True, (B, HKV))):
+        good = dict(lens=ints(*rows), out=torch.zeros(B, HQ, 128), accum=torch.zeros(*rows, cap))
+
+        def attend(**kw):
+            a = {**good, **kw}
+            return lambda: hill.hill_paged_attn(d, q, p, a["lens"], 0, 5, a["out"], accum=a["accum"], kvh=kvh, stream=1)
+
+        reaches_the_library(monkeypatch, attend())
+        reaches_the_library(monkeypatch, attend(accum=None))
+        reaches_the_library(monkeypatch, attend(lens=good["lens"].data_ptr(), accum=good["accum"].data_ptr()))
+        for name, t in good.items():
+            for bad in others(t):
+                refused(attend(**{name: bad}))
+        other = (B, HKV) if rows == (B,) else (B,)
+        for bad in (dict(lens=ints(*other)), dict(lens=ints(B + 1)), dict(accum=torch.zeros(*other, cap)),
+                    dict(accum=torch.zeros(*rows, cap - 1)), dict(out=torch.zeros(B, HKV, 128)), dict(out=torch.zeros(B, HQ * 128))):
+            refused(attend(**bad))
+
+    strided = torch.zeros(B, cap, HKV, 128, dtype=f16).transpose(1, 2)
+    caches = (torch.zeros(B, HKV, cap, 128, dtype=f16), strided, torch.zeros(B, HKV, cap, 136, dtype=f16)[..., :128])
+    read = lambda desc, K, V, lo=ints(B), hi=ints(B): (lambda: hill.hill_paged_read(desc, p, lo, hi, 3, K, V, stream=1))
+    for K in caches:
+        for V in caches:
+            own = hill.make_desc(q, K, V)
+            reaches_the_library(monkeypatch, read(own, K, V))
+            reaches_the_library(monkeypatch, read(own, K.data_ptr(), V.data_ptr()))
+            reaches_the_library(monkeypatch, read(d, K, V))    # the caches say how they lie
+            for bad in caches:
+                if bad is not V:
+                    refused(read(own, K, bad))
+                if bad is not K:
+                    refused(read(own, bad, V))
+    K, V = caches[:2]
+    own = hill.make_desc(q, K, V)
+    for bad in (K.bfloat16(), K.float(), K[:1], K[:, :2], K[:, :, :-1], K[..., :64], K[0], torch.zeros(B, HKV, cap + 16, 128, dtype=f16)):
+        for desc in (own, d):
+            refused(read(desc, bad, V))
+            refused(read(desc, K, bad))
+    for bad in others(ints(B)):
+        refused(read(own, K, V, lo=bad))
+        refused(read(own, K, V, hi=bad))
+    refused(read(own, K, V, lo=ints(B + 1)))
+    one = torch.zeros(1, 1, cap, 128, dtype=f16)      # dimensions of one element may have any stride
+    p1 = hill.make_pages(pool[:, :1].contiguous(), pool[:, :1].contiguous(), ints(1, 3), p.tensors[3][:, :1].contiguous() if e4m3 else None)
+    d1 = hill.make_desc(torch.zeros(1, HQ, 128, dtype=f16), one, one)
+    reaches_the_library(monkeypatch, lambda: hill.hill_paged_read(d1, p1, ints(1), ints(1), 3, one.as_strided(one.shape, (8, 16, 128, 1)), one, stream=1))
+
+
+def test_reading_pages_takes_the_caches_strides(monkeypatch):
+    """With a descriptor of the pages the rows go where the caches have them; the descriptor itself stays as it is."""
+    torch = pytest.importorskip("torch")
+    from paper_2602_18750_gb300 import hill
+    pool = torch.zeros(5, 2, 16, 128, dtype=torch.bfloat16)
+    p = hill.make_pages(pool, pool, torch.zeros(3, 4, dtype=torch.int32))
+    d = hill.make_desc_paged(torch.zeros(3, 8, 128, dtype=torch.bfloat16), p)
+    K, V = torch.zeros(3, 2, 64, 128, dtype=torch.bfloat16), torch.zeros(3, 64, 2, 128, dtype=torch.bfloat16).transpose(1, 2)
+    at, seen = torch.zeros(3, dtype=torch.int32), []
+
+    class Library:
+        def hill_paged_read(self, desc, *a):
+            seen.append(((desc.k_sb, desc.k_sh, desc.k_sn), (desc.v_sb, desc.v_sh, desc.v_sn), desc.capacity))
+            return 0
+
+    monkeypatch.setattr(hill, "_lib", Library())
+    hill.hill_paged_read(d, p, at, at, 3, K, V, stream=1)
+    assert seen == [(K.stride()[:3], V.stride()[:3], 64)] and (d.k_sb, d.k_sn, d.v_sh) == (0, 0, 0)
+
+
 # ---------------------------------------------------------------- the plain forms themselves
 def test_plain_prompt_is_softmax_over_what_is_seen():
     torch = pytest.importorskip("torch")
