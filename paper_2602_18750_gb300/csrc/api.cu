@@ -1331,7 +1331,7 @@ hill_status check_pages(const hill_desc* d, const hill_pages* p) {
   if ((p->pages > 0 && (!p->k || !p->v)) || (p->cols > 0 && d->batch > 0 && !p->table)) return HILL_ERR_INVALID_ARG;
   if (!aligned16(p->k) || !aligned16(p->v) || !aligned16(p->scales)) return HILL_ERR_INVALID_ARG;
   if (p->page % 16) return HILL_ERR_UNSUPPORTED;
-  if (p->page > kRowsMax / 2 || (int64_t)(p->pages + 1) * d->num_kv_heads > kRowsMax || (int64_t)p->cols * p->page > kRowsMax)
+  if (p->page > kRowsMax / 2 || ((int64_t)p->pages + 1) * d->num_kv_heads > kRowsMax || (int64_t)p->cols * p->page > kRowsMax)
     return HILL_ERR_UNSUPPORTED;
   return HILL_OK;
 }

@@ -143,6 +143,20 @@ def test_paged_refusals(lib):
         assert write(_desc(), pages(pages=0, k=None, v=None), rows()) == CUDA   # (no page is there: every row is dropped)
 
 
+@pytest.mark.parametrize("count", [(1 << 29) - 1, 1 << 29, (1 << 30) - 1, (1 << 31) - 2, (1 << 31) - 1])
+def test_pools_of_more_pages_than_are_numbered(lib, count):
+    """(pages + 1) x KV heads is at most 2^30, up to the largest count that the field holds."""
+    from paper_2602_18750_gb300 import hill
+    from paper_2602_18750_gb300.hill import HILL_ERR_UNSUPPORTED as UNS
+    p = lambda: ctypes.byref(pages(pages=count))
+    rows = hill.hill_rows(k=FAKE, v=FAKE, k_st=256, k_sh=128, v_st=256, v_sh=128, rows=0)   # (nothing to do where it is not refused)
+    fits = (count + 1) * 2 <= 1 << 30
+    assert lib.hill_paged_write(ctypes.byref(_desc()), p(), ctypes.byref(rows), FAKE, FAKE, None) == (0 if fits else UNS)
+    assert lib.hill_paged_read(ctypes.byref(_desc()), p(), FAKE, FAKE, 0, FAKE, FAKE, None) == (0 if fits else UNS)
+    if not fits:
+        assert lib.hill_paged_attn(ctypes.byref(_desc()), FAKE, p(), FAKE, 0, 5, 0, None, FAKE, FAKE, 1 << 40, None) == UNS
+
+
 # ---------------------------------------------------------------- the binding
 def refused(f):
     with pytest.raises(ValueError):
