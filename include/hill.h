@@ -520,7 +520,8 @@ hill_status hill_paged_write(const hill_desc* desc, const hill_pages* pages, con
 
 /* Positions [row_begin[b], row_end[b]) (clamped to the table and to desc's capacity) of every KV
  * head into 16-bit caches of desc's strides, for the calls that read those: copied, or
- * code * scale rounded to desc's type.  max_rows bounds row_end - row_begin over b. */
+ * code * scale rounded to desc's type.  max_rows bounds row_end - row_begin over b.  (A stride
+ * of 0, of rows that would lie in one place, is HILL_ERR_INVALID_ARG.) */
 hill_status hill_paged_read(const hill_desc* desc, const hill_pages* pages, const int32_t* row_begin,
                             const int32_t* row_end, int32_t max_rows, void* k_cache, void* v_cache, void* stream);
 

@@ -1485,6 +1485,10 @@ hill_status hill_paged_read(const hill_desc* desc, const hill_pages* pages, cons
   if (s != HILL_OK) return s;
   if (!row_begin || !row_end || max_rows < 0 || !k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache))
     return HILL_ERR_INVALID_ARG;
+  // (a descriptor without strides of a cache would put all rows in one place)
+  if ((desc->capacity > 1 && (!desc->k_sn || !desc->v_sn)) || (desc->num_kv_heads > 1 && (!desc->k_sh || !desc->v_sh)) ||
+      (desc->batch > 1 && (!desc->k_sb || !desc->v_sb)))
+    return HILL_ERR_INVALID_ARG;
   DeviceInfo di;
   PagesArgs a = pages_args(desc, pages, nullptr);
   a.cap = std::min(a.cap, desc->capacity);

@@ -157,6 +157,17 @@ def test_pools_of_more_pages_than_are_numbered(lib, count):
         assert lib.hill_paged_attn(ctypes.byref(_desc()), FAKE, p(), FAKE, 0, 5, 0, None, FAKE, FAKE, 1 << 40, None) == UNS
 
 
+def test_reading_pages_into_one_place_is_refused(lib):
+    """A descriptor of the pages, or any without strides of a cache, does not say where rows go."""
+    from paper_2602_18750_gb300.hill import HILL_ERR_INVALID_ARG as INV, HILL_OK as OK
+    read = lambda **kw: lib.hill_paged_read(ctypes.byref(_desc(**kw)), ctypes.byref(pages()), FAKE, FAKE, 0, FAKE, FAKE, None)
+    assert read() == OK
+    for stride in ("k_sb", "k_sh", "k_sn", "v_sb", "v_sh", "v_sn"):
+        assert read(**{stride: 0}) == INV, stride
+    assert read(batch=1, k_sb=0, v_sb=0) == OK and read(num_kv_heads=1, k_sh=0, v_sh=0) == OK
+    assert read(capacity=1, k_sn=0, v_sn=0) == OK
+
+
 # ---------------------------------------------------------------- the binding
 def refused(f):
     with pytest.raises(ValueError):
