@@ -437,6 +437,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) hill_score_tc_kernel(const __gr
           const int w = x / kTcU, u = x % kTcU;
           const int gi = (ui + w) * kTcU + u;
           if (w >= nb || gi >= nkv) continue;
+          tc_tied(v[x]);
           const int g = a.goff + gi;
           const float* sqb = a.sq + (int64_t)b * H + g * a.G;
           if constexpr (RAW) {

@@ -63,7 +63,7 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
                : "memory");
 }
 // 16 consecutive columns of this warp's 32 lanes: thread i gets lane i's
-// values once tc_wait_ld() has returned
+// values, which are there after tc_landed, or after tc_wait_ld and then tc_tied
 __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
@@ -74,6 +74,11 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
       : "memory");
 }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// For loads that one tc_wait_ld has waited for: no use of r moves ahead of this (and so of the wait).
+__device__ __forceinline__ void tc_tied(uint32_t (&r)[16]) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
 
 // 32 consecutive columns of this warp's 32 lanes, in the background: the values are there after tc_landed.
 __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&r)[32]) {
