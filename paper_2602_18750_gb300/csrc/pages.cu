@@ -7,13 +7,13 @@
 // amax / 448, so rows that a program quantised there and rows written here are the same, bit for bit.)
 //
 // Bound by HBM: a row's 256 bytes in, 256 or 132 out.  8 lanes cover a row with
-// 32 bytes each, and a lane takes kU rows of K and of V, all loaded before the first is used.  What
-// says where a row goes -- its sequence (a count over the starts, by the row's 8 lanes), the sequence's
-// first position and its page -- is a chain of three loads, under way beside the row's own.
-// Measured (us in a graph, 8 KV heads, one row / 2 / 4 to a lane): writes of 16 tokens 3.0 / 3.8 / 5.2 (E4M3 3.1 / 3.9 /
-// 5.1), 1024 4.1 / 4.3 / 5.5 (3.7 / 4.0 / 5.2), 2048 6.6 / 5.7 / 5.9 (5.4 / 4.8 / 5.5), 16K 22.9 / 23.2 / 26.8 (17.6 / 18.1 /
-// 23.5); reads (2 / 4 rows) 16 tokens 2.5 / 2.8, 1024 3.6 / 5.0, 16K 21.8 / 22.5.  Prompts of 4 x up to 16K tokens into an
-// E4M3 cache and back 107 us, 6.0 TB/s.
+// 32 bytes each.  What says where a new row goes -- its sequence (a count over the starts, by the row's 8 lanes), the
+// sequence's first position and its page -- is a chain of three loads, under way beside the row's own.  A lane of a write has
+// one row of K and of V, of a read two, all loaded before the first is used.
+// Measured (us in a graph, 8 KV heads; writes with one row / 2 / 4 to a lane): writes of 16 tokens 3.0 / 3.8 / 5.2 (E4M3
+// 3.1 / 3.9 / 5.1), 1024 4.1 / 4.3 / 5.5 (3.7 / 4.0 / 5.2), 2048 6.6 / 5.7 / 5.9 (5.4 / 4.8 / 5.5), 16K 22.9 / 23.2 / 26.8 (17.6 /
+// 18.1 / 23.5); reads (2 / 4 rows) 16 tokens 2.5 / 2.8, 1024 3.6 / 5.0, 16K 21.8 / 22.5.  Prompts of 4 x up to 16K tokens
+// into an E4M3 cache and back 107 us, 6.0 TB/s.
 #include <type_traits>
 
 #include "hill_internal.h"
@@ -57,8 +57,8 @@ __device__ __forceinline__ Place place_of(const PagesArgs& a, int b, int p) {
   return Place{page >= 0 && page < a.pages ? page : -1, p - c * a.page};
 }
 
-// Row r of the new ones is (token r / Hkv, KV head r % Hkv); 8 lanes take kU consecutive rows.
-template <int DT, bool F8, int kU>
+// Row r of the new ones is (token r / Hkv, KV head r % Hkv); 8 lanes take one.
+template <int DT, bool F8>
 __global__ void __launch_bounds__(kWarps * 32) hill_paged_write_kernel(const PagesArgs a) {
   const int lane = threadIdx.x & 31, l8 = lane & 7;
   pdl_wait();
@@ -66,74 +66,58 @@ __global__ void __launch_bounds__(kWarps * 32) hill_paged_write_kernel(const Pag
   // rows the scoring calls read before their own wait.  (Codes are read after it by every call.)
   if (F8) pdl_launch_dependents();
   const int64_t rows = (int64_t)a.rows * a.Hkv;
-  const int64_t r0 = (((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * 4 + (lane >> 3)) * kU;
-  Dims16 raw[kU][2];
-  int tok[kU], head[kU];
-#pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    const int64_t r = r0 + u;
-    tok[u] = r >= rows ? -1 : r >> 32 ? (int)(r / a.Hkv) : (int)((uint32_t)r / (uint32_t)a.Hkv);   // (mostly the short division)
-    head[u] = r < rows ? (int)(r - (int64_t)tok[u] * a.Hkv) : 0;
-    raw[u][0] = raw[u][1] = Dims16{};
-    if (tok[u] < 0) continue;
-    raw[u][0] = load_dims(static_cast<const uint16_t*>(a.k) + tok[u] * a.k_sn + head[u] * a.k_sh + l8 * 16);
-    raw[u][1] = load_dims(static_cast<const uint16_t*>(a.v) + tok[u] * a.v_sn + head[u] * a.v_sh + l8 * 16);
+  const int64_t r = ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * 4 + (lane >> 3);
+  const int tok = r >= rows ? -1 : r >> 32 ? (int)(r / a.Hkv) : (int)((uint32_t)r / (uint32_t)a.Hkv);   // (mostly the short division)
+  const int head = tok >= 0 ? (int)(r - (int64_t)tok * a.Hkv) : 0;
+  Dims16 raw[2] = {Dims16{}, Dims16{}};
+  if (tok >= 0) {
+    raw[0] = load_dims(static_cast<const uint16_t*>(a.k) + tok * a.k_sn + head * a.k_sh + l8 * 16);
+    raw[1] = load_dims(static_cast<const uint16_t*>(a.v) + tok * a.v_sn + head * a.v_sh + l8 * 16);
   }
-  // the sequence of the first row's token: how many sequences end at or before it
-  const int t0 = max(tok[0], 0);
+  // the token's sequence: how many sequences end at or before it
   int b = 0;
-  for (int i = l8; i < a.B; i += 8) b += a.starts[i + 1] <= t0;
+  for (int i = l8; i < a.B; i += 8) b += a.starts[i + 1] <= tok;
 #pragma unroll
   for (int o = 4; o > 0; o >>= 1) b += __shfl_xor_sync(0xffffffffu, b, o);
-  int known = -1;
   Place at{-1, 0};
-#pragma unroll
-  for (int u = 0; u < kU; ++u) {
-    if (tok[u] >= 0 && tok[u] != known) {
-      known = tok[u];
-      while (b < a.B && a.starts[b + 1] <= known) ++b;
-      at.page = -1;
-      if (b < a.B && known >= a.starts[b]) {   // (rows behind the last sequence go nowhere)
-        const int64_t p = (int64_t)a.begin[b] + (known - a.starts[b]);
-        if (p >= 0 && p < a.cap) at = place_of(a, b, (int)p);
-        if (at.page < 0 && l8 == 0) raise_error(a.err, kErrDevArg);
-      }
-    }
-    const bool there = tok[u] >= 0 && at.page >= 0;
-    const int64_t row = there ? at.row(a, head[u]) : 0;
-    [[maybe_unused]] float scale[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t v[8] = {raw[u][i].a.x, raw[u][i].a.y, raw[u][i].a.z, raw[u][i].a.w,
-                             raw[u][i].b.x, raw[u][i].b.y, raw[u][i].b.z, raw[u][i].b.w};
-      if constexpr (!F8) {
-        if (there) {
-          uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(i ? a.pv : a.pk) + row * kHeadDim + l8 * 16);
-          dst[0] = raw[u][i].a;
-          dst[1] = raw[u][i].b;
-        }
-      } else {
-        uint32_t m = absmax2<DT>(absmax2<DT>(absmax2<DT>(v[0], v[1]), absmax2<DT>(v[2], v[3])),
-                                 absmax2<DT>(absmax2<DT>(v[4], v[5]), absmax2<DT>(v[6], v[7])));
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) m = absmax2<DT>(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const float2 p = unpack2<DT>(m);
-        const float2 rs = row_scale(fmaxf(p.x, p.y));
-        scale[i] = rs.y;
-        uint32_t code[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 x = unpack2<DT>(v[2 * e]), y = unpack2<DT>(v[2 * e + 1]);
-          code[e] = e4m3x2(__fmul_rn(x.x, rs.x), __fmul_rn(x.y, rs.x)) |
-                    (e4m3x2(__fmul_rn(y.x, rs.x), __fmul_rn(y.y, rs.x)) << 16);
-        }
-        if (there)
-          *reinterpret_cast<uint4*>(static_cast<uint8_t*>(i ? a.pv : a.pk) + row * kHeadDim + l8 * 16) =
-              uint4{code[0], code[1], code[2], code[3]};
-      }
-    }
-    if (F8 && there && l8 == 0) a.scales[row] = float2{scale[0], scale[1]};
+  if (tok >= 0 && b < a.B && tok >= a.starts[b]) {   // (rows before the first sequence or behind the last go nowhere)
+    const int64_t p = (int64_t)a.begin[b] + tok - a.starts[b];
+    if (p >= 0 && p < a.cap) at = place_of(a, b, (int)p);
+    if (at.page < 0 && l8 == 0) raise_error(a.err, kErrDevArg);
   }
+  const bool there = at.page >= 0;
+  const int64_t row = there ? at.row(a, head) : 0;
+  [[maybe_unused]] float scale[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t v[8] = {raw[i].a.x, raw[i].a.y, raw[i].a.z, raw[i].a.w, raw[i].b.x, raw[i].b.y, raw[i].b.z, raw[i].b.w};
+    if constexpr (!F8) {
+      if (there) {
+        uint4* dst = reinterpret_cast<uint4*>(static_cast<uint16_t*>(i ? a.pv : a.pk) + row * kHeadDim + l8 * 16);
+        dst[0] = raw[i].a;
+        dst[1] = raw[i].b;
+      }
+    } else {
+      uint32_t m = absmax2<DT>(absmax2<DT>(absmax2<DT>(v[0], v[1]), absmax2<DT>(v[2], v[3])),
+                               absmax2<DT>(absmax2<DT>(v[4], v[5]), absmax2<DT>(v[6], v[7])));
+#pragma unroll
+      for (int o = 4; o > 0; o >>= 1) m = absmax2<DT>(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const float2 p = unpack2<DT>(m);
+      const float2 rs = row_scale(fmaxf(p.x, p.y));
+      scale[i] = rs.y;
+      uint32_t code[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 x = unpack2<DT>(v[2 * e]), y = unpack2<DT>(v[2 * e + 1]);
+        code[e] = e4m3x2(__fmul_rn(x.x, rs.x), __fmul_rn(x.y, rs.x)) |
+                  (e4m3x2(__fmul_rn(y.x, rs.x), __fmul_rn(y.y, rs.x)) << 16);
+      }
+      if (there)
+        *reinterpret_cast<uint4*>(static_cast<uint8_t*>(i ? a.pv : a.pk) + row * kHeadDim + l8 * 16) =
+            uint4{code[0], code[1], code[2], code[3]};
+    }
+  }
+  if (F8 && there && l8 == 0) a.scales[row] = float2{scale[0], scale[1]};
 }
 
 // Codes -> values of the 16-bit type: the float32 product of code and scale, rounded once.
@@ -203,10 +187,9 @@ __global__ void __launch_bounds__(kWarps * 32) hill_paged_read_kernel(const Page
 
 template <int DT, bool F8>
 cudaError_t launch_write_t(const PagesArgs& a, cudaStream_t st) {
-  constexpr int kU = 1, per = kWarps * 4 * kU;
+  constexpr int per = kWarps * 4;
   const int64_t rows = (int64_t)a.rows * a.Hkv;
-  return launch_pdl(hill_paged_write_kernel<DT, F8, kU>, dim3((unsigned)((rows + per - 1) / per)), dim3(kWarps * 32), 0, st, 0,
-                    a);
+  return launch_pdl(hill_paged_write_kernel<DT, F8>, dim3((unsigned)((rows + per - 1) / per)), dim3(kWarps * 32), 0, st, 0, a);
 }
 
 template <int DT, bool F8>
