@@ -1253,13 +1253,7 @@ hill_status make_rows_map(int dtype, const void* p, int heads, int64_t rows, int
 // What both calls over prompts take; the maps (v may be NULL), keys by tiles of tile_keys.
 hill_status prompt_args(const hill_packed* d, const void* q, const void* k, const void* v, const int32_t* q_start,
                         const int32_t* k_start, int32_t sinks, int32_t window, int tile_keys, PromptArgs* a) {
-  a->q = q;
-  a->k = k;
   a->v = v;
-  a->q_st = d->q_st;
-  a->q_sh = d->q_sh;
-  a->k_st = d->k_st;
-  a->k_sh = d->k_sh;
   a->v_st = d->v_st;
   a->v_sh = d->v_sh;
   a->q_start = q_start;
@@ -1275,9 +1269,9 @@ hill_status prompt_args(const hill_packed* d, const void* q, const void* k, cons
   a->passes = cdiv(a->G, a->q_heads);
   a->sinks = std::min(sinks, kRowsMax);
   a->window = std::min(window, kRowsMax);
-  hill_status s = make_rows_map(d->dtype, q, a->H, a->q_rows, a->q_sh, a->q_st, a->q_heads, a->q_tokens, &a->qmap);
+  hill_status s = make_rows_map(d->dtype, q, a->H, a->q_rows, d->q_sh, d->q_st, a->q_heads, a->q_tokens, &a->qmap);
   // (without keys nothing is read through these)
-  if (s == HILL_OK) s = make_rows_map(d->dtype, d->k_rows ? k : q, a->Hkv, a->k_rows, a->k_sh, a->k_st, 1, tile_keys, &a->kmap);
+  if (s == HILL_OK) s = make_rows_map(d->dtype, d->k_rows ? k : q, a->Hkv, a->k_rows, d->k_sh, d->k_st, 1, tile_keys, &a->kmap);
   if (s == HILL_OK && v)
     s = make_rows_map(d->dtype, d->k_rows ? v : q, a->Hkv, a->k_rows, a->v_sh, a->v_st, 1, tile_keys, &a->vmap);
   return s;

@@ -207,10 +207,8 @@ struct BlockInfo;   // importance.cu
 struct PromptArgs {
   CUtensorMap qmap, kmap, vmap;   // 3-D (head dimension, head, row), 128-byte swizzle; boxes of 64 dims x q_heads x
                                   // q_tokens query rows, 64 dims x 1 x a tile of keys
-  const void* q;
-  const void* k;
-  const void* v;
-  int64_t q_st, q_sh, k_st, k_sh, v_st, v_sh;
+  const void* v;                  // attention: for values that are not finite
+  int64_t v_st, v_sh;
   const int32_t* q_start;         // [B + 1] first row of each sequence
   const int32_t* k_start;
   int B, H, Hkv, G, q_rows, k_rows;
