@@ -455,3 +455,30 @@ def test_importance_of_a_key_at_minus_infinity(H, heads, dtype, low):
     _, got, _ = run_importance(H, c, 0, ALL, ALL, True, 300, lse)
     H.hill_sync_status()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("kvh", [False, True], ids=["seq", "kvh"])
+def test_importance_as_the_first_weights_of_an_insert(H, kvh):
+    """Prompts go into bounded caches with the weights that their tokens received, as they lie; the next tokens take the
+    slots of the smallest."""
+    B, T, HQ, HKV, sinks, more = 2, 60, 8, 2, 4, 6
+    c = Case(H, [(T, 0)] * B, HQ, HKV, seed=60)
+    c.attend(0, ALL)
+    rows = (B, HKV) if kvh else (B,)
+    w = torch.zeros(*rows, T, device="cuda")
+    H.hill_prompt_importance(c.desc, c.q, c.k, c.lse, c.qs, c.ks, 0, ALL, ALL, w, kvh=kvh, ws=H.alloc_prompt_workspace(c.desc))
+    cache = H.BoundedCache(B, HQ, HKV, T + sinks, c.dt, sinks=sinks, kvh=kvh, max_new=T)
+    new = [x.view(B, T, HKV, 128).transpose(1, 2) for x in (c.k, c.v)]
+    cache.insert(*new, w_new=w)
+    H.hill_sync_status()
+    assert torch.equal(cache.accum[..., :T], w) and torch.all(cache.slots == torch.arange(T, device="cuda"))
+    for x, held in zip(new, (cache.K, cache.V)):
+        assert torch.equal(held[:, :, :T], x)
+    assert (w.sum(-1) - T * HQ / (HKV if kvh else 1)).abs().max() < 1e-2      # every query gives 1 per head, to 2^-16
+    # the free slots first, then the least weights behind the sinks; ties go to the later slot
+    cache.insert(*(x[:, :, :sinks + more].contiguous() for x in new), w_new=torch.full((*rows, sinks + more), 1e6, device="cuda"))
+    H.hill_sync_status()
+    got = cache.slots.flatten()[:w[..., 0].numel() * (sinks + more)].view(*rows, sinks + more).cpu()
+    for at in np.ndindex(rows):
+        order = sorted(range(sinks, T), key=lambda j: (-float(w[at][j]), j))
+        assert got[at].tolist() == list(range(T, T + sinks)) + sorted(order[-more:])
