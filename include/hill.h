@@ -28,7 +28,9 @@
  *   writes them afterwards.  Ordinary kernels and copies satisfy this.  What
  *   an earlier call of this library writes (scores, accum, hits, idx, count,
  *   the E4M3 shadow, workspaces) is read after the wait, and outputs and
- *   workspace are written only after it.
+ *   workspace are written only after it.  The calls that write 16-bit K rows
+ *   (hill_cache_insert, hill_cache_read_q4, hill_paged_read, hill_paged_write
+ *   into 16-bit pools) do not trigger their dependents early.
  * - Host-side validation failures return immediately and launch nothing.
  *   Launch failures return HILL_ERR_CUDA.  Conditions only visible on the
  *   device (a budget larger than max_k, a selected index outside the cache, a
@@ -47,7 +49,8 @@
  *   [0, cap] on the device.  Entries of scores/accum at j >= lens[b] are not
  *   touched.  k[b] is clamped to [0, lens[b]].
  * - Supported: head_dim 128; any H and Hkv with H a multiple of Hkv (MHA,
- *   GQA with any group size G = H / Hkv, MQA); B <= 512; fp16 or bf16 q/K/V.
+ *   GQA with any group size G = H / Hkv, MQA); B <= 512; fp16 or bf16 q/K/V;
+ *   capacities up to 385024 tokens (the keys that a selection holds on chip).
  *   Groups of more than 8 query heads are scored in passes of at most 8 over
  *   the same keys, except with at most 4 KV heads (MQA-like), where one pass
  *   scores up to 32 query heads of each KV head from every key tile; the

@@ -13,12 +13,16 @@
 //    sum (p scale_v) codes.  The query is fp16 under a power of two that puts its largest element at 2^14;
 //    p scale_v goes in as a high part and a residual under a power of two F of each head (window.cu's header
 //    has the errors: 2^-21 of itself and 2^-32 of the largest).
+//  16 bits    p goes in as a high part and a residual of V's type, off by at most 2^-16 of itself in bf16, and in fp16 by
+//    2^-22 and 2^-32 of the head's largest.
 //
 // Mathematics of a tile: S = K q^T with tokens as rows (m16n8k16), p = 2^(z - m) with a running maximum that is
 // raised only where a weight passes 2^15, p transposed by 8x8 blocks to be the column operand of O^T += V^T p.
 //
-// Bound by HBM: 512 bytes per position and KV head in 16 bits, 264 in E4M3.  8 ragged sequences of up to 32K tokens of 8 KV
-// heads in 16 bits 138 us, 6.7 TB/s; 4 of up to 32K tokens of 32 heads in E4M3, with their importance, 153 us, 5.9 TB/s.
+// Long rows are bound by HBM: 512 bytes per position and KV head in 16 bits, 264 in E4M3.  8 ragged sequences of up to 32K
+// tokens of 8 KV heads in 16 bits 138 us, 6.7 TB/s; 4 of up to 32K tokens of 32 heads in E4M3, with their importance, 153 us,
+// 5.9 TB/s.  Short ones are bound by latency: 4001 tokens of 8 KV heads 8.6 us in a graph (E4M3 8.9) for 2.4 (1.2) of bytes,
+// two tiles to a warp between the chain lengths, table, first boxes and two merges; no pipe is busy.
 #include <cooperative_groups.h>
 
 #include <algorithm>
@@ -808,7 +812,8 @@ constexpr int kSizes = 5;   // clusters of 1, 2, 4, 8, 16 CTAs
 // Clusters or the list, by the rule of window.cu.  Measured here, list / clusters (us, pages of 16, 16 bits and E4M3): 4000
 // tokens of 8 KV heads 10.2 / 8.8, 9.9 / 8.6; 32768 of 8 29.0 / 28.4, 21.1 / 22.8; 4 x 8000 of 8 27.6 / 25.7, 18.9 / 17.4;
 // 8 x 2000 of 8 18.4 / 15.5, 17.0 / 13.0; 2 x 5000 of 32 32.8 / 30.8, 21.5 / 19.9; 32768 of 4 20.7 / 19.5, 18.5 / 16.8; 30000 of 1
-// 16.0 / 18.4 (the list is taken), 15.9 / 15.0; 32 heads of one KV head 13000 13.4 / 12.6, 13.4 / 11.5.
+// 16.0 / 18.4 (the list is taken), 15.9 / 15.0; 32 heads of one KV head 13000 13.4 / 12.6, 13.4 / 11.5.  (The constants are
+// those of 16-bit tiles, and an E4M3 tile is half the bytes: at 32768 of 8 in E4M3 the rule takes the slower.)
 constexpr double kIdleRounds = 1.45, kIdleRounds16 = 2.4, kIdleRoundsFew = 5.5;
 constexpr int kFewUnits = 8, kStreamCtas = 64, kStreamRounds = 16;
 

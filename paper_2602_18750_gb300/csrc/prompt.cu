@@ -31,7 +31,7 @@
 // Few rows behind many keys leave most SMs without a unit: then a cluster of CTAs shares each, every CTA an even part of
 // its key tiles, and they merge their (maximum, sum, O) through one another's shared memory, a CTA every so many rows.
 // 32 heads in 8 groups, one CTA to a unit / clusters (us): 2 x 8 tokens behind 9000 110 / 46, one token behind 16000
-// 185 / 36, 200 tokens behind 4000 65 / 34; in two parts 64 tokens behind 1000 27.7 / 29.9, behind 500 21.6 / 29.8.
+// 185 / 36 (29 where K and V are in L2), 200 tokens behind 4000 65 / 34; in two parts 64 tokens behind 1000 27.7 / 29.9, behind 500 21.6 / 29.8.
 //
 // The running maximum m of a row is set 7 below its largest logit (base 2) and raised only when the weights of a
 // tile sum to more than 2^15: no maximum is searched for, and O is not rescaled, until then.  Since S of a tile is
